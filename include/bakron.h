@@ -54,7 +54,9 @@ typedef enum {
   BAKRON_ERR_NONFINITE = 6      /* NaN/Inf met while rounding                 */
 } bakron_status;
 
-typedef enum { BAKRON_F32 = 0, BAKRON_BF16 = 1 } bakron_dtype;
+/* E4M3: 8-bit floats of 4 exponent and 3 fraction bits, largest value 448; only where
+ * an entry point names it. */
+typedef enum { BAKRON_F32 = 0, BAKRON_BF16 = 1, BAKRON_E4M3 = 2 } bakron_dtype;
 
 /* Bytes of the opaque factor buffer for an m x n problem (L^A, L^B and the
  * RevCholesky diagonals, padded to the kernels' tile size). */
@@ -464,6 +466,132 @@ int bakron_diag_leaf_chain(const void* W, int wdtype, const void* factors,
                            uint8_t* codes, float* scales, float* zeros,
                            void* workspace, size_t workspace_bytes,
                            double* cycles_per_step, void* stream);
+
+/*
+ * Running and scoring a quantised model (no counterpart in the paper): the product with
+ * a weight as the solve leaves it, the norm before it, and the log probabilities after
+ * it with their gradient, which gives the output-side samples of the Hessian factors.
+ * Rows are tokens; every row stride is in elements.  These calls are asynchronous on
+ * `stream` unless stated otherwise, and a call of zero rows does nothing.
+ *
+ * bakron_pack_weight -- lay a quantised weight out for bakron_linear.
+ *   codes    device, m rows of n uint8 codes 0..qmax, row stride ldc (>= n)
+ *   scales, zeros  device, m x G fp32 (G = 1, or n / group_size): code c of row i and
+ *            group g stands for s[i, g] (c - z[i, g]), as bakron_solve and
+ *            bakron_solve_with_grid leave it; each zero an integer in [0, qmax]
+ *   qmax     1..255; up to 15 a code takes 4 bits, above that 8
+ *   group_size  0 (one grid per row), or a multiple of 32 that divides n
+ *   packed   device, bakron_packed_bytes(m, n, qmax, group_size) bytes, 16-byte aligned
+ * Synchronises `stream`; BAKRON_ERR_INVALID_ARG also where a code is above qmax or a
+ * zero is no integer in [0, qmax] (found on the device; `packed` is then of no use).
+ * The buffer holds the weight alone: it may be copied, and used by any number of calls.
+ */
+size_t bakron_packed_bytes(int m, int n, int qmax, int group_size);
+int bakron_pack_weight(const uint8_t* codes, int64_t ldc, const float* scales,
+                       const float* zeros, int m, int n, int qmax, int group_size,
+                       void* packed, size_t packed_bytes, void* stream);
+
+typedef enum {
+  BAKRON_NO_ACTIVATION = 0,
+  BAKRON_RELU = 1,   /* max(v, 0) */
+  BAKRON_SILU = 2,   /* v / (1 + exp(-v)) */
+  BAKRON_GELU = 3    /* v (1 + erf(v / sqrt(2))) / 2 */
+} bakron_activation;
+
+/*
+ * bakron_linear -- y = act(x What^T + bias) + residual for `rows` tokens, What the m x n
+ * weight of a packed buffer.
+ *   x        device, rows x n, BAKRON_BF16 or BAKRON_E4M3, row stride ldx (>= n)
+ *   xscales  device, `rows` fp32: token t stands for xscales[t] x[t], as
+ *            bakron_rmsnorm leaves it; NULL: 1
+ *   packed, m, n, qmax, group_size  the weight, as given to bakron_pack_weight
+ *   bias     device, m fp32, or NULL
+ *   residual device, rows x m of y's type, row stride ldr (>= m), or NULL; may be y
+ *   y        device, rows x m, BAKRON_BF16 or BAKRON_F32, row stride ldy (>= m); must not
+ *            overlap x
+ *   workspace device, >= bakron_linear_workspace_bytes(...) bytes, 16-byte aligned (may
+ *            be NULL where that is 0); its first word is the status
+ *   sync     nonzero: synchronise `stream` and return the device status
+ *            (BAKRON_ERR_TIMEOUT: a bounded wait ran out, y is undefined); zero:
+ *            bakron_read_status(workspace, stream) returns it later, where there is one
+ * The codes' integers c - z and the tokens' values meet on the tensor cores, where both
+ * are exact; sums are fp32, a group's scale multiplies its sum, and y is rounded once.
+ * A row of x that holds a NaN or an infinity affects its own row of y alone.
+ */
+size_t bakron_linear_workspace_bytes(const void* x, int xdtype, int rows, int64_t ldx, int n,
+                                     int qmax);
+int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float* xscales,
+                  const void* packed, int m, int n, int qmax, int group_size,
+                  const float* bias, int activation, const void* residual, int64_t ldr,
+                  void* y, int ydtype, int64_t ldy, void* workspace, size_t workspace_bytes,
+                  int sync, void* stream);
+
+/*
+ * bakron_rmsnorm -- h = x + residual, y = weight * h / sqrt(mean(h^2) + eps), row by row.
+ *   x, residual  device, rows x d, `dtype` BAKRON_F32 or BAKRON_BF16; residual may be NULL
+ *   weight   device, d values, wdtype BAKRON_F32 or BAKRON_BF16
+ *   sum      device, rows x d of `dtype`, or NULL: h, rounded; may be x or residual
+ *   y        device, rows x d of `dtype`, or of BAKRON_E4M3 with
+ *   scales   device, `rows` fp32: max |y| / 448 of the row (1 where that is 0); y then
+ *            holds y / scale, rounded to nearest
+ *   d        1..65536
+ * All in fp32; y comes from the unrounded h.  A row that holds a NaN or an infinity
+ * gives NaNs (in 8 bits: a NaN scale).
+ */
+int bakron_rmsnorm(const void* x, int dtype, int rows, int d, int64_t ldx,
+                   const void* residual, int64_t ldr, const void* weight, int wdtype,
+                   float eps, void* sum, int64_t lds, void* y, int ydtype, int64_t ldy,
+                   float* scales, void* stream);
+
+/*
+ * bakron_rmsnorm_backward -- the gradients of y = weight * h * rho, rho = 1 / sqrt(mean(h^2) + eps):
+ *   dx = rho (w dy - h rho^2 mean(w dy h)) + dsum,   dw = sum over rows of dy h rho
+ *   dy, h    device, rows x d of `dtype` (h: what the norm was taken of)
+ *   dsum     device, rows x d of `dtype`, or NULL: the gradient that reaches h past the
+ *            norm (dx is the gradient of both x and residual)
+ *   dx       device, rows x d of `dtype`; may be dsum, must not overlap dy or h
+ *   dw       device, d fp32, written (zeros for no rows); summed in a fixed order
+ *   workspace device, >= bakron_rmsnorm_backward_workspace_bytes(rows, d) bytes, 16-byte
+ *            aligned
+ */
+size_t bakron_rmsnorm_backward_workspace_bytes(int rows, int d);
+int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh,
+                            int dtype, int rows, int d, const void* weight, int wdtype,
+                            float eps, const void* dsum, int64_t ldds, void* dx, int64_t lddx,
+                            float* dw, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * bakron_token_logprobs -- of each row of logits l (rows x v, BAKRON_F32 or BAKRON_BF16):
+ *   lse      rows fp32: log sum_j exp(l_j)
+ *   logp     rows fp32: l[target] - lse; 0 where the target is outside 0..v-1 (a position
+ *            that is not scored); NULL if targets is NULL
+ *   entropy  rows fp32: -sum_j p_j log p_j, p = exp(l - lse)
+ *   top_logp, top_ids  rows x top fp32 and int32: the `top` (0..32, at most v) largest log
+ *            probabilities and their indices, the larger first, the lower index first
+ *            among equal ones
+ * Logits may be -inf (p = 0).  A row of nothing else has lse = -inf, entropy 0, logp and
+ * top_logp -inf.  A row that holds a NaN or +inf has NaN in lse, entropy, logp and
+ * top_logp; where fewer than `top` values are no NaN, top_ids ends in -1.
+ */
+int bakron_token_logprobs(const void* logits, int dtype, int rows, int v, int64_t ldl,
+                          const int64_t* targets, int top, float* logp, float* entropy,
+                          float* lse, float* top_logp, int* top_ids, void* stream);
+
+/*
+ * bakron_token_logprobs_backward -- the gradient at the logits of
+ * sum_t (dlogp_t logp_t + dentropy_t entropy_t):
+ *   dlogits_j = dlogp ([j = target] - p_j) - dentropy p_j (log p_j + entropy)
+ *   lse, entropy  what the forward call wrote (entropy may be NULL without dentropy)
+ *   dlogp, dentropy  rows fp32; either may be NULL (0).  A row whose target is outside
+ *            0..v-1 has no dlogp; targets may be NULL without dlogp
+ *   dlogits  rows x v of `dtype`, row stride ldd (>= v); may be logits
+ * A row of lse = -inf gets zeros.
+ */
+int bakron_token_logprobs_backward(const void* logits, int dtype, int rows, int v, int64_t ldl,
+                                   const int64_t* targets, const float* lse,
+                                   const float* dlogp, const float* entropy,
+                                   const float* dentropy, void* dlogits, int64_t ldd,
+                                   void* stream);
 
 /* Static description of a status code. */
 const char* bakron_strerror(int status);

@@ -19,3 +19,6 @@ from .bakron import (BakronError, Factors, alloc_workspace, bakron_diag_gemm_tf3
                      bakron_last_cuda_error, dequantize, factors_bytes, lib, library_path,
                      strerror, workspace_bytes)
 from .buildlib import build  # noqa: F401
+from .operators import (PackedWeight, bakron_linear, bakron_pack_weight, bakron_rmsnorm,  # noqa: F401
+                        bakron_rmsnorm_backward, bakron_token_logprobs,
+                        bakron_token_logprobs_backward)

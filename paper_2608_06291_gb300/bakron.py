@@ -14,7 +14,7 @@ import torch
 from . import buildlib as _build
 
 OK, ERR_INVALID_ARG, ERR_NOT_SPD, ERR_CUDA, ERR_TIMEOUT, ERR_WORKSPACE, ERR_NONFINITE = range(7)
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 
 _lib = None
 
@@ -114,6 +114,26 @@ def lib() -> ctypes.CDLL:
     L.bakron_diag_mma_rate.argtypes = [i32, vp, sz, ctypes.POINTER(ctypes.c_double),
                                        ctypes.POINTER(ctypes.c_double), vp]
     L.bakron_diag_mma_rate.restype = i32
+    L.bakron_packed_bytes.argtypes = [i32, i32, i32, i32]
+    L.bakron_packed_bytes.restype = sz
+    L.bakron_pack_weight.argtypes = [vp, i64, vp, vp, i32, i32, i32, i32, vp, sz, vp]
+    L.bakron_pack_weight.restype = i32
+    L.bakron_linear_workspace_bytes.argtypes = [vp, i32, i32, i64, i32, i32]
+    L.bakron_linear_workspace_bytes.restype = sz
+    L.bakron_linear.argtypes = [vp, i32, i32, i64, vp, vp, i32, i32, i32, i32, vp, i32, vp, i64, vp, i32,
+                                i64, vp, sz, i32, vp]
+    L.bakron_linear.restype = i32
+    L.bakron_rmsnorm.argtypes = [vp, i32, i32, i32, i64, vp, i64, vp, i32, f32, vp, i64, vp, i32, i64, vp, vp]
+    L.bakron_rmsnorm.restype = i32
+    L.bakron_rmsnorm_backward_workspace_bytes.argtypes = [i32, i32]
+    L.bakron_rmsnorm_backward_workspace_bytes.restype = sz
+    L.bakron_rmsnorm_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, i32, f32, vp, i64, vp, i64, vp,
+                                          vp, sz, vp]
+    L.bakron_rmsnorm_backward.restype = i32
+    L.bakron_token_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp]
+    L.bakron_token_logprobs.restype = i32
+    L.bakron_token_logprobs_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.bakron_token_logprobs_backward.restype = i32
     L.bakron_strerror.argtypes = [i32]
     L.bakron_strerror.restype = ctypes.c_char_p
     L.bakron_last_cuda_error.argtypes = [ctypes.POINTER(ctypes.c_char_p),
