@@ -246,6 +246,7 @@ void launch_few(const LinearParams& P, bool w8, bool x8, cudaStream_t s) {
 }
 
 constexpr int LIN_MAX_DIM = 1 << 17;
+constexpr int FEW_TOKENS = 16;
 
 bool weight_ok(int m, int n, int qmax, int group_size) {
   return m >= 1 && n >= 1 && m <= LIN_MAX_DIM && n <= LIN_MAX_DIM && qmax >= 1 && qmax <= 255 &&
@@ -284,8 +285,8 @@ extern "C" int bakron_pack_weight(const uint8_t* codes, int64_t ldc, const float
 
 extern "C" size_t bakron_linear_workspace_bytes(const void* x, int xdtype, int rows, int64_t ldx,
                                                 int n, int qmax) {
-  (void)x; (void)xdtype; (void)rows; (void)ldx; (void)n; (void)qmax;
-  return 0;
+  if (rows <= FEW_TOKENS || n < 1) return 0;
+  return linear_tc_workspace(x, xdtype == BAKRON_E4M3, rows, ldx, n, qmax > 15);
 }
 
 extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float* xscales,
@@ -301,7 +302,8 @@ extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, c
   if (!x || !packed || !y || ldx < n || ldy < m || (residual && ldr < m) || (uintptr_t)packed % 16 != 0)
     return BAKRON_ERR_INVALID_ARG;
   const size_t need = bakron_linear_workspace_bytes(x, xdtype, rows, ldx, n, qmax);
-  if (need && (!workspace || workspace_bytes < need)) return BAKRON_ERR_WORKSPACE;
+  if (need && (!workspace || (uintptr_t)workspace % 16 != 0)) return BAKRON_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return BAKRON_ERR_WORKSPACE;
   const WeightLayout L(m, n, qmax, group_size);
   const unsigned char* p = (const unsigned char*)packed;
   const bool x8 = xdtype == BAKRON_E4M3;
@@ -313,13 +315,18 @@ extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, c
   P.chunks = L.G == 1 ? (int)(L.np / 32) : L.group / 32;
   P.G = (int)L.G; P.activation = activation; P.yf32 = ydtype == BAKRON_F32;
   P.xvec = x8 ? ((uintptr_t)x | (uintptr_t)ldx) % 8 == 0 : aligned16(x, ldx * 2);
+  const int ys = P.yf32 ? 4 : 2;
+  P.yvec = aligned16(y, ldy * ys) && (!residual || aligned16(residual, ldr * ys));
   cudaStream_t s = (cudaStream_t)stream;
+  if (rows > FEW_TOKENS) {
+    const int rc = linear_tc(P, x8, L.bytes8, workspace, s);
+    return rc != BAKRON_OK || !sync ? rc : bakron_read_status(workspace, stream);
+  }
   if (rows <= 8)
     launch_few<1>(P, L.bytes8, x8, s);
   else
     launch_few<2>(P, L.bytes8, x8, s);
   BK_CUDA_OK(cudaGetLastError());
-  if (!sync) return BAKRON_OK;
-  BK_CUDA_OK(cudaStreamSynchronize(s));
+  if (sync) BK_CUDA_OK(cudaStreamSynchronize(s));
   return BAKRON_OK;
 }

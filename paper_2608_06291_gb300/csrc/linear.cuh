@@ -62,6 +62,7 @@ struct LinearParams {
   int G;
   int activation, yf32;
   int xvec;                 // x can be read 8 elements at a time
+  int yvec;                 // y and the residual 16 bytes at a time, from columns that are multiples of 8
 };
 
 __device__ __forceinline__ float activate(float v, int a) {
@@ -108,5 +109,10 @@ __device__ __forceinline__ uint32_t pair8(uint32_t w0, uint32_t w1, int p, __nv_
   __nv_bfloat162 r = __hadd2(__hfma2(hh, c16, __hneg2(z)), ll);
   return *reinterpret_cast<uint32_t*>(&r);
 }
+
+// Many tokens (linear_tc.cu): the bytes of workspace its call needs (a status of 256, and
+// the tokens' copy where they cannot be read as they are), and the call.
+size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8);
+int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cudaStream_t s);
 
 }  // namespace bakron

@@ -1,0 +1,682 @@
+// bakron_linear for many tokens: What's codes become exact operands of the tensor cores.
+//
+// D (128 rows of What x BN tokens) += A B: A, the integers c - z, is written into TMEM by
+// four expanding warps (a thread is a row: its zero is a register), B, the tokens, lies
+// in shared memory as TMA leaves it (K-major, 128-byte swizzle).  So a code is read once
+// as 4 or 8 bits and never goes through shared memory in its expanded form.
+//   bf16 tokens: kind::f16, c - z in bf16 (|c - z| <= 255: exact).
+//   e4m3 tokens: kind::f8f6f4, c - z in e4m3 (|c - z| <= 15: exact).
+// A grid's sum (a segment; 1024 columns where a row has one grid) accumulates in TMEM
+// from zero; the epilogue warps multiply it by the grid's scale and add it in fp32
+// registers while the next one is formed.
+//
+// Roles: warp 0 loads tokens, warp 2 codes, warp 1 issues the MMAs, warps 4-7 expand,
+// warps 8-15 (two per lane quarter of TMEM) sum and write out.  With 256 tokens the
+// accumulators are halves of 128 columns in three buffers (2 x 256 would leave no room
+// for A).  CTAs are persistent, or, where there are fewer tiles than SMs, up to 8 CTAs of
+// a cluster share a tile's columns and add their parts through each other's shared
+// memory, always in the same order.
+#include <cooperative_groups.h>
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "linear.cuh"
+#include "tc_gemm.cuh"
+#include "tcgen05.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace bakron {
+namespace {
+
+constexpr int TC_THREADS = 512;
+constexpr int SEG_CHUNKS = 32;           // a segment where a row has one grid: 1024 columns
+constexpr int TOKEN_GROUP = 16;          // token tiles that share a pass over the weight
+
+// The way out: an epilogue warp's 32 rows of 16 tokens at a time, token by token.
+constexpr int STAGE_LD = 36;             // floats of a token: 16-byte reads of 8 lanes meet no bank twice
+constexpr uint32_t STAGE_BYTES = 8 * 16 * STAGE_LD * 4;
+
+template <int BN_, bool W8_, bool X8_>
+struct TcShape {
+  static constexpr int BN = BN_;
+  static constexpr bool W8 = W8_, X8 = X8_;
+  static constexpr int H = BN == 256 ? 2 : 1;            // accumulators of a tile
+  static constexpr int NB = BN / H;                      // their columns
+  static constexpr int NACC = BN >= 128 ? 3 : 4;
+  static constexpr int NA = BN >= 128 ? 4 : 8;           // A stages, 32 TMEM columns each
+  static constexpr int ACC_COLS = NACC * NB;
+  static constexpr int CH = X8 ? 4 : 2;                  // 32-column chunks of a stage
+  static constexpr int SPB = 4 / CH;                     // stages of a 128-column block
+  static constexpr uint32_t XS = BN * 128;               // bytes of a stage's tokens
+  static constexpr uint32_t WS = W8 ? 16384 : 8192;      // bytes of a block's codes
+  static constexpr int NX = BN == 256 ? 5 : 8;
+  static constexpr int NW = BN == 256 ? (W8 ? 2 : 4) : BN == 128 ? (W8 ? 4 : 6) : (W8 ? 6 : 12);
+  static constexpr int COLS = NB / 2;                    // columns an epilogue warp sums
+  static constexpr uint32_t SMEM_USED = NX * XS + NW * WS + STAGE_BYTES + 1024 /*align*/ + 512 /*barriers*/;
+  static constexpr uint32_t SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA an SM
+  // registers a thread of each warpgroup (512 in sum, as launched)
+  static constexpr int R_LOAD = 56, R_EXPAND = 104, R_SUM = 176;
+  static_assert(ACC_COLS + NA * 32 <= 512, "TMEM");
+  static_assert(SMEM <= 232448, "shared memory");
+  static_assert(R_LOAD + R_EXPAND + 2 * R_SUM <= 512, "registers");
+  static_assert((uint32_t)BN * 128 * 4 <= NX * XS || BN == 256, "parts of a split tile");
+};
+
+struct TcParams {
+  LinearParams L;
+  int row_tiles, token_tiles, splits;
+  int seg_chunks, segs;   // chunks of a segment; how many there are (the last takes the rest)
+  int* status;
+  long long spin_cycles;
+};
+
+__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, long long limit,
+                                        volatile int* abort_flag) {
+  if (mbar_test(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (true) {
+    if (mbar_test(bar, parity)) return true;
+    if (*abort_flag || clock64() - t0 > limit) return false;
+  }
+}
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+          smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+      : "memory");
+}
+
+// 32 columns of this thread's TMEM lane.
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+      "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+      "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+      "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+}
+
+// 16 columns of this thread's TMEM lane; valid after tmem_wait_ld().
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+
+// D += A B, A in TMEM: 16 bf16 or 32 e4m3 columns, 8 TMEM columns either way.
+template <bool X8>
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (X8)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// kind::f8f6f4: D fp32, A and B e4m3 (format 0), K-major, 128 x N.
+__host__ __device__ constexpr uint32_t idesc_e4m3(int N) {
+  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+template <int R>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+
+// The segment of the chunks as they go by.
+struct Segments {
+  int seg, left, each, last;
+  __device__ Segments(const TcParams& P, int chunk) : each(P.seg_chunks), last(P.segs - 1) {
+    seg = min(chunk / each, last);
+    left = seg == last ? INT_MAX : (seg + 1) * each - chunk;
+  }
+  __device__ __forceinline__ void next() {
+    ++seg;
+    left = seg == last ? INT_MAX : each;
+  }
+};
+
+// e4m3 bytes of c - z for c = 0..15, as prmt looks them up.
+struct Table {
+  uint32_t t[4];
+  __device__ __forceinline__ explicit Table(int z) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float v = (float)(4 * i - z);
+      t[i] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v, v + 1.f), __NV_SATFINITE, __NV_E4M3) |
+             (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v + 2.f, v + 3.f), __NV_SATFINITE, __NV_E4M3) << 16;
+    }
+  }
+  // four codes (the low 16 bits of lo3: their low three bits, of hi1: their high bit)
+  __device__ __forceinline__ uint32_t four(uint32_t lo3, uint32_t hi1) const {
+    const uint32_t a = __byte_perm(t[0], t[1], lo3), b = __byte_perm(t[2], t[3], lo3);
+    const uint32_t m = __byte_perm(0x0000FF00u, 0u, hi1);
+    return (a & ~m) | (b & m);
+  }
+  // the 8 codes of a word, in the columns' order
+  __device__ __forceinline__ void eight(uint32_t w, uint32_t& o0, uint32_t& o1) const {
+    const uint32_t lo3 = w & 0x77777777u, hi1 = (w >> 3) & 0x11111111u;
+    const uint32_t even = four(lo3 & 0xFFFFu, hi1 & 0xFFFFu), odd = four(lo3 >> 16, hi1 >> 16);
+    o0 = __byte_perm(even, odd, 0x5140);
+    o1 = __byte_perm(even, odd, 0x7362);
+  }
+};
+
+// 16 neighbouring rows' sums of one token (16-byte aligned in shared memory): epilogue and store.
+__device__ __forceinline__ void linear_store16(const LinearParams& L, const float* sums, int64_t tok, int row0) {
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 f = reinterpret_cast<const float4*>(sums)[i];
+    v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
+  }
+  if (row0 + 16 > L.m || !L.yvec) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (row0 + i < L.m) linear_store(L, v[i], tok, row0 + i);
+    return;
+  }
+  const float xs = L.xscales ? L.xscales[tok] : 1.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    v[i] *= xs;
+    if (L.bias) v[i] += L.bias[row0 + i];
+    v[i] = activate(v[i], L.activation);
+  }
+#pragma unroll
+  for (int i = 0; i < 16; i += 8) {
+    float w[8], r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = v[i + j];
+    if (L.residual) {
+      if (L.yf32)
+        load8((const float*)L.residual + tok * L.ldr + row0 + i, r);
+      else
+        load8((const __nv_bfloat16*)L.residual + tok * L.ldr + row0 + i, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] += r[j];
+    }
+    if (L.yf32)
+      store8((float*)L.y + tok * L.ldy + row0 + i, w);
+    else
+      store8((__nv_bfloat16*)L.y + tok * L.ldy + row0 + i, w);
+  }
+}
+
+template <class S>
+__global__ void __launch_bounds__(TC_THREADS, 1)
+    k_linear_tc(const __grid_constant__ CUtensorMap xmap, const TcParams P) {
+  extern __shared__ __align__(1024) unsigned char tc_smem[];
+  unsigned char* xring = (unsigned char*)(((uintptr_t)tc_smem + 1023) & ~(uintptr_t)1023);
+  unsigned char* wring = xring + S::NX * S::XS;
+  float* stage = (float*)(wring + S::NW * S::WS);
+  uint64_t* bars = (uint64_t*)((unsigned char*)stage + STAGE_BYTES);
+  uint64_t *xF = bars, *xE = xF + S::NX, *wF = xE + S::NX, *wE = wF + S::NW, *aF = wE + S::NW, *aE = aF + S::NA,
+           *cF = aE + S::NA, *cE = cF + S::NACC, *done = cE + S::NACC;
+  uint32_t* tmem_slot = (uint32_t*)(done + 1);
+  volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::NX; ++i) mbar_init(&xF[i], 1), mbar_init(&xE[i], 1);
+    for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], 4);
+    for (int i = 0; i < S::NA; ++i) mbar_init(&aF[i], 4), mbar_init(&aE[i], 1);
+    for (int i = 0; i < S::NACC; ++i) mbar_init(&cF[i], 1), mbar_init(&cE[i], 8);
+    mbar_init(done, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *tmem_slot, tmem_a = tmem + S::ACC_COLS;
+
+  const LinearParams& L = P.L;
+  const int tiles = P.row_tiles * P.token_tiles, part = blockIdx.x % P.splits;
+  const int tile0 = blockIdx.x / P.splits, tile_step = gridDim.x / P.splits;
+  const int per = ceil_div(L.kblocks, P.splits);     // 128-column blocks of a part
+  const int kb0 = part * per, kb1 = min(L.kblocks, kb0 + per);
+  const long long drain = 4000000000LL;   // ~2 s: wind-down bound
+  auto place = [&](int tile, int& rt, int& tt) {
+    const int group = tile / (P.row_tiles * TOKEN_GROUP), in = tile - group * P.row_tiles * TOKEN_GROUP;
+    const int wide = min(TOKEN_GROUP, P.token_tiles - group * TOKEN_GROUP);
+    rt = in / wide;
+    tt = group * TOKEN_GROUP + in % wide;
+  };
+  auto timed_out = [&]() {
+    if (!*abort_flag) raise_status(P.status, BAKRON_ERR_TIMEOUT);
+    *abort_flag = 1;
+  };
+  auto wait = [&](uint64_t* bar, uint32_t parity) {      // one thread
+    if (tc_wait(bar, parity, P.spin_cycles, abort_flag)) return true;
+    timed_out();
+    return false;
+  };
+  auto wait_warp = [&](uint64_t* bar, uint32_t parity) { // a warp: one lane waits
+    int ok = 1;
+    if (lane == 0) ok = wait(bar, parity) ? 1 : 0;
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+  };
+  float acc[S::H][S::COLS];       // the epilogue's sums
+
+  if (warp < 4) {
+    if constexpr (S::BN == 256) regs_down<S::R_LOAD>();
+    if (warp == 0 && lane == 0) {
+      int it = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+        int rt, tt;
+        place(tile, rt, tt);
+        for (int st = kb0 * S::SPB; st < kb1 * S::SPB; ++st, ++it) {
+          const int s = it % S::NX;
+          if (it >= S::NX && !wait(&xE[s], (uint32_t)(it / S::NX - 1) & 1u)) {
+            ok = false;
+            break;
+          }
+          mbar_expect_tx(&xF[s], S::XS);
+          tma_load_2d(xring + s * S::XS, &xmap, &xF[s], st * S::CH * 32, tt * S::BN);
+        }
+      }
+      // every copy issued has landed before the CTA (and its shared memory) goes
+      for (int j = it > S::NX ? it - S::NX : 0; j < it; ++j)
+        if (!mbar_wait(&xF[j % S::NX], (uint32_t)(j / S::NX) & 1u, drain)) timed_out();
+    } else if (warp == 2 && lane == 0) {
+      int it = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+        int rt, tt;
+        place(tile, rt, tt);
+        const unsigned char* src = L.codes + (int64_t)rt * L.kblocks * S::WS;
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+          const int s = it % S::NW;
+          if (it >= S::NW && !wait(&wE[s], (uint32_t)(it / S::NW - 1) & 1u)) {
+            ok = false;
+            break;
+          }
+          mbar_expect_tx(&wF[s], S::WS);
+          bulk_load(wring + s * S::WS, src + (int64_t)kb * S::WS, S::WS, &wF[s]);
+        }
+      }
+      for (int j = it > S::NW ? it - S::NW : 0; j < it; ++j)
+        if (!mbar_wait(&wF[j % S::NW], (uint32_t)(j / S::NW) & 1u, drain)) timed_out();
+    } else if (warp == 1 && lane == 0) {
+      constexpr uint32_t idesc = S::X8 ? idesc_e4m3(S::NB) : idesc_bf16(128, S::NB);
+      constexpr int MPC = S::X8 ? 1 : 2;     // MMAs of a chunk
+      const uint64_t desc0 = smem_desc(smem_u32(xring));
+      int it = 0, g = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+        Segments seg(P, kb0 * 4);
+        bool fresh = true;
+        const int st1 = kb1 * S::SPB;
+        for (int st = kb0 * S::SPB; st < st1 && ok; ++st, ++it) {
+          const int sx = it % S::NX, sa = it % S::NA;
+          if (!wait(&aF[sa], (uint32_t)(it / S::NA) & 1u) || !wait(&xF[sx], (uint32_t)(it / S::NX) & 1u)) {
+            ok = false;
+            break;
+          }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint64_t b0 = desc0 + (uint64_t)((sx * S::XS) >> 4);
+          const uint32_t a0 = tmem_a + sa * 32;
+          for (int c = 0; c < S::CH && ok;) {
+            const int run = min(S::CH - c, seg.left);
+            const bool ends = run == seg.left || (st == st1 - 1 && c + run == S::CH);
+#pragma unroll
+            for (int h = 0; h < S::H; ++h) {
+              const int buf = (g + h) % S::NACC;
+              if (fresh && g + h >= S::NACC) {
+                if (!wait(&cE[buf], (uint32_t)((g + h) / S::NACC - 1) & 1u)) {
+                  ok = false;
+                  break;
+                }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              }
+              const uint32_t d = tmem + buf * S::NB;
+              const uint64_t b = b0 + (uint64_t)((h * S::NB * 128) >> 4);
+#pragma unroll 4
+              for (int k = c * MPC; k < (c + run) * MPC; ++k)
+                mma_ts<S::X8>(d, a0 + 8 * k, b + 2 * k, idesc, (!fresh || k > c * MPC) ? 1u : 0u);
+              if (ends) mma_commit(&cF[buf]);
+            }
+            if (!ok) break;
+            c += run;
+            fresh = ends;
+            if (ends) g += S::H;
+            if (run == seg.left)
+              seg.next();
+            else if (seg.left != INT_MAX)
+              seg.left -= run;
+          }
+          mma_commit(&aE[sa]);
+          mma_commit(&xE[sx]);
+        }
+      }
+      mma_commit(done);
+      if (!mbar_wait(done, 0, drain)) timed_out();   // before anyone frees TMEM
+    }
+    __syncwarp();
+  } else if (warp < 8) {
+    if constexpr (S::BN == 256) regs_down<S::R_EXPAND>();
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    int ib = 0, ia = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+      int rt, tt;
+      place(tile, rt, tt);
+      const uint8_t* zeros = L.zeros + (int64_t)rt * LIN_BLOCK + row;
+      auto zero_of = [&](int chunk) { return (int)zeros[(L.G == 1 ? 0 : min(chunk / L.chunks, L.G - 1)) * L.mp]; };
+      int z[4], zn[4];
+      const bool one = L.G == 1 || L.chunks % 4 == 0;     // one grid a block
+#pragma unroll
+      for (int j = 0; j < 4; ++j) zn[j] = j == 0 || !one ? zero_of(kb0 * 4 + j) : zn[0];
+      for (int kb = kb0; kb < kb1 && ok; ++kb, ++ib) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = zn[j];
+        if (L.G > 1 && kb + 1 < kb1) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) zn[j] = j == 0 || !one ? zero_of(kb * 4 + 4 + j) : zn[0];
+        }
+        const int sw = ib % S::NW;
+        if (!wait_warp(&wF[sw], (uint32_t)(ib / S::NW) & 1u)) {
+          ok = false;
+          break;
+        }
+        const uint4* u = reinterpret_cast<const uint4*>(wring + sw * S::WS) + row;
+#pragma unroll
+        for (int half = 0; half < S::SPB; ++half, ++ia) {
+          uint32_t a[32];
+          if constexpr (S::X8) {
+            uint4 q[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) q[t] = u[t * 128];
+            Table tab(z[0]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (j > 0 && z[j] != z[j - 1]) tab = Table(z[j]);
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+                tab.eight(j == 0 ? q[t].x : j == 1 ? q[t].y : j == 2 ? q[t].z : q[t].w, a[8 * j + 2 * t],
+                          a[8 * j + 2 * t + 1]);
+            }
+          } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              if constexpr (S::W8) {
+                const uint4 q = u[(t + 4 * half) * 128];
+                const __nv_bfloat162 z0 = __float2bfloat162_rn((float)z[2 * half]);
+                const __nv_bfloat162 z1 = __float2bfloat162_rn((float)z[2 * half + 1]);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                  a[4 * t + p] = pair8(q.x, q.y, p, z0);
+                  a[16 + 4 * t + p] = pair8(q.z, q.w, p, z1);
+                }
+              } else {
+                const uint2 q = reinterpret_cast<const uint2*>(u + t * 128)[half];
+                const __nv_bfloat162 z0 = __float2bfloat162_rn((float)z[2 * half] + 128.f);
+                const __nv_bfloat162 z1 = __float2bfloat162_rn((float)z[2 * half + 1] + 128.f);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                  a[4 * t + p] = pair4(q.x, p, z0);
+                  a[16 + 4 * t + p] = pair4(q.y, p, z1);
+                }
+              }
+            }
+          }
+          const int sa = ia % S::NA;
+          if (ok && ia >= S::NA && !wait_warp(&aE[sa], (uint32_t)(ia / S::NA - 1) & 1u)) ok = false;
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          tmem_st32(tmem_a + sa * 32 + lanes, a);
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&aF[sa]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&wE[sw]);
+      }
+    }
+  } else {
+    if constexpr (S::BN == 256) regs_up<S::R_SUM>();
+    const int q = warp & 3, ch = (warp - 8) >> 2;      // lane quarter, half of the columns
+    const uint32_t lanes = (uint32_t)(q * 32) << 16;
+    int g = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+      int rt, tt;
+      place(tile, rt, tt);
+      const int row = rt * LIN_BLOCK + q * 32 + lane;
+#pragma unroll
+      for (int h = 0; h < S::H; ++h)
+#pragma unroll
+        for (int i = 0; i < S::COLS; ++i) acc[h][i] = 0.f;
+      Segments seg(P, kb0 * 4);
+      for (int chunk = kb0 * 4; chunk < kb1 * 4 && ok;) {
+        const float s = L.scales[(L.G == 1 ? 0 : seg.seg) * L.mp + row];
+#pragma unroll
+        for (int h = 0; h < S::H; ++h, ++g) {
+          const int buf = g % S::NACC;
+          if (ok && !wait_warp(&cF[buf], (uint32_t)(g / S::NACC) & 1u)) ok = false;
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t at = tmem + lanes + buf * S::NB + ch * S::COLS;
+#pragma unroll
+          for (int c = 0; c < S::COLS; c += 16) {
+            uint32_t r[16];
+            tmem_ld16(at + c, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[h][c + i] = fmaf(s, __uint_as_float(r[i]), acc[h][c + i]);
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&cE[buf]);
+        }
+        if (seg.left == INT_MAX) break;
+        chunk += seg.left;
+        seg.next();
+      }
+      if (!ok) break;
+      if (P.splits == 1) {
+        float* mine = stage + (warp - 8) * 16 * STAGE_LD;
+        const int row0 = rt * LIN_BLOCK + q * 32 + (lane & 1) * 16;
+#pragma unroll 1
+        for (int b = 0; b < S::H * S::COLS / 16; ++b) {
+          __syncwarp();
+#pragma unroll
+          for (int h = 0; h < S::H; ++h)
+#pragma unroll
+            for (int c = 0; c < S::COLS / 16; ++c)
+              if (b == h * (S::COLS / 16) + c) {     // registers: no index that is not constant
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mine[i * STAGE_LD + lane] = acc[h][16 * c + i];
+              }
+          __syncwarp();
+          const int64_t tok = (int64_t)tt * S::BN + b / (S::COLS / 16) * S::NB + ch * S::COLS + b % (S::COLS / 16) * 16 +
+                              (lane >> 1);
+          if (tok < L.rows) linear_store16(L, mine + (lane >> 1) * STAGE_LD + (lane & 1) * 16, tok, row0);
+        }
+      }
+    }
+  }
+  if constexpr (S::BN <= 128) {
+    if (P.splits > 1) {      // one tile a cluster; every thread of it comes here
+      cg::cluster_group cluster = cg::this_cluster();
+      float* mine = (float*)xring;       // [token][128 rows]: every MMA that read the ring is complete
+      __syncthreads();
+      if (warp >= 8) {
+        const int q = warp & 3, ch = (warp - 8) >> 2;
+#pragma unroll
+        for (int i = 0; i < S::COLS; ++i) mine[(ch * S::COLS + i) * 128 + q * 32 + lane] = acc[0][i];
+      }
+      cluster.sync();
+      int rt, tt;
+      place(tile0, rt, tt);
+      const int row = rt * LIN_BLOCK + (threadIdx.x & 127);
+      for (int t = part * 4 + (threadIdx.x >> 7); t < S::BN; t += 4 * P.splits) {
+        const int64_t tok = (int64_t)tt * S::BN + t;
+        if (tok >= L.rows) break;
+        float v = 0.f;
+        for (int p = 0; p < P.splits; ++p)
+          v += cluster.map_shared_rank(mine, p)[t * 128 + (threadIdx.x & 127)];
+        if (row < L.m) linear_store(L, v, tok, row);
+      }
+      cluster.sync();          // nobody's shared memory goes before it is read
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// Tokens as TMA can read them: rows of 16-byte multiples, e4m3 widened to bf16 (exact)
+// where the codes have 8 bits.
+template <bool X8, bool WIDEN>
+__global__ void __launch_bounds__(256) k_linear_rows(const void* x, int64_t ldx, int rows, int n, void* out, int64_t ldo) {
+  const int64_t row = blockIdx.x;
+  for (int k = threadIdx.x; k < n; k += 256) {
+    if constexpr (!X8) {
+      ((uint16_t*)out)[row * ldo + k] = ((const uint16_t*)x)[row * ldx + k];
+    } else {
+      const uint8_t v = ((const uint8_t*)x)[row * ldx + k];
+      if constexpr (WIDEN)
+        ((__nv_bfloat16*)out)[row * ldo + k] =
+            __float2bfloat16_rn(__half2float(__half(__nv_cvt_fp8_to_halfraw(v, __NV_E4M3))));
+      else
+        ((uint8_t*)out)[row * ldo + k] = v;
+    }
+  }
+}
+
+template <class S>
+int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
+  static OncePerDevice once;
+  BK_CUDA_OK(once([] {
+    cudaFuncAttributes a;
+    cudaError_t e = cudaFuncGetAttributes(&a, k_linear_tc<S>);
+    // the warpgroups' shares (setmaxnreg) are taken from what the block is launched with
+    if (e == cudaSuccess && S::BN == 256 && a.numRegs != 128) e = cudaErrorInvalidConfiguration;
+    return e != cudaSuccess
+               ? e
+               : cudaFuncSetAttribute(k_linear_tc<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
+  }));
+  const LinearParams& L = P.L;
+  P.token_tiles = ceil_div(L.rows, S::BN);
+  const int64_t tiles = (int64_t)P.row_tiles * P.token_tiles;
+  if (tiles > INT_MAX / 16) return BAKRON_ERR_INVALID_ARG;
+  P.splits = 1;
+  if (S::BN <= 128)
+    while (P.splits < 8 && tiles * P.splits * 2 <= ROW_SMS && L.kblocks >= 4 * P.splits) P.splits *= 2;
+  CUtensorMap map;
+  const cuuint64_t dims[2] = {(cuuint64_t)L.n, (cuuint64_t)L.rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ldx * (S::X8 ? 1 : 2)};
+  const cuuint32_t box[2] = {S::X8 ? 128u : 64u, (cuuint32_t)S::BN}, ones[2] = {1u, 1u};
+  if (!get_encode() ||
+      g_encode(&map, S::X8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(x), dims,
+               strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return BAKRON_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(P.splits > 1 ? tiles * P.splits : std::min<int64_t>(tiles, ROW_SMS)));
+  cfg.blockDim = dim3(TC_THREADS);
+  cfg.dynamicSmemBytes = S::SMEM;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = P.splits;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = P.splits > 1 ? 1 : 0;
+  BK_CUDA_OK(cudaLaunchKernelEx(&cfg, k_linear_tc<S>, map, P));
+  return BAKRON_OK;
+}
+
+template <bool W8, bool X8>
+int launch_bn(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
+  // The token tile with the shortest schedule: rounds of tiles over the SMs, a tile costing
+  // its tokens and about 32 more (expanding the codes, the way out).
+  int best = 32;
+  double cost = 1e300;
+  for (int bn = 256; bn >= 32; bn /= 2) {
+    const double tiles = (double)P.row_tiles * ceil_div(P.L.rows, bn);
+    const double c = tiles >= ROW_SMS ? ceil(tiles / ROW_SMS) * (bn + 32) : tiles / ROW_SMS * (bn + 32) + (bn == 256 ? bn : 0);
+    if (c < 0.97 * cost) {
+      best = bn;
+      cost = c;
+    }
+  }
+  switch (best) {
+    case 256: return launch_tc<TcShape<256, W8, X8>>(x, ldx, P, s);
+    case 128: return launch_tc<TcShape<128, W8, X8>>(x, ldx, P, s);
+    case 64: return launch_tc<TcShape<64, W8, X8>>(x, ldx, P, s);
+    default: return launch_tc<TcShape<32, W8, X8>>(x, ldx, P, s);
+  }
+}
+
+}  // namespace
+
+// Whether TMA reads the tokens as they are; if not, they are copied first.
+static bool rows_in_place(const void* x, bool x8, int64_t ldx, bool bytes8) {
+  return !(x8 && bytes8) && aligned16(x, x8 ? ldx : 2 * ldx);
+}
+
+size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8) {
+  if (rows_in_place(x, x8, ldx, bytes8)) return 256;
+  return 256 + (size_t)rows * (size_t)round_up(n, 16) * (x8 && !bytes8 ? 1 : 2);
+}
+
+int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cudaStream_t s) {
+  TcParams P{};
+  P.L = L;
+  P.row_tiles = (int)(L.mp / LIN_BLOCK);
+  P.seg_chunks = L.G == 1 ? SEG_CHUNKS : L.chunks;
+  P.segs = L.G == 1 ? INT_MAX / SEG_CHUNKS - 1 : L.G;
+  P.status = (int*)workspace;
+  P.spin_cycles = spin_cycles_from_env();
+  BK_CUDA_OK(cudaMemsetAsync(workspace, 0, 256, s));
+  const void* x = L.x;
+  int64_t ldx = L.ldx;
+  if (!rows_in_place(x, x8, ldx, bytes8)) {
+    void* out = (char*)workspace + 256;
+    ldx = round_up(L.n, 16);
+    if (!x8)
+      k_linear_rows<false, false><<<L.rows, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+    else if (bytes8)
+      k_linear_rows<true, true><<<L.rows, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+    else
+      k_linear_rows<true, false><<<L.rows, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+    BK_CUDA_OK(cudaGetLastError());
+    x = out;
+  }
+  if (bytes8) return launch_bn<true, false>(x, ldx, P, s);
+  return x8 ? launch_bn<false, true>(x, ldx, P, s) : launch_bn<false, false>(x, ldx, P, s);
+}
+
+}  // namespace bakron
