@@ -10,12 +10,11 @@
 // from zero; the epilogue warps multiply it by the grid's scale and add it in fp32
 // registers while the next one is formed.
 //
-// Roles: warp 0 loads tokens, warp 2 codes, warp 1 issues the MMAs, warps 4-7 expand,
-// warps 8-15 (two per lane quarter of TMEM) sum and write out.  With 256 tokens the
-// accumulators are halves of 128 columns in three buffers (2 x 256 would leave no room
-// for A).  CTAs are persistent, or, where there are fewer tiles than SMs, up to 8 CTAs of
-// a cluster share a tile's columns and add their parts through each other's shared
-// memory, always in the same order.
+// Roles: warp 0 loads tokens, warp 2 codes, warp 1 issues the MMAs, warps 4-7 and 8-11
+// expand (every other stage each), warps 12-19 (two per lane quarter of TMEM) sum and write
+// out.  CTAs are persistent, or, where there are fewer tiles than SMs, up to 8 CTAs of a
+// cluster share a tile's columns and add their parts through each other's shared memory,
+// always in the same order.
 #include <cooperative_groups.h>
 #include <cuda.h>
 
@@ -30,7 +29,7 @@ namespace cg = cooperative_groups;
 namespace bakron {
 namespace {
 
-constexpr int TC_THREADS = 512;
+constexpr int TC_THREADS = 640;
 constexpr int SEG_CHUNKS = 32;           // a segment where a row has one grid: 1024 columns
 constexpr int TOKEN_GROUP = 16;          // token tiles that share a pass over the weight
 
@@ -42,26 +41,25 @@ template <int BN_, bool W8_, bool X8_>
 struct TcShape {
   static constexpr int BN = BN_;
   static constexpr bool W8 = W8_, X8 = X8_;
-  static constexpr int H = BN == 256 ? 2 : 1;            // accumulators of a tile
-  static constexpr int NB = BN / H;                      // their columns
-  static constexpr int NACC = BN >= 128 ? 3 : 4;
-  static constexpr int NA = BN >= 128 ? 4 : 8;           // A stages, 32 TMEM columns each
-  static constexpr int ACC_COLS = NACC * NB;
+  static constexpr int NACC = 2;                         // accumulators of BN columns
+  static constexpr int NA = BN > 128 ? 4 : 8;            // A stages, 32 TMEM columns each
+  static constexpr int ACC_COLS = NACC * BN;
   static constexpr int CH = X8 ? 4 : 2;                  // 32-column chunks of a stage
   static constexpr int SPB = 4 / CH;                     // stages of a 128-column block
   static constexpr uint32_t XS = BN * 128;               // bytes of a stage's tokens
   static constexpr uint32_t WS = W8 ? 16384 : 8192;      // bytes of a block's codes
-  static constexpr int NX = BN == 256 ? 5 : 8;
-  static constexpr int NW = BN == 256 ? (W8 ? 2 : 4) : BN == 128 ? (W8 ? 4 : 6) : (W8 ? 6 : 12);
-  static constexpr int COLS = NB / 2;                    // columns an epilogue warp sums
+  static constexpr int NX = BN > 128 ? 6 : 8;
+  static constexpr int NW = BN > 128 ? (W8 ? 3 : 6) : BN == 128 ? (W8 ? 4 : 8) : (W8 ? 6 : 12);
+  static constexpr int COLS = BN / 2;                    // columns an epilogue warp sums
   static constexpr uint32_t SMEM_USED = NX * XS + NW * WS + STAGE_BYTES + 1024 /*align*/ + 512 /*barriers*/;
   static constexpr uint32_t SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA an SM
-  // registers a thread of each warpgroup (512 in sum, as launched)
-  static constexpr int R_LOAD = 56, R_EXPAND = 104, R_SUM = 176;
+  // registers a thread of each warpgroup, out of 5 x 96 as launched
+  static constexpr bool SPLIT_REGS = BN >= 128;
+  static constexpr int R_LOAD = 56, R_EXPAND = 72, R_SUM = 136;
   static_assert(ACC_COLS + NA * 32 <= 512, "TMEM");
   static_assert(SMEM <= 232448, "shared memory");
-  static_assert(R_LOAD + R_EXPAND + 2 * R_SUM <= 512, "registers");
-  static_assert((uint32_t)BN * 128 * 4 <= NX * XS || BN == 256, "parts of a split tile");
+  static_assert(R_LOAD + 2 * R_EXPAND + 2 * R_SUM <= 5 * 96, "registers");
+  static_assert((uint32_t)BN * 128 * 4 <= NX * XS || BN > 128, "parts of a split tile");
 };
 
 struct TcParams {
@@ -72,13 +70,14 @@ struct TcParams {
   long long spin_cycles;
 };
 
-__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, long long limit,
-                                        volatile int* abort_flag) {
-  if (mbar_test(bar, parity)) return true;
+// A warp's wait, every lane testing (a vote is what keeps the control flow uniform);
+// gives up after `limit` cycles, or once another role has.
+__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, long long limit, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
   const long long t0 = clock64();
   while (true) {
-    if (mbar_test(bar, parity)) return true;
-    if (*abort_flag || clock64() - t0 > limit) return false;
+    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+    if (__any_sync(0xffffffffu, *abort_flag || clock64() - t0 > limit)) return false;
   }
 }
 
@@ -90,17 +89,13 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       : "memory");
 }
 
-// 32 columns of this thread's TMEM lane.
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+// 16 columns of this thread's TMEM lane.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]),
       "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-      "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-      "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-      "r"(r[30]), "r"(r[31]), "r"(taddr)
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
       : "memory");
 }
 
@@ -115,21 +110,31 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "r"(taddr));
 }
 
-// D += A B, A in TMEM: 16 bf16 or 32 e4m3 columns, 8 TMEM columns either way.
+// D += A B, A in TMEM: 16 bf16 or 32 e4m3 columns, 8 TMEM columns either way.  The warp
+// goes through it together and `lead` (one lane) issues, so that the operands can stay in
+// uniform registers.
 template <bool X8>
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
+                                       uint32_t lead) {
   if constexpr (X8)
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
         : "memory");
   else
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
         : "memory");
+}
+__device__ __forceinline__ void commit_by(uint64_t* bar, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)),
+      "r"(lead)
+      : "memory");
 }
 
 // kind::f8f6f4: D fp32, A and B e4m3 (format 0), K-major, 128 x N.
@@ -238,7 +243,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::NX; ++i) mbar_init(&xF[i], 1), mbar_init(&xE[i], 1);
-    for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], 4);
+    for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], S::X8 ? 4 : 8);
     for (int i = 0; i < S::NA; ++i) mbar_init(&aF[i], 4), mbar_init(&aE[i], 1);
     for (int i = 0; i < S::NACC; ++i) mbar_init(&cF[i], 1), mbar_init(&cE[i], 8);
     mbar_init(done, 1);
@@ -271,21 +276,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if (!*abort_flag) raise_status(P.status, BAKRON_ERR_TIMEOUT);
     *abort_flag = 1;
   };
-  auto wait = [&](uint64_t* bar, uint32_t parity) {      // one thread
+  auto wait = [&](uint64_t* bar, uint32_t parity) {      // a warp
     if (tc_wait(bar, parity, P.spin_cycles, abort_flag)) return true;
     timed_out();
     return false;
   };
-  auto wait_warp = [&](uint64_t* bar, uint32_t parity) { // a warp: one lane waits
-    int ok = 1;
-    if (lane == 0) ok = wait(bar, parity) ? 1 : 0;
-    return __shfl_sync(0xffffffffu, ok, 0) != 0;
-  };
-  float acc[S::H][S::COLS];       // the epilogue's sums
-
+  const uint32_t lead = lane == 0;
   if (warp < 4) {
-    if constexpr (S::BN == 256) regs_down<S::R_LOAD>();
-    if (warp == 0 && lane == 0) {
+    if constexpr (S::SPLIT_REGS) regs_down<S::R_LOAD>();
+    if (warp == 0) {
       int it = 0;
       bool ok = true;
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
@@ -297,14 +296,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             ok = false;
             break;
           }
-          mbar_expect_tx(&xF[s], S::XS);
-          tma_load_2d(xring + s * S::XS, &xmap, &xF[s], st * S::CH * 32, tt * S::BN);
+          if (lead) {
+            mbar_expect_tx(&xF[s], S::XS);
+            tma_load_2d(xring + s * S::XS, &xmap, &xF[s], st * S::CH * 32, tt * S::BN);
+          }
+          __syncwarp();
         }
       }
       // every copy issued has landed before the CTA (and its shared memory) goes
       for (int j = it > S::NX ? it - S::NX : 0; j < it; ++j)
         if (!mbar_wait(&xF[j % S::NX], (uint32_t)(j / S::NX) & 1u, drain)) timed_out();
-    } else if (warp == 2 && lane == 0) {
+    } else if (warp == 2) {
       int it = 0;
       bool ok = true;
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
@@ -317,153 +319,149 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             ok = false;
             break;
           }
-          mbar_expect_tx(&wF[s], S::WS);
-          bulk_load(wring + s * S::WS, src + (int64_t)kb * S::WS, S::WS, &wF[s]);
+          if (lead) {
+            mbar_expect_tx(&wF[s], S::WS);
+            bulk_load(wring + s * S::WS, src + (int64_t)kb * S::WS, S::WS, &wF[s]);
+          }
+          __syncwarp();
         }
       }
       for (int j = it > S::NW ? it - S::NW : 0; j < it; ++j)
         if (!mbar_wait(&wF[j % S::NW], (uint32_t)(j / S::NW) & 1u, drain)) timed_out();
-    } else if (warp == 1 && lane == 0) {
-      constexpr uint32_t idesc = S::X8 ? idesc_e4m3(S::NB) : idesc_bf16(128, S::NB);
+    } else if (warp == 1) {
+      constexpr uint32_t idesc = S::X8 ? idesc_e4m3(S::BN) : idesc_bf16(128, S::BN);
       constexpr int MPC = S::X8 ? 1 : 2;     // MMAs of a chunk
       const uint64_t desc0 = smem_desc(smem_u32(xring));
       int it = 0, g = 0;
       bool ok = true;
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
         Segments seg(P, kb0 * 4);
-        bool fresh = true;
+        uint32_t more = 0;       // the segment has begun
         const int st1 = kb1 * S::SPB;
-        for (int st = kb0 * S::SPB; st < st1 && ok; ++st, ++it) {
+        for (int st = kb0 * S::SPB; st < st1; ++st, ++it) {
           const int sx = it % S::NX, sa = it % S::NA;
-          if (!wait(&aF[sa], (uint32_t)(it / S::NA) & 1u) || !wait(&xF[sx], (uint32_t)(it / S::NX) & 1u)) {
+          if (!wait(&xF[sx], (uint32_t)(it / S::NX) & 1u) || !wait(&aF[sa], (uint32_t)(it / S::NA) & 1u)) {
             ok = false;
             break;
           }
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint64_t b0 = desc0 + (uint64_t)((sx * S::XS) >> 4);
-          const uint32_t a0 = tmem_a + sa * 32;
-          for (int c = 0; c < S::CH && ok;) {
-            const int run = min(S::CH - c, seg.left);
-            const bool ends = run == seg.left || (st == st1 - 1 && c + run == S::CH);
+          const uint64_t b = desc0 + (uint64_t)((sx * S::XS) >> 4);
+          const uint32_t a = tmem_a + sa * 32;
 #pragma unroll
-            for (int h = 0; h < S::H; ++h) {
-              const int buf = (g + h) % S::NACC;
-              if (fresh && g + h >= S::NACC) {
-                if (!wait(&cE[buf], (uint32_t)((g + h) / S::NACC - 1) & 1u)) {
-                  ok = false;
-                  break;
-                }
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-              }
-              const uint32_t d = tmem + buf * S::NB;
-              const uint64_t b = b0 + (uint64_t)((h * S::NB * 128) >> 4);
-#pragma unroll 4
-              for (int k = c * MPC; k < (c + run) * MPC; ++k)
-                mma_ts<S::X8>(d, a0 + 8 * k, b + 2 * k, idesc, (!fresh || k > c * MPC) ? 1u : 0u);
-              if (ends) mma_commit(&cF[buf]);
-            }
+          for (int c = 0; c < S::CH; ++c) {
+            const int buf = g % S::NACC;
+            if (!more && g >= S::NACC && ok && !wait(&cE[buf], (uint32_t)(g / S::NACC - 1) & 1u)) ok = false;
             if (!ok) break;
-            c += run;
-            fresh = ends;
-            if (ends) g += S::H;
-            if (run == seg.left)
+            if (c == 0 || !more) asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int k = c * MPC; k < (c + 1) * MPC; ++k)
+              mma_ts<S::X8>(tmem + buf * S::BN, a + 8 * k, b + 2 * k, idesc, k == c * MPC ? more : 1u, lead);
+            more = 1;
+            if (seg.left == 1 || (st == st1 - 1 && c == S::CH - 1)) {
+              commit_by(&cF[buf], lead);
+              ++g;
+              more = 0;
               seg.next();
-            else if (seg.left != INT_MAX)
-              seg.left -= run;
+            } else if (seg.left != INT_MAX) {
+              --seg.left;
+            }
           }
-          mma_commit(&aE[sa]);
-          mma_commit(&xE[sx]);
+          commit_by(&aE[sa], lead);
+          commit_by(&xE[sx], lead);
+          if (!ok) break;
         }
       }
-      mma_commit(done);
+      commit_by(done, lead);
       if (!mbar_wait(done, 0, drain)) timed_out();   // before anyone frees TMEM
     }
     __syncwarp();
-  } else if (warp < 8) {
-    if constexpr (S::BN == 256) regs_down<S::R_EXPAND>();
-    const int row = (warp & 3) * 32 + lane;
+  } else if (warp < 12) {
+    if constexpr (S::SPLIT_REGS) regs_down<S::R_EXPAND>();
+    const int row = (warp & 3) * 32 + lane, team = (warp - 4) >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    int ib = 0, ia = 0;
+    int ib = 0;
     bool ok = true;
     for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
       int rt, tt;
       place(tile, rt, tt);
       const uint8_t* zeros = L.zeros + (int64_t)rt * LIN_BLOCK + row;
       auto zero_of = [&](int chunk) { return (int)zeros[(L.G == 1 ? 0 : min(chunk / L.chunks, L.G - 1)) * L.mp]; };
-      int z[4], zn[4];
-      const bool one = L.G == 1 || L.chunks % 4 == 0;     // one grid a block
+      // the zeros of this team's chunks of a block: one grid a block, or one a chunk
+      constexpr int NZ = S::X8 ? 4 : 2;
+      const int c0 = S::X8 ? 0 : 2 * team;
+      const bool one = L.G == 1 || L.chunks % 4 == 0;
+      int z[NZ], zn[NZ];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) zn[j] = j == 0 || !one ? zero_of(kb0 * 4 + j) : zn[0];
-      for (int kb = kb0; kb < kb1 && ok; ++kb, ++ib) {
+      for (int j = 0; j < NZ; ++j) zn[j] = j == 0 || !one ? zero_of(kb0 * 4 + c0 + j) : zn[0];
+      for (int kb = kb0; kb < kb1; ++kb, ++ib) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = zn[j];
+        for (int j = 0; j < NZ; ++j) z[j] = zn[j];
         if (L.G > 1 && kb + 1 < kb1) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) zn[j] = j == 0 || !one ? zero_of(kb * 4 + 4 + j) : zn[0];
+          for (int j = 0; j < NZ; ++j) zn[j] = j == 0 || !one ? zero_of(kb * 4 + 4 + c0 + j) : zn[0];
         }
-        const int sw = ib % S::NW;
-        if (!wait_warp(&wF[sw], (uint32_t)(ib / S::NW) & 1u)) {
+        if (S::X8 && (ib & 1) != team) continue;
+        const int sw = ib % S::NW, ia = S::X8 ? ib : 2 * ib + team, sa = ia % S::NA;
+        if (!wait(&wF[sw], (uint32_t)(ib / S::NW) & 1u) || (ia >= S::NA && !wait(&aE[sa], (uint32_t)(ia / S::NA - 1) & 1u))) {
           ok = false;
           break;
         }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint4* u = reinterpret_cast<const uint4*>(wring + sw * S::WS) + row;
+        const uint32_t to = tmem_a + sa * 32 + lanes;
+        uint32_t a[16];
+        if constexpr (S::X8) {
+          uint4 q[4];
 #pragma unroll
-        for (int half = 0; half < S::SPB; ++half, ++ia) {
-          uint32_t a[32];
-          if constexpr (S::X8) {
-            uint4 q[4];
+          for (int t = 0; t < 4; ++t) q[t] = u[t * 128];
+          Table tab(z[0]);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) q[t] = u[t * 128];
-            Table tab(z[0]);
+          for (int j = 0; j < 4; ++j) {
+            if (j > 0 && z[j] != z[j - 1]) tab = Table(z[j]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if (j > 0 && z[j] != z[j - 1]) tab = Table(z[j]);
-#pragma unroll
-              for (int t = 0; t < 4; ++t)
-                tab.eight(j == 0 ? q[t].x : j == 1 ? q[t].y : j == 2 ? q[t].z : q[t].w, a[8 * j + 2 * t],
-                          a[8 * j + 2 * t + 1]);
-            }
-          } else {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-              if constexpr (S::W8) {
-                const uint4 q = u[(t + 4 * half) * 128];
-                const __nv_bfloat162 z0 = __float2bfloat162_rn((float)z[2 * half]);
-                const __nv_bfloat162 z1 = __float2bfloat162_rn((float)z[2 * half + 1]);
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                  a[4 * t + p] = pair8(q.x, q.y, p, z0);
-                  a[16 + 4 * t + p] = pair8(q.z, q.w, p, z1);
-                }
-              } else {
-                const uint2 q = reinterpret_cast<const uint2*>(u + t * 128)[half];
-                const __nv_bfloat162 z0 = __float2bfloat162_rn((float)z[2 * half] + 128.f);
-                const __nv_bfloat162 z1 = __float2bfloat162_rn((float)z[2 * half + 1] + 128.f);
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                  a[4 * t + p] = pair4(q.x, p, z0);
-                  a[16 + 4 * t + p] = pair4(q.y, p, z1);
-                }
-              }
-            }
+            for (int t = 0; t < 4; ++t)
+              tab.eight(j == 0 ? q[t].x : j == 1 ? q[t].y : j == 2 ? q[t].z : q[t].w, a[8 * (j & 1) + 2 * t],
+                        a[8 * (j & 1) + 2 * t + 1]);
+            if (j & 1) tmem_st16(to + 8 * (j - 1), a);
           }
-          const int sa = ia % S::NA;
-          if (ok && ia >= S::NA && !wait_warp(&aE[sa], (uint32_t)(ia / S::NA - 1) & 1u)) ok = false;
-          if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          tmem_st32(tmem_a + sa * 32 + lanes, a);
-          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&aF[sa]);
+        } else if constexpr (S::W8) {
+          uint4 q[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) q[t] = u[(t + 4 * team) * 128];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const __nv_bfloat162 zz = __float2bfloat162_rn((float)z[j]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int p = 0; p < 4; ++p) a[4 * t + p] = pair8(j ? q[t].z : q[t].x, j ? q[t].w : q[t].y, p, zz);
+            tmem_st16(to + 16 * j, a);
+          }
+        } else {
+          uint2 q[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) q[t] = reinterpret_cast<const uint2*>(u + t * 128)[team];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const __nv_bfloat162 zz = __float2bfloat162_rn((float)z[j] + 128.f);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int p = 0; p < 4; ++p) a[4 * t + p] = pair4(j ? q[t].y : q[t].x, p, zz);
+            tmem_st16(to + 16 * j, a);
+          }
         }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(&wE[sw]);
+        if (lead) {
+          mbar_arrive(&aF[sa]);
+          mbar_arrive(&wE[sw]);
+        }
       }
     }
   } else {
-    if constexpr (S::BN == 256) regs_up<S::R_SUM>();
-    const int q = warp & 3, ch = (warp - 8) >> 2;      // lane quarter, half of the columns
+    if constexpr (S::SPLIT_REGS) regs_up<S::R_SUM>();
+    const int q = warp & 3, ch = (warp - 12) >> 2;      // lane quarter, half of the columns
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     int g = 0;
     bool ok = true;
@@ -471,54 +469,52 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       int rt, tt;
       place(tile, rt, tt);
       const int row = rt * LIN_BLOCK + q * 32 + lane;
+      float acc[S::COLS];
 #pragma unroll
-      for (int h = 0; h < S::H; ++h)
-#pragma unroll
-        for (int i = 0; i < S::COLS; ++i) acc[h][i] = 0.f;
+      for (int i = 0; i < S::COLS; ++i) acc[i] = 0.f;
       Segments seg(P, kb0 * 4);
-      for (int chunk = kb0 * 4; chunk < kb1 * 4 && ok;) {
+      for (int chunk = kb0 * 4; chunk < kb1 * 4; ++g) {
         const float s = L.scales[(L.G == 1 ? 0 : seg.seg) * L.mp + row];
-#pragma unroll
-        for (int h = 0; h < S::H; ++h, ++g) {
-          const int buf = g % S::NACC;
-          if (ok && !wait_warp(&cF[buf], (uint32_t)(g / S::NACC) & 1u)) ok = false;
-          if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t at = tmem + lanes + buf * S::NB + ch * S::COLS;
-#pragma unroll
-          for (int c = 0; c < S::COLS; c += 16) {
-            uint32_t r[16];
-            tmem_ld16(at + c, r);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[h][c + i] = fmaf(s, __uint_as_float(r[i]), acc[h][c + i]);
-          }
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&cE[buf]);
+        const int buf = g % S::NACC;
+        if (!wait(&cF[buf], (uint32_t)(g / S::NACC) & 1u)) {
+          ok = false;
+          break;
         }
-        if (seg.left == INT_MAX) break;
-        chunk += seg.left;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t at = tmem + lanes + buf * S::BN + ch * S::COLS;
+#pragma unroll
+        for (int c = 0; c < S::COLS; c += 16) {
+          uint32_t r[16];
+          tmem_ld16(at + c, r);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[c + i] = fmaf(s, __uint_as_float(r[i]), acc[c + i]);
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lead) mbar_arrive(&cE[buf]);
+        chunk = seg.left == INT_MAX ? INT_MAX : chunk + seg.left;
         seg.next();
       }
       if (!ok) break;
-      if (P.splits == 1) {
-        float* mine = stage + (warp - 8) * 16 * STAGE_LD;
+      if (S::BN <= 128 && P.splits > 1) {
+        // [token][128 rows] over the tokens' ring: every MMA that read it is complete
+#pragma unroll
+        for (int i = 0; i < S::COLS; ++i) ((float*)xring)[(ch * S::COLS + i) * 128 + q * 32 + lane] = acc[i];
+      } else {
+        float* mine = stage + (warp - 12) * 16 * STAGE_LD;
         const int row0 = rt * LIN_BLOCK + q * 32 + (lane & 1) * 16;
 #pragma unroll 1
-        for (int b = 0; b < S::H * S::COLS / 16; ++b) {
+        for (int b = 0; b < S::COLS / 16; ++b) {
           __syncwarp();
 #pragma unroll
-          for (int h = 0; h < S::H; ++h)
+          for (int c = 0; c < S::COLS / 16; ++c)
+            if (b == c) {     // registers: no index that is not constant
 #pragma unroll
-            for (int c = 0; c < S::COLS / 16; ++c)
-              if (b == h * (S::COLS / 16) + c) {     // registers: no index that is not constant
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mine[i * STAGE_LD + lane] = acc[h][16 * c + i];
-              }
+              for (int i = 0; i < 16; ++i) mine[i * STAGE_LD + lane] = acc[16 * c + i];
+            }
           __syncwarp();
-          const int64_t tok = (int64_t)tt * S::BN + b / (S::COLS / 16) * S::NB + ch * S::COLS + b % (S::COLS / 16) * 16 +
-                              (lane >> 1);
+          const int64_t tok = (int64_t)tt * S::BN + ch * S::COLS + b * 16 + (lane >> 1);
           if (tok < L.rows) linear_store16(L, mine + (lane >> 1) * STAGE_LD + (lane & 1) * 16, tok, row0);
         }
       }
@@ -527,18 +523,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   if constexpr (S::BN <= 128) {
     if (P.splits > 1) {      // one tile a cluster; every thread of it comes here
       cg::cluster_group cluster = cg::this_cluster();
-      float* mine = (float*)xring;       // [token][128 rows]: every MMA that read the ring is complete
-      __syncthreads();
-      if (warp >= 8) {
-        const int q = warp & 3, ch = (warp - 8) >> 2;
-#pragma unroll
-        for (int i = 0; i < S::COLS; ++i) mine[(ch * S::COLS + i) * 128 + q * 32 + lane] = acc[0][i];
-      }
+      float* mine = (float*)xring;
       cluster.sync();
       int rt, tt;
       place(tile0, rt, tt);
       const int row = rt * LIN_BLOCK + (threadIdx.x & 127);
-      for (int t = part * 4 + (threadIdx.x >> 7); t < S::BN; t += 4 * P.splits) {
+      for (int t = part * 5 + (threadIdx.x >> 7); t < S::BN; t += 5 * P.splits) {
         const int64_t tok = (int64_t)tt * S::BN + t;
         if (tok >= L.rows) break;
         float v = 0.f;
@@ -582,7 +572,7 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
     cudaFuncAttributes a;
     cudaError_t e = cudaFuncGetAttributes(&a, k_linear_tc<S>);
     // the warpgroups' shares (setmaxnreg) are taken from what the block is launched with
-    if (e == cudaSuccess && S::BN == 256 && a.numRegs != 128) e = cudaErrorInvalidConfiguration;
+    if (e == cudaSuccess && S::SPLIT_REGS && a.numRegs != 96) e = cudaErrorInvalidConfiguration;
     return e != cudaSuccess
                ? e
                : cudaFuncSetAttribute(k_linear_tc<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
@@ -624,16 +614,16 @@ int launch_bn(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   // its tokens and about 32 more (expanding the codes, the way out).
   int best = 32;
   double cost = 1e300;
-  for (int bn = 256; bn >= 32; bn /= 2) {
+  for (int bn : {192, 128, 64, 32}) {
     const double tiles = (double)P.row_tiles * ceil_div(P.L.rows, bn);
-    const double c = tiles >= ROW_SMS ? ceil(tiles / ROW_SMS) * (bn + 32) : tiles / ROW_SMS * (bn + 32) + (bn == 256 ? bn : 0);
+    const double c = tiles >= ROW_SMS ? ceil(tiles / ROW_SMS) * (bn + 32) : tiles / ROW_SMS * (bn + 32) + (bn > 128 ? bn : 0);
     if (c < 0.97 * cost) {
       best = bn;
       cost = c;
     }
   }
   switch (best) {
-    case 256: return launch_tc<TcShape<256, W8, X8>>(x, ldx, P, s);
+    case 192: return launch_tc<TcShape<192, W8, X8>>(x, ldx, P, s);
     case 128: return launch_tc<TcShape<128, W8, X8>>(x, ldx, P, s);
     case 64: return launch_tc<TcShape<64, W8, X8>>(x, ldx, P, s);
     default: return launch_tc<TcShape<32, W8, X8>>(x, ldx, P, s);
