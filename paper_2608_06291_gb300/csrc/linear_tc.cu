@@ -49,6 +49,7 @@ struct TcShape {
   static constexpr uint32_t XS = BN * 128;               // bytes of a stage's tokens
   static constexpr uint32_t WS = W8 ? 16384 : 8192;      // bytes of a block's codes
   static constexpr int NX = BN > 128 ? 6 : 8;
+  static constexpr int ND = 8;                           // barriers of "the stage's MMAs are done"
   static constexpr int NW = BN > 128 ? (W8 ? 3 : 6) : BN == 128 ? (W8 ? 4 : 8) : (W8 ? 6 : 12);
   static constexpr int COLS = BN / 2;                    // columns an epilogue warp sums
   static constexpr uint32_t SMEM_USED = NX * XS + NW * WS + STAGE_BYTES + 1024 /*align*/ + 512 /*barriers*/;
@@ -56,6 +57,7 @@ struct TcShape {
   // registers a thread of each warpgroup, out of 5 x 96 as launched
   static constexpr bool SPLIT_REGS = BN >= 128;
   static constexpr int R_LOAD = 56, R_EXPAND = 72, R_SUM = 136;
+  static_assert(ND >= NX && ND >= NA, "a barrier's phase is waited for before the next one can end");
   static_assert(ACC_COLS + NA * 32 <= 512, "TMEM");
   static_assert(SMEM <= 232448, "shared memory");
   static_assert(R_LOAD + 2 * R_EXPAND + 2 * R_SUM <= 5 * 96, "registers");
@@ -235,16 +237,19 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   unsigned char* wring = xring + S::NX * S::XS;
   float* stage = (float*)(wring + S::NW * S::WS);
   uint64_t* bars = (uint64_t*)((unsigned char*)stage + STAGE_BYTES);
-  uint64_t *xF = bars, *xE = xF + S::NX, *wF = xE + S::NX, *wE = wF + S::NW, *aF = wE + S::NW, *aE = aF + S::NA,
-           *cF = aE + S::NA, *cE = cF + S::NACC, *done = cE + S::NACC;
+  // full: xF tokens, wF codes, aF expanded codes, cF sums; free again: sD tokens and expanded
+  // codes of a stage, wE codes, cE sums
+  uint64_t *xF = bars, *sD = xF + S::NX, *wF = sD + S::ND, *wE = wF + S::NW, *aF = wE + S::NW, *cF = aF + S::NA,
+           *cE = cF + S::NACC, *done = cE + S::NACC;
   uint32_t* tmem_slot = (uint32_t*)(done + 1);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < S::NX; ++i) mbar_init(&xF[i], 1), mbar_init(&xE[i], 1);
+    for (int i = 0; i < S::NX; ++i) mbar_init(&xF[i], 1);
+    for (int i = 0; i < S::ND; ++i) mbar_init(&sD[i], 1);
     for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], S::X8 ? 4 : 8);
-    for (int i = 0; i < S::NA; ++i) mbar_init(&aF[i], 4), mbar_init(&aE[i], 1);
+    for (int i = 0; i < S::NA; ++i) mbar_init(&aF[i], 4);
     for (int i = 0; i < S::NACC; ++i) mbar_init(&cF[i], 1), mbar_init(&cE[i], 8);
     mbar_init(done, 1);
     *abort_flag = 0;
@@ -281,6 +286,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     timed_out();
     return false;
   };
+  auto wait_stage = [&](int it) { return wait(&sD[it % S::ND], (uint32_t)(it / S::ND) & 1u); };
   const uint32_t lead = lane == 0;
   if (warp < 4) {
     if constexpr (S::SPLIT_REGS) regs_down<S::R_LOAD>();
@@ -292,7 +298,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         place(tile, rt, tt);
         for (int st = kb0 * S::SPB; st < kb1 * S::SPB; ++st, ++it) {
           const int s = it % S::NX;
-          if (it >= S::NX && !wait(&xE[s], (uint32_t)(it / S::NX - 1) & 1u)) {
+          if (it >= S::NX && !wait_stage(it - S::NX)) {
             ok = false;
             break;
           }
@@ -333,40 +339,63 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       constexpr int MPC = S::X8 ? 1 : 2;     // MMAs of a chunk
       const uint64_t desc0 = smem_desc(smem_u32(xring));
       int it = 0, g = 0;
-      bool ok = true;
+      bool ok = true, x_here = false, a_here = false;
+      auto sum_free = [&]() {     // before the first MMA of a segment
+        return g < S::NACC || wait(&cE[g % S::NACC], (uint32_t)(g / S::NACC - 1) & 1u);
+      };
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
         Segments seg(P, kb0 * 4);
         uint32_t more = 0;       // the segment has begun
         const int st1 = kb1 * S::SPB;
         for (int st = kb0 * S::SPB; st < st1; ++st, ++it) {
           const int sx = it % S::NX, sa = it % S::NA;
-          if (!wait(&xF[sx], (uint32_t)(it / S::NX) & 1u) || !wait(&aF[sa], (uint32_t)(it / S::NA) & 1u)) {
+          if ((!x_here && !wait(&xF[sx], (uint32_t)(it / S::NX) & 1u)) ||
+              (!a_here && !wait(&aF[sa], (uint32_t)(it / S::NA) & 1u)) || (!more && !sum_free())) {
             ok = false;
             break;
           }
+          // a look at the next stage's barriers, of no consequence until then
+          const int nt = it + 1;
+          const bool nx = mbar_test(&xF[nt % S::NX], (uint32_t)(nt / S::NX) & 1u);
+          const bool na = mbar_test(&aF[nt % S::NA], (uint32_t)(nt / S::NA) & 1u);
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint64_t b = desc0 + (uint64_t)((sx * S::XS) >> 4);
           const uint32_t a = tmem_a + sa * 32;
+          if (seg.left >= S::CH) {       // no segment ends inside the stage
+            const uint32_t d = tmem + (g % S::NACC) * S::BN;
 #pragma unroll
-          for (int c = 0; c < S::CH; ++c) {
-            const int buf = g % S::NACC;
-            if (!more && g >= S::NACC && ok && !wait(&cE[buf], (uint32_t)(g / S::NACC - 1) & 1u)) ok = false;
-            if (!ok) break;
-            if (c == 0 || !more) asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-            for (int k = c * MPC; k < (c + 1) * MPC; ++k)
-              mma_ts<S::X8>(tmem + buf * S::BN, a + 8 * k, b + 2 * k, idesc, k == c * MPC ? more : 1u, lead);
+            for (int k = 0; k < S::CH * MPC; ++k) mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k ? 1u : more, lead);
             more = 1;
-            if (seg.left == 1 || (st == st1 - 1 && c == S::CH - 1)) {
-              commit_by(&cF[buf], lead);
+            if (seg.left != INT_MAX) seg.left -= S::CH;
+            if (seg.left == 0 || st == st1 - 1) {
+              commit_by(&cF[g % S::NACC], lead);
               ++g;
               more = 0;
               seg.next();
-            } else if (seg.left != INT_MAX) {
-              --seg.left;
+            }
+          } else {
+#pragma unroll 1
+            for (int c = 0; c < S::CH && ok; ++c) {
+              if (!more && c > 0) {
+                ok = sum_free();
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              }
+              const uint32_t d = tmem + (g % S::NACC) * S::BN;
+              for (int k = c * MPC; ok && k < (c + 1) * MPC; ++k)
+                mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k > c * MPC ? 1u : more, lead);
+              more = 1;
+              if (seg.left != INT_MAX) --seg.left;
+              if (seg.left == 0 || (st == st1 - 1 && c == S::CH - 1)) {
+                commit_by(&cF[g % S::NACC], lead);
+                ++g;
+                more = 0;
+                seg.next();
+              }
             }
           }
-          commit_by(&aE[sa], lead);
-          commit_by(&xE[sx], lead);
+          commit_by(&sD[it % S::ND], lead);
+          x_here = __all_sync(0xffffffffu, nx);
+          a_here = __all_sync(0xffffffffu, na);
           if (!ok) break;
         }
       }
@@ -401,7 +430,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         }
         if (S::X8 && (ib & 1) != team) continue;
         const int sw = ib % S::NW, ia = S::X8 ? ib : 2 * ib + team, sa = ia % S::NA;
-        if (!wait(&wF[sw], (uint32_t)(ib / S::NW) & 1u) || (ia >= S::NA && !wait(&aE[sa], (uint32_t)(ia / S::NA - 1) & 1u))) {
+        if (!wait(&wF[sw], (uint32_t)(ib / S::NW) & 1u) || (ia >= S::NA && !wait_stage(ia - S::NA))) {
           ok = false;
           break;
         }
