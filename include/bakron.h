@@ -519,7 +519,7 @@ typedef enum {
  * A row of x that holds a NaN or an infinity affects its own row of y alone.
  */
 size_t bakron_linear_workspace_bytes(const void* x, int xdtype, int rows, int64_t ldx, int n,
-                                     int qmax);
+                                     int qmax, int group_size);
 int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float* xscales,
                   const void* packed, int m, int n, int qmax, int group_size,
                   const float* bias, int activation, const void* residual, int64_t ldr,

@@ -118,7 +118,7 @@ def lib() -> ctypes.CDLL:
     L.bakron_packed_bytes.restype = sz
     L.bakron_pack_weight.argtypes = [vp, i64, vp, vp, i32, i32, i32, i32, vp, sz, vp]
     L.bakron_pack_weight.restype = i32
-    L.bakron_linear_workspace_bytes.argtypes = [vp, i32, i32, i64, i32, i32]
+    L.bakron_linear_workspace_bytes.argtypes = [vp, i32, i32, i64, i32, i32, i32]
     L.bakron_linear_workspace_bytes.restype = sz
     L.bakron_linear.argtypes = [vp, i32, i32, i64, vp, vp, i32, i32, i32, i32, vp, i32, vp, i64, vp, i32,
                                 i64, vp, sz, i32, vp]

@@ -284,9 +284,10 @@ extern "C" int bakron_pack_weight(const uint8_t* codes, int64_t ldc, const float
 }
 
 extern "C" size_t bakron_linear_workspace_bytes(const void* x, int xdtype, int rows, int64_t ldx,
-                                                int n, int qmax) {
-  if (rows <= FEW_TOKENS || n < 1) return 0;
-  return linear_tc_workspace(x, xdtype == BAKRON_E4M3, rows, ldx, n, qmax > 15);
+                                                int n, int qmax, int group_size) {
+  if (rows <= FEW_TOKENS || !weight_ok(1, n, qmax, group_size)) return 0;
+  return linear_tc_workspace(x, xdtype == BAKRON_E4M3, rows, ldx, n, qmax > 15,
+                             group_size ? n / group_size : 1);
 }
 
 extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float* xscales,
@@ -301,7 +302,7 @@ extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, c
   if (rows == 0) return BAKRON_OK;
   if (!x || !packed || !y || ldx < n || ldy < m || (residual && ldr < m) || (uintptr_t)packed % 16 != 0)
     return BAKRON_ERR_INVALID_ARG;
-  const size_t need = bakron_linear_workspace_bytes(x, xdtype, rows, ldx, n, qmax);
+  const size_t need = bakron_linear_workspace_bytes(x, xdtype, rows, ldx, n, qmax, group_size);
   if (need && (!workspace || (uintptr_t)workspace % 16 != 0)) return BAKRON_ERR_INVALID_ARG;
   if (workspace_bytes < need) return BAKRON_ERR_WORKSPACE;
   const WeightLayout L(m, n, qmax, group_size);

@@ -5,7 +5,11 @@
 // in shared memory as TMA leaves it (K-major, 128-byte swizzle).  So a code is read once
 // as 4 or 8 bits and never goes through shared memory in its expanded form.
 //   bf16 tokens: kind::f16, c - z in bf16 (|c - z| <= 255: exact).
-//   e4m3 tokens: kind::f8f6f4, c - z in e4m3 (|c - z| <= 15: exact).
+//   e4m3 tokens: kind::f8f6f4.  e4m3 is linear up to 16 2^-9 (byte i is i 2^-9), so the odd
+//     integer 2 c - 15 is a sign and its own four bits; c - z = (2 c - 15) / 2 + (7.5 - z),
+//     and the second part is a product with the sum of a token's values, formed once per
+//     grid by k_token_sums.  (From c and z by table it took 15 instructions of the integer
+//     pipe for 8 codes, which bound the whole kernel; this takes 9.)
 // A grid's sum (a segment; 1024 columns where a row has one grid) accumulates in TMEM
 // from zero; the epilogue warps multiply it by the grid's scale and add it in fp32
 // registers while the next one is formed.
@@ -66,14 +70,16 @@ struct TcShape {
 
 struct TcParams {
   LinearParams L;
-  int row_tiles, token_tiles, splits;
+  int row_tiles, token_tiles, splits, per;   // per: 128-column blocks of a split's part
   int seg_chunks, segs;   // chunks of a segment; how many there are (the last takes the rest)
+  const float* sums;      // e4m3 tokens: [segment of a grid][token, padded] sum of the values
+  int64_t sums_ld;
   int* status;
   long long spin_cycles;
 };
 
-// A warp's wait, every lane testing (a vote is what keeps the control flow uniform);
-// gives up after `limit` cycles, or once another role has.
+// A warp's wait, every lane testing (the vote keeps the control flow uniform); gives up
+// after `limit` cycles, or once another role has.
 __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, long long limit, volatile int* abort_flag) {
   if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
   const long long t0 = clock64();
@@ -112,31 +118,29 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "r"(taddr));
 }
 
-// D += A B, A in TMEM: 16 bf16 or 32 e4m3 columns, 8 TMEM columns either way.  The warp
-// goes through it together and `lead` (one lane) issues, so that the operands can stay in
-// uniform registers.
+// D += A B, A in TMEM: 16 bf16 or 32 e4m3 columns, 8 TMEM columns either way.
 template <bool X8>
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
-                                       uint32_t lead) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   if constexpr (X8)
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
   else
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(lead)
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void commit_by(uint64_t* bar, uint32_t lead) {
-  asm volatile(
-      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)),
-      "r"(lead)
-      : "memory");
+
+// One lane of a whole warp, the way the compiler knows it: what it does keeps its operands
+// in uniform registers.
+__device__ __forceinline__ bool elected() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
 }
 
 // kind::f8f6f4: D fp32, A and B e4m3 (format 0), K-major, 128 x N.
@@ -162,31 +166,18 @@ struct Segments {
   }
 };
 
-// e4m3 bytes of c - z for c = 0..15, as prmt looks them up.
-struct Table {
-  uint32_t t[4];
-  __device__ __forceinline__ explicit Table(int z) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float v = (float)(4 * i - z);
-      t[i] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v, v + 1.f), __NV_SATFINITE, __NV_E4M3) |
-             (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v + 2.f, v + 3.f), __NV_SATFINITE, __NV_E4M3) << 16;
-    }
-  }
-  // four codes (the low 16 bits of lo3: their low three bits, of hi1: their high bit)
-  __device__ __forceinline__ uint32_t four(uint32_t lo3, uint32_t hi1) const {
-    const uint32_t a = __byte_perm(t[0], t[1], lo3), b = __byte_perm(t[2], t[3], lo3);
-    const uint32_t m = __byte_perm(0x0000FF00u, 0u, hi1);
-    return (a & ~m) | (b & m);
-  }
-  // the 8 codes of a word, in the columns' order
-  __device__ __forceinline__ void eight(uint32_t w, uint32_t& o0, uint32_t& o1) const {
-    const uint32_t lo3 = w & 0x77777777u, hi1 = (w >> 3) & 0x11111111u;
-    const uint32_t even = four(lo3 & 0xFFFFu, hi1 & 0xFFFFu), odd = four(lo3 >> 16, hi1 >> 16);
-    o0 = __byte_perm(even, odd, 0x5140);
-    o1 = __byte_perm(even, odd, 0x7362);
-  }
-};
+// Four codes (the low nibbles of u's bytes) as e4m3 (2 c - 15) 2^-9: bits 1-3 of 2 c, turned
+// over, with the sign, where c < 8.
+__device__ __forceinline__ uint32_t odd4(uint32_t u) {
+  const uint32_t low = ~(u >> 2) & 0x02020202u;          // 2 where c < 8
+  return ((u << 1) & 0x0E0E0E0Eu) ^ (low * 0x47u + 0x01010101u);
+}
+// The 8 codes of a word, in the columns' order.
+__device__ __forceinline__ void odd8(uint32_t w, uint32_t& o0, uint32_t& o1) {
+  const uint32_t a = odd4(w), b = odd4(w >> 4);          // columns 0 4 1 5 and 2 6 3 7
+  o0 = __byte_perm(a, b, 0x6420);
+  o1 = __byte_perm(a, b, 0x7531);
+}
 
 // 16 neighbouring rows' sums of one token (16-byte aligned in shared memory): epilogue and store.
 __device__ __forceinline__ void linear_store16(const LinearParams& L, const float* sums, int64_t tok, int row0) {
@@ -248,8 +239,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::NX; ++i) mbar_init(&xF[i], 1);
     for (int i = 0; i < S::ND; ++i) mbar_init(&sD[i], 1);
-    for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], S::X8 ? 4 : 8);
     for (int i = 0; i < S::NA; ++i) mbar_init(&aF[i], 4);
+    for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], S::X8 ? 4 : 8);
     for (int i = 0; i < S::NACC; ++i) mbar_init(&cF[i], 1), mbar_init(&cE[i], 8);
     mbar_init(done, 1);
     *abort_flag = 0;
@@ -268,8 +259,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   const LinearParams& L = P.L;
   const int tiles = P.row_tiles * P.token_tiles, part = blockIdx.x % P.splits;
   const int tile0 = blockIdx.x / P.splits, tile_step = gridDim.x / P.splits;
-  const int per = ceil_div(L.kblocks, P.splits);     // 128-column blocks of a part
-  const int kb0 = part * per, kb1 = min(L.kblocks, kb0 + per);
+  const int kb0 = part * P.per, kb1 = min(L.kblocks, kb0 + P.per);
   const long long drain = 4000000000LL;   // ~2 s: wind-down bound
   auto place = [&](int tile, int& rt, int& tt) {
     const int group = tile / (P.row_tiles * TOKEN_GROUP), in = tile - group * P.row_tiles * TOKEN_GROUP;
@@ -335,11 +325,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       for (int j = it > S::NW ? it - S::NW : 0; j < it; ++j)
         if (!mbar_wait(&wF[j % S::NW], (uint32_t)(j / S::NW) & 1u, drain)) timed_out();
     } else if (warp == 1) {
+      // The warp goes through the loop together and an elected lane issues.  Cycles an MMA
+      // (128 x 32, four a stage with two barrier tests, fence and commit) beside warps busy
+      // on the same schedulers: elected 96, one lane all the way 117, predicated 194.
       constexpr uint32_t idesc = S::X8 ? idesc_e4m3(S::BN) : idesc_bf16(128, S::BN);
       constexpr int MPC = S::X8 ? 1 : 2;     // MMAs of a chunk
       const uint64_t desc0 = smem_desc(smem_u32(xring));
       int it = 0, g = 0;
-      bool ok = true, x_here = false, a_here = false;
+      bool ok = true, here = false;
       auto sum_free = [&]() {     // before the first MMA of a segment
         return g < S::NACC || wait(&cE[g % S::NACC], (uint32_t)(g / S::NACC - 1) & 1u);
       };
@@ -348,14 +341,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         uint32_t more = 0;       // the segment has begun
         const int st1 = kb1 * S::SPB;
         for (int st = kb0 * S::SPB; st < st1; ++st, ++it) {
-          const int sx = it % S::NX, sa = it % S::NA;
-          if ((!x_here && !wait(&xF[sx], (uint32_t)(it / S::NX) & 1u)) ||
-              (!a_here && !wait(&aF[sa], (uint32_t)(it / S::NA) & 1u)) || (!more && !sum_free())) {
+          const int sx = it % S::NX, sa = it % S::NA, nt = it + 1;
+          if ((!here && (!wait(&xF[sx], (uint32_t)(it / S::NX) & 1u) || !wait(&aF[sa], (uint32_t)(it / S::NA) & 1u))) ||
+              (!more && !sum_free())) {
             ok = false;
             break;
           }
           // a look at the next stage's barriers, of no consequence until then
-          const int nt = it + 1;
           const bool nx = mbar_test(&xF[nt % S::NX], (uint32_t)(nt / S::NX) & 1u);
           const bool na = mbar_test(&aF[nt % S::NA], (uint32_t)(nt / S::NA) & 1u);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -363,12 +355,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           const uint32_t a = tmem_a + sa * 32;
           if (seg.left >= S::CH) {       // no segment ends inside the stage
             const uint32_t d = tmem + (g % S::NACC) * S::BN;
-#pragma unroll
-            for (int k = 0; k < S::CH * MPC; ++k) mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k ? 1u : more, lead);
-            more = 1;
             if (seg.left != INT_MAX) seg.left -= S::CH;
-            if (seg.left == 0 || st == st1 - 1) {
-              commit_by(&cF[g % S::NACC], lead);
+            const bool ends = seg.left == 0 || st == st1 - 1;
+            if (elected()) {
+#pragma unroll
+              for (int k = 0; k < S::CH * MPC; ++k) mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k ? 1u : more);
+              mma_commit(&sD[it % S::ND]);
+              if (ends) mma_commit(&cF[g % S::NACC]);
+            }
+            __syncwarp();
+            more = 1;
+            if (ends) {
               ++g;
               more = 0;
               seg.next();
@@ -381,25 +378,29 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               }
               const uint32_t d = tmem + (g % S::NACC) * S::BN;
-              for (int k = c * MPC; ok && k < (c + 1) * MPC; ++k)
-                mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k > c * MPC ? 1u : more, lead);
-              more = 1;
               if (seg.left != INT_MAX) --seg.left;
-              if (seg.left == 0 || (st == st1 - 1 && c == S::CH - 1)) {
-                commit_by(&cF[g % S::NACC], lead);
+              const bool ends = seg.left == 0 || (st == st1 - 1 && c == S::CH - 1);
+              if (elected()) {
+                for (int k = c * MPC; ok && k < (c + 1) * MPC; ++k)
+                  mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k > c * MPC ? 1u : more);
+                if (c == S::CH - 1) mma_commit(&sD[it % S::ND]);
+                if (ends) mma_commit(&cF[g % S::NACC]);
+              }
+              __syncwarp();
+              more = 1;
+              if (ends) {
                 ++g;
                 more = 0;
                 seg.next();
               }
             }
           }
-          commit_by(&sD[it % S::ND], lead);
-          x_here = __all_sync(0xffffffffu, nx);
-          a_here = __all_sync(0xffffffffu, na);
+          here = __all_sync(0xffffffffu, nx && na);
           if (!ok) break;
         }
       }
-      commit_by(done, lead);
+      if (elected()) mma_commit(done);
+      __syncwarp();
       if (!mbar_wait(done, 0, drain)) timed_out();   // before anyone frees TMEM
     }
     __syncwarp();
@@ -414,20 +415,19 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       place(tile, rt, tt);
       const uint8_t* zeros = L.zeros + (int64_t)rt * LIN_BLOCK + row;
       auto zero_of = [&](int chunk) { return (int)zeros[(L.G == 1 ? 0 : min(chunk / L.chunks, L.G - 1)) * L.mp]; };
-      // the zeros of this team's chunks of a block: one grid a block, or one a chunk
-      constexpr int NZ = S::X8 ? 4 : 2;
-      const int c0 = S::X8 ? 0 : 2 * team;
+      // the zeros of this team's two chunks of a block: one grid a block, or one a chunk
       const bool one = L.G == 1 || L.chunks % 4 == 0;
-      int z[NZ], zn[NZ];
-#pragma unroll
-      for (int j = 0; j < NZ; ++j) zn[j] = j == 0 || !one ? zero_of(kb0 * 4 + c0 + j) : zn[0];
+      int z[2], zn[2];
+      auto zeros_of = [&](int kb) {
+        if (S::X8) return;
+        zn[0] = zero_of(kb * 4 + 2 * team);
+        zn[1] = one ? zn[0] : zero_of(kb * 4 + 2 * team + 1);
+      };
+      zeros_of(kb0);
       for (int kb = kb0; kb < kb1; ++kb, ++ib) {
-#pragma unroll
-        for (int j = 0; j < NZ; ++j) z[j] = zn[j];
-        if (L.G > 1 && kb + 1 < kb1) {
-#pragma unroll
-          for (int j = 0; j < NZ; ++j) zn[j] = j == 0 || !one ? zero_of(kb * 4 + 4 + c0 + j) : zn[0];
-        }
+        z[0] = zn[0];
+        z[1] = zn[1];
+        if (L.G > 1 && kb + 1 < kb1) zeros_of(kb + 1);
         if (S::X8 && (ib & 1) != team) continue;
         const int sw = ib % S::NW, ia = S::X8 ? ib : 2 * ib + team, sa = ia % S::NA;
         if (!wait(&wF[sw], (uint32_t)(ib / S::NW) & 1u) || (ia >= S::NA && !wait_stage(ia - S::NA))) {
@@ -442,14 +442,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           uint4 q[4];
 #pragma unroll
           for (int t = 0; t < 4; ++t) q[t] = u[t * 128];
-          Table tab(z[0]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            if (j > 0 && z[j] != z[j - 1]) tab = Table(z[j]);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-              tab.eight(j == 0 ? q[t].x : j == 1 ? q[t].y : j == 2 ? q[t].z : q[t].w, a[8 * (j & 1) + 2 * t],
-                        a[8 * (j & 1) + 2 * t + 1]);
+              odd8(j == 0 ? q[t].x : j == 1 ? q[t].y : j == 2 ? q[t].z : q[t].w, a[8 * (j & 1) + 2 * t],
+                   a[8 * (j & 1) + 2 * t + 1]);
             if (j & 1) tmem_st16(to + 8 * (j - 1), a);
           }
         } else if constexpr (S::W8) {
@@ -503,7 +501,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       for (int i = 0; i < S::COLS; ++i) acc[i] = 0.f;
       Segments seg(P, kb0 * 4);
       for (int chunk = kb0 * 4; chunk < kb1 * 4; ++g) {
-        const float s = L.scales[(L.G == 1 ? 0 : seg.seg) * L.mp + row];
+        const int grid = L.G == 1 ? 0 : seg.seg;
+        const float s = L.scales[grid * L.mp + row] * (S::X8 ? 256.f : 1.f);
         const int buf = g % S::NACC;
         if (!wait(&cF[buf], (uint32_t)(g / S::NACC) & 1u)) {
           ok = false;
@@ -524,6 +523,19 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         if (lead) mbar_arrive(&cE[buf]);
         chunk = seg.left == INT_MAX ? INT_MAX : chunk + seg.left;
         seg.next();
+        if (S::X8 && (L.G > 1 || chunk >= kb1 * 4)) {
+          // the rest of c - z, 7.5 - z, with the sum of the grid's (of this part's) tokens
+          const float c = s * (1.f / 256.f) * (7.5f - (float)L.zeros[grid * L.mp + row]);
+          const float* sums = P.sums + (int64_t)(L.G == 1 ? part : grid) * P.sums_ld + tt * S::BN + ch * S::COLS;
+#pragma unroll
+          for (int i = 0; i < S::COLS; i += 4) {
+            const float4 x = __ldg(reinterpret_cast<const float4*>(sums + i));
+            acc[i] = fmaf(c, x.x, acc[i]);
+            acc[i + 1] = fmaf(c, x.y, acc[i + 1]);
+            acc[i + 2] = fmaf(c, x.z, acc[i + 2]);
+            acc[i + 3] = fmaf(c, x.w, acc[i + 3]);
+          }
+        }
       }
       if (!ok) break;
       if (S::BN <= 128 && P.splits > 1) {
@@ -594,6 +606,35 @@ __global__ void __launch_bounds__(256) k_linear_rows(const void* x, int64_t ldx,
   }
 }
 
+// Sums of e4m3 tokens' values over each of `pieces` ranges of `width` columns, a warp per
+// token (zeros for the padding tokens up to ld); the status word cleared beside.
+__global__ void __launch_bounds__(256)
+    k_token_sums(const uint8_t* x, int64_t ldx, int rows, int n, int pieces, int width, float* sums, int64_t ld, int* status) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
+  const int64_t tok = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (tok >= ld) return;
+  for (int p = 0; p < pieces; ++p) {
+    float s = 0.f;
+    if (tok < rows) {
+      const int64_t end = min((int64_t)n, (int64_t)(p + 1) * width);
+      for (int64_t k = (int64_t)p * width + 4 * lane; k < end; k += 128) {
+        uint32_t w = 0u;
+        if (k + 4 <= end) {      // rows start on 16 bytes, ranges on 32
+          w = *reinterpret_cast<const uint32_t*>(x + tok * ldx + k);
+        } else {
+          for (int j = 0; k + j < end; ++j) w |= (uint32_t)x[tok * ldx + k + j] << (8 * j);
+        }
+        const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3)));
+        const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3)));
+        s += (a.x + a.y) + (b.x + b.y);
+      }
+      s = warp_all(s, AddOp());
+    }
+    if (lane == 0) sums[p * ld + tok] = s;
+  }
+}
+
 template <class S>
 int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   static OncePerDevice once;
@@ -613,6 +654,17 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   P.splits = 1;
   if (S::BN <= 128)
     while (P.splits < 8 && tiles * P.splits * 2 <= ROW_SMS && L.kblocks >= 4 * P.splits) P.splits *= 2;
+  P.per = ceil_div(L.kblocks, P.splits);
+  if (S::X8) {
+    // no grid in two parts: a part ends where a grid does
+    int whole = 1;
+    while (L.G > 1 && whole * 4 % L.chunks != 0) ++whole;
+    P.per = (int)round_up(P.per, whole);
+    const int pieces = L.G == 1 ? P.splits : L.G, width = L.G == 1 ? P.per * LIN_BLOCK : L.chunks * 32;
+    k_token_sums<<<(unsigned)((P.sums_ld + 7) / 8), 256, 0, s>>>((const uint8_t*)x, ldx, L.rows, L.n, pieces, width,
+                                                               const_cast<float*>(P.sums), P.sums_ld, P.status);
+    BK_CUDA_OK(cudaGetLastError());
+  }
   CUtensorMap map;
   const cuuint64_t dims[2] = {(cuuint64_t)L.n, (cuuint64_t)L.rows};
   const cuuint64_t strides[1] = {(cuuint64_t)ldx * (S::X8 ? 1 : 2)};
@@ -666,9 +718,20 @@ static bool rows_in_place(const void* x, bool x8, int64_t ldx, bool bytes8) {
   return !(x8 && bytes8) && aligned16(x, x8 ? ldx : 2 * ldx);
 }
 
-size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8) {
-  if (rows_in_place(x, x8, ldx, bytes8)) return 256;
-  return 256 + (size_t)rows * (size_t)round_up(n, 16) * (x8 && !bytes8 ? 1 : 2);
+// Where the workspace keeps things: [status 256 B][e4m3 tokens' sums][tokens' copy].
+struct TcWorkspace {
+  int64_t sums_ld;
+  size_t off_copy, bytes;
+  TcWorkspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8, int G) {
+    sums_ld = round_up((int64_t)rows + 191, 64);     // whole token tiles, whichever their width
+    off_copy = 256 + (x8 && !bytes8 ? align256((size_t)std::max(G, 8) * sums_ld * 4) : 0);
+    bytes = off_copy;
+    if (!rows_in_place(x, x8, ldx, bytes8)) bytes += (size_t)rows * round_up(n, 16) * (x8 && !bytes8 ? 1 : 2);
+  }
+};
+
+size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8, int G) {
+  return TcWorkspace(x, x8, rows, ldx, n, bytes8, G).bytes;
 }
 
 int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cudaStream_t s) {
@@ -679,11 +742,14 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
   P.segs = L.G == 1 ? INT_MAX / SEG_CHUNKS - 1 : L.G;
   P.status = (int*)workspace;
   P.spin_cycles = spin_cycles_from_env();
-  BK_CUDA_OK(cudaMemsetAsync(workspace, 0, 256, s));
+  const TcWorkspace W(L.x, x8, L.rows, L.ldx, L.n, bytes8, L.G);
+  P.sums = (const float*)((char*)workspace + 256);
+  P.sums_ld = W.sums_ld;
+  if (!x8 || bytes8) BK_CUDA_OK(cudaMemsetAsync(workspace, 0, 4, s));
   const void* x = L.x;
   int64_t ldx = L.ldx;
   if (!rows_in_place(x, x8, ldx, bytes8)) {
-    void* out = (char*)workspace + 256;
+    void* out = (char*)workspace + W.off_copy;
     ldx = round_up(L.n, 16);
     if (!x8)
       k_linear_rows<false, false><<<L.rows, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);

@@ -139,7 +139,7 @@ def bakron_linear(x, weight: PackedWeight, x_scales=None, bias=None, activation=
     if y.data_ptr() != out.data_ptr():
         raise ValueError("out must have evenly spaced rows and a contiguous last dimension")
     dt = _DTYPES[x.dtype]
-    need = L.bakron_linear_workspace_bytes(x.data_ptr(), dt, rows, ldx, n, weight.qmax)
+    need = L.bakron_linear_workspace_bytes(x.data_ptr(), dt, rows, ldx, n, weight.qmax, weight.group_size)
     if need and workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     rc = L.bakron_linear(x.data_ptr(), dt, rows, ldx, _p(x_scales), weight.buf.data_ptr(), m, n, weight.qmax,
