@@ -61,6 +61,7 @@ struct TcShape {
   // registers a thread of each warpgroup, out of 5 x 96 as launched
   static constexpr bool SPLIT_REGS = BN >= 128;
   static constexpr int R_LOAD = 56, R_EXPAND = 72, R_SUM = 136;
+  static_assert((ND & (ND - 1)) == 0 && (NACC & (NACC - 1)) == 0, "masks");
   static_assert(ND >= NX && ND >= NA, "a barrier's phase is waited for before the next one can end");
   static_assert(ACC_COLS + NA * 32 <= 512, "TMEM");
   static_assert(SMEM <= 232448, "shared memory");
@@ -331,7 +332,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       constexpr uint32_t idesc = S::X8 ? idesc_e4m3(S::BN) : idesc_bf16(128, S::BN);
       constexpr int MPC = S::X8 ? 1 : 2;     // MMAs of a chunk
       const uint64_t desc0 = smem_desc(smem_u32(xring));
-      int it = 0, g = 0;
+      int g = 0;
+      uint32_t xs = 0, xp = 0, as = 0, ap = 0, ds = 0;     // slots and parities of the stage
       bool ok = true, here = false;
       auto sum_free = [&]() {     // before the first MMA of a segment
         return g < S::NACC || wait(&cE[g % S::NACC], (uint32_t)(g / S::NACC - 1) & 1u);
@@ -339,29 +341,26 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
         Segments seg(P, kb0 * 4);
         uint32_t more = 0;       // the segment has begun
-        const int st1 = kb1 * S::SPB;
-        for (int st = kb0 * S::SPB; st < st1; ++st, ++it) {
-          const int sx = it % S::NX, sa = it % S::NA, nt = it + 1;
-          if ((!here && (!wait(&xF[sx], (uint32_t)(it / S::NX) & 1u) || !wait(&aF[sa], (uint32_t)(it / S::NA) & 1u))) ||
-              (!more && !sum_free())) {
+        for (int left = (kb1 - kb0) * S::SPB; left > 0; --left) {
+          if ((!here && (!wait(&xF[xs], xp) || !wait(&aF[as], ap))) || (!more && !sum_free())) {
             ok = false;
             break;
           }
           // a look at the next stage's barriers, of no consequence until then
-          const bool nx = mbar_test(&xF[nt % S::NX], (uint32_t)(nt / S::NX) & 1u);
-          const bool na = mbar_test(&aF[nt % S::NA], (uint32_t)(nt / S::NA) & 1u);
+          const uint32_t nxs = xs + 1 == S::NX ? 0 : xs + 1, nas = as + 1 == S::NA ? 0 : as + 1;
+          const uint32_t nxp = xp ^ (uint32_t)(nxs == 0), nap = ap ^ (uint32_t)(nas == 0);
+          const bool nx = mbar_test(&xF[nxs], nxp), na = mbar_test(&aF[nas], nap);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint64_t b = desc0 + (uint64_t)((sx * S::XS) >> 4);
-          const uint32_t a = tmem_a + sa * 32;
+          const uint64_t b = desc0 + (uint64_t)(xs * (S::XS >> 4));
+          const uint32_t a = tmem_a + as * 32, d = tmem + (g & (S::NACC - 1)) * S::BN;
           if (seg.left >= S::CH) {       // no segment ends inside the stage
-            const uint32_t d = tmem + (g % S::NACC) * S::BN;
             if (seg.left != INT_MAX) seg.left -= S::CH;
-            const bool ends = seg.left == 0 || st == st1 - 1;
+            const bool ends = seg.left == 0 || left == 1;
             if (elected()) {
 #pragma unroll
               for (int k = 0; k < S::CH * MPC; ++k) mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k ? 1u : more);
-              mma_commit(&sD[it % S::ND]);
-              if (ends) mma_commit(&cF[g % S::NACC]);
+              mma_commit(&sD[ds]);
+              if (ends) mma_commit(&cF[g & (S::NACC - 1)]);
             }
             __syncwarp();
             more = 1;
@@ -377,14 +376,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 ok = sum_free();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               }
-              const uint32_t d = tmem + (g % S::NACC) * S::BN;
+              const uint32_t dc = tmem + (g & (S::NACC - 1)) * S::BN;
               if (seg.left != INT_MAX) --seg.left;
-              const bool ends = seg.left == 0 || (st == st1 - 1 && c == S::CH - 1);
+              const bool ends = seg.left == 0 || (left == 1 && c == S::CH - 1);
               if (elected()) {
                 for (int k = c * MPC; ok && k < (c + 1) * MPC; ++k)
-                  mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k > c * MPC ? 1u : more);
-                if (c == S::CH - 1) mma_commit(&sD[it % S::ND]);
-                if (ends) mma_commit(&cF[g % S::NACC]);
+                  mma_ts<S::X8>(dc, a + 8 * k, b + 2 * k, idesc, k > c * MPC ? 1u : more);
+                if (c == S::CH - 1) mma_commit(&sD[ds]);
+                if (ends) mma_commit(&cF[g & (S::NACC - 1)]);
               }
               __syncwarp();
               more = 1;
@@ -396,6 +395,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             }
           }
           here = __all_sync(0xffffffffu, nx && na);
+          xs = nxs;
+          xp = nxp;
+          as = nas;
+          ap = nap;
+          ds = (ds + 1) & (S::ND - 1);
           if (!ok) break;
         }
       }
