@@ -37,36 +37,40 @@ constexpr int TC_THREADS = 640;
 constexpr int SEG_CHUNKS = 32;           // a segment where a row has one grid: 1024 columns
 constexpr int TOKEN_GROUP = 16;          // token tiles that share a pass over the weight
 
-// The way out: an epilogue warp's 32 rows of 16 tokens at a time, token by token.
+// The way out: an epilogue warp's 32 rows of 8 tokens at a time, token by token.
 constexpr int STAGE_LD = 36;             // floats of a token: 16-byte reads of 8 lanes meet no bank twice
-constexpr uint32_t STAGE_BYTES = 8 * 16 * STAGE_LD * 4;
+constexpr uint32_t STAGE_BYTES = 8 * 8 * STAGE_LD * 4;
 
+// A stage is 256 bytes of a token (two boxes of 128): 128 bf16 columns or 256 e4m3 columns,
+// eight MMAs.  What an iteration of the issuing warp costs beside its MMAs (barriers,
+// fence, commit: some 200 cycles) is only partly hidden by the MMAs in the queue, so
+// a stage has as many as TMEM has room for (four a stage: 4096 x 28672 x 8192 in bf16 1.67 ms).
 template <int BN_, bool W8_, bool X8_>
 struct TcShape {
   static constexpr int BN = BN_;
   static constexpr bool W8 = W8_, X8 = X8_;
   static constexpr int NACC = 2;                         // accumulators of BN columns
-  static constexpr int NA = BN > 128 ? 4 : 8;            // A stages, 32 TMEM columns each
+  static constexpr int NA = BN > 128 ? 2 : 4;            // A stages, 64 TMEM columns each
   static constexpr int ACC_COLS = NACC * BN;
-  static constexpr int CH = X8 ? 4 : 2;                  // 32-column chunks of a stage
-  static constexpr int SPB = 4 / CH;                     // stages of a 128-column block
-  static constexpr uint32_t XS = BN * 128;               // bytes of a stage's tokens
+  static constexpr int BPS = X8 ? 2 : 1;                 // 128-column blocks of a stage
+  static constexpr int MPC = X8 ? 1 : 2;                 // MMAs of a 32-column chunk
+  static constexpr uint32_t BOX = BN * 128;              // bytes of a box of tokens
   static constexpr uint32_t WS = W8 ? 16384 : 8192;      // bytes of a block's codes
-  static constexpr int NX = BN > 128 ? 6 : 8;
-  static constexpr int ND = 8;                           // barriers of "the stage's MMAs are done"
-  static constexpr int NW = BN > 128 ? (W8 ? 3 : 6) : BN == 128 ? (W8 ? 4 : 8) : (W8 ? 6 : 12);
+  static constexpr int NX = BN > 128 ? 3 : 4;
+  static constexpr int NW = W8 ? (BN > 64 ? 4 : 6) : BN > 64 ? 8 : 12;
   static constexpr int COLS = BN / 2;                    // columns an epilogue warp sums
-  static constexpr uint32_t SMEM_USED = NX * XS + NW * WS + STAGE_BYTES + 1024 /*align*/ + 512 /*barriers*/;
+  static constexpr uint32_t SMEM_USED = 2 * NX * BOX + NW * WS + STAGE_BYTES + 1024 /*align*/ + 512 /*barriers*/;
   static constexpr uint32_t SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA an SM
   // registers a thread of each warpgroup, out of 5 x 96 as launched
   static constexpr bool SPLIT_REGS = BN >= 128;
   static constexpr int R_LOAD = 56, R_EXPAND = 72, R_SUM = 136;
+  static constexpr int ND = 4;                           // barriers of "the stage's MMAs are done"
   static_assert((ND & (ND - 1)) == 0 && (NACC & (NACC - 1)) == 0, "masks");
   static_assert(ND >= NX && ND >= NA, "a barrier's phase is waited for before the next one can end");
-  static_assert(ACC_COLS + NA * 32 <= 512, "TMEM");
+  static_assert(ACC_COLS + NA * 64 <= 512, "TMEM");
   static_assert(SMEM <= 232448, "shared memory");
   static_assert(R_LOAD + 2 * R_EXPAND + 2 * R_SUM <= 5 * 96, "registers");
-  static_assert((uint32_t)BN * 128 * 4 <= NX * XS || BN > 128, "parts of a split tile");
+  static_assert((uint32_t)BN * 128 * 4 <= 2 * NX * BOX || BN > 128, "parts of a split tile");
 };
 
 struct TcParams {
@@ -180,45 +184,35 @@ __device__ __forceinline__ void odd8(uint32_t w, uint32_t& o0, uint32_t& o1) {
   o1 = __byte_perm(a, b, 0x7531);
 }
 
-// 16 neighbouring rows' sums of one token (16-byte aligned in shared memory): epilogue and store.
-__device__ __forceinline__ void linear_store16(const LinearParams& L, const float* sums, int64_t tok, int row0) {
-  float v[16];
+// 8 neighbouring rows' sums of one token (16-byte aligned in shared memory): epilogue and store.
+__device__ __forceinline__ void linear_store8(const LinearParams& L, const float* sums, int64_t tok, int row0) {
+  float v[8], r[8];
+  load8(sums, v);
+  if (row0 + 8 > L.m || !L.yvec) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 f = reinterpret_cast<const float4*>(sums)[i];
-    v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
-  }
-  if (row0 + 16 > L.m || !L.yvec) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < 8; ++i)
       if (row0 + i < L.m) linear_store(L, v[i], tok, row0 + i);
     return;
   }
   const float xs = L.xscales ? L.xscales[tok] : 1.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 8; ++i) {
     v[i] *= xs;
     if (L.bias) v[i] += L.bias[row0 + i];
     v[i] = activate(v[i], L.activation);
   }
-#pragma unroll
-  for (int i = 0; i < 16; i += 8) {
-    float w[8], r[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = v[i + j];
-    if (L.residual) {
-      if (L.yf32)
-        load8((const float*)L.residual + tok * L.ldr + row0 + i, r);
-      else
-        load8((const __nv_bfloat16*)L.residual + tok * L.ldr + row0 + i, r);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] += r[j];
-    }
+  if (L.residual) {
     if (L.yf32)
-      store8((float*)L.y + tok * L.ldy + row0 + i, w);
+      load8((const float*)L.residual + tok * L.ldr + row0, r);
     else
-      store8((__nv_bfloat16*)L.y + tok * L.ldy + row0 + i, w);
+      load8((const __nv_bfloat16*)L.residual + tok * L.ldr + row0, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
   }
+  if (L.yf32)
+    store8((float*)L.y + tok * L.ldy + row0, v);
+  else
+    store8((__nv_bfloat16*)L.y + tok * L.ldy + row0, v);
 }
 
 template <class S>
@@ -226,7 +220,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     k_linear_tc(const __grid_constant__ CUtensorMap xmap, const TcParams P) {
   extern __shared__ __align__(1024) unsigned char tc_smem[];
   unsigned char* xring = (unsigned char*)(((uintptr_t)tc_smem + 1023) & ~(uintptr_t)1023);
-  unsigned char* wring = xring + S::NX * S::XS;
+  unsigned char* wring = xring + 2 * S::NX * S::BOX;
   float* stage = (float*)(wring + S::NW * S::WS);
   uint64_t* bars = (uint64_t*)((unsigned char*)stage + STAGE_BYTES);
   // full: xF tokens, wF codes, aF expanded codes, cF sums; free again: sD tokens and expanded
@@ -240,8 +234,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::NX; ++i) mbar_init(&xF[i], 1);
     for (int i = 0; i < S::ND; ++i) mbar_init(&sD[i], 1);
-    for (int i = 0; i < S::NA; ++i) mbar_init(&aF[i], 4);
-    for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], S::X8 ? 4 : 8);
+    for (int i = 0; i < S::NA; ++i) mbar_init(&aF[i], 8);
+    for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], S::X8 ? 4 : 8);   // the teams that read it
+
     for (int i = 0; i < S::NACC; ++i) mbar_init(&cF[i], 1), mbar_init(&cE[i], 8);
     mbar_init(done, 1);
     *abort_flag = 0;
@@ -260,7 +255,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   const LinearParams& L = P.L;
   const int tiles = P.row_tiles * P.token_tiles, part = blockIdx.x % P.splits;
   const int tile0 = blockIdx.x / P.splits, tile_step = gridDim.x / P.splits;
-  const int kb0 = part * P.per, kb1 = min(L.kblocks, kb0 + P.per);
+  const int kb0 = part * P.per, kb1 = max(kb0, min(L.kblocks, kb0 + P.per));
+  const int stages = ceil_div(kb1 - kb0, S::BPS);     // of a tile
   const long long drain = 4000000000LL;   // ~2 s: wind-down bound
   auto place = [&](int tile, int& rt, int& tt) {
     const int group = tile / (P.row_tiles * TOKEN_GROUP), in = tile - group * P.row_tiles * TOKEN_GROUP;
@@ -287,15 +283,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
         int rt, tt;
         place(tile, rt, tt);
-        for (int st = kb0 * S::SPB; st < kb1 * S::SPB; ++st, ++it) {
+        for (int st = 0; st < stages; ++st, ++it) {
           const int s = it % S::NX;
           if (it >= S::NX && !wait_stage(it - S::NX)) {
             ok = false;
             break;
           }
           if (lead) {
-            mbar_expect_tx(&xF[s], S::XS);
-            tma_load_2d(xring + s * S::XS, &xmap, &xF[s], st * S::CH * 32, tt * S::BN);
+            // the second box, unless it belongs to the next part (or to nobody)
+            const int col = (kb0 + st * S::BPS) * LIN_BLOCK;
+            const bool two = !S::X8 || kb0 + st * 2 + 1 < kb1;
+            unsigned char* to = xring + 2 * s * S::BOX;
+            mbar_expect_tx(&xF[s], two ? 2 * S::BOX : S::BOX);
+            tma_load_2d(to, &xmap, &xF[s], col, tt * S::BN);
+            if (two) tma_load_2d(to + S::BOX, &xmap, &xF[s], col + (S::X8 ? 128 : 64), tt * S::BN);
           }
           __syncwarp();
         }
@@ -330,18 +331,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       // (128 x 32, four a stage with two barrier tests, fence and commit) beside warps busy
       // on the same schedulers: elected 96, one lane all the way 117, predicated 194.
       constexpr uint32_t idesc = S::X8 ? idesc_e4m3(S::BN) : idesc_bf16(128, S::BN);
-      constexpr int MPC = S::X8 ? 1 : 2;     // MMAs of a chunk
       const uint64_t desc0 = smem_desc(smem_u32(xring));
       int g = 0;
       uint32_t xs = 0, xp = 0, as = 0, ap = 0, ds = 0;     // slots and parities of the stage
       bool ok = true, here = false;
       auto sum_free = [&]() {     // before the first MMA of a segment
-        return g < S::NACC || wait(&cE[g % S::NACC], (uint32_t)(g / S::NACC - 1) & 1u);
+        return g < S::NACC || wait(&cE[g & (S::NACC - 1)], (uint32_t)(g / S::NACC - 1) & 1u);
       };
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
         Segments seg(P, kb0 * 4);
         uint32_t more = 0;       // the segment has begun
-        for (int left = (kb1 - kb0) * S::SPB; left > 0; --left) {
+        for (int st = 0; st < stages; ++st) {
           if ((!here && (!wait(&xF[xs], xp) || !wait(&aF[as], ap))) || (!more && !sum_free())) {
             ok = false;
             break;
@@ -351,14 +351,18 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           const uint32_t nxp = xp ^ (uint32_t)(nxs == 0), nap = ap ^ (uint32_t)(nas == 0);
           const bool nx = mbar_test(&xF[nxs], nxp), na = mbar_test(&aF[nas], nap);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint64_t b = desc0 + (uint64_t)(xs * (S::XS >> 4));
-          const uint32_t a = tmem_a + as * 32, d = tmem + (g & (S::NACC - 1)) * S::BN;
-          if (seg.left >= S::CH) {       // no segment ends inside the stage
-            if (seg.left != INT_MAX) seg.left -= S::CH;
-            const bool ends = seg.left == 0 || left == 1;
+          const uint64_t b = desc0 + (uint64_t)(xs * (2 * S::BOX >> 4));
+          const uint32_t a = tmem_a + as * 64;
+          // MMA k of the stage: 8 TMEM columns of A, 32 bytes of the tokens' rows in box k / 4
+          const int nk = !S::X8 || kb0 + st * 2 + 1 < kb1 ? 8 : 4;
+          if (nk == 8 && seg.left >= 8 / S::MPC) {       // no segment ends inside the stage
+            if (seg.left != INT_MAX) seg.left -= 8 / S::MPC;
+            const bool ends = seg.left == 0 || st == stages - 1;
+            const uint32_t d = tmem + (g & (S::NACC - 1)) * S::BN;
             if (elected()) {
 #pragma unroll
-              for (int k = 0; k < S::CH * MPC; ++k) mma_ts<S::X8>(d, a + 8 * k, b + 2 * k, idesc, k ? 1u : more);
+              for (int k = 0; k < 8; ++k)
+                mma_ts<S::X8>(d, a + 8 * k, b + (k / 4) * (S::BOX >> 4) + 2 * (k % 4), idesc, k ? 1u : more);
               mma_commit(&sD[ds]);
               if (ends) mma_commit(&cF[g & (S::NACC - 1)]);
             }
@@ -371,21 +375,23 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             }
           } else {
 #pragma unroll 1
-            for (int c = 0; c < S::CH && ok; ++c) {
-              if (!more && c > 0) {
+            for (int k = 0; k < nk && ok;) {
+              if (!more && k > 0) {
                 ok = sum_free();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               }
-              const uint32_t dc = tmem + (g & (S::NACC - 1)) * S::BN;
-              if (seg.left != INT_MAX) --seg.left;
-              const bool ends = seg.left == 0 || (left == 1 && c == S::CH - 1);
+              const int run = seg.left < (nk - k) / S::MPC ? seg.left * S::MPC : nk - k;
+              if (seg.left != INT_MAX) seg.left -= run / S::MPC;
+              const bool ends = seg.left == 0 || (st == stages - 1 && k + run == nk);
+              const uint32_t d = tmem + (g & (S::NACC - 1)) * S::BN;
               if (elected()) {
-                for (int k = c * MPC; ok && k < (c + 1) * MPC; ++k)
-                  mma_ts<S::X8>(dc, a + 8 * k, b + 2 * k, idesc, k > c * MPC ? 1u : more);
-                if (c == S::CH - 1) mma_commit(&sD[ds]);
+                for (int j = k; ok && j < k + run; ++j)
+                  mma_ts<S::X8>(d, a + 8 * j, b + (j / 4) * (S::BOX >> 4) + 2 * (j % 4), idesc, j > k ? 1u : more);
+                if (k + run == nk) mma_commit(&sD[ds]);
                 if (ends) mma_commit(&cF[g & (S::NACC - 1)]);
               }
               __syncwarp();
+              k += run;
               more = 1;
               if (ends) {
                 ++g;
@@ -412,7 +418,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if constexpr (S::SPLIT_REGS) regs_down<S::R_EXPAND>();
     const int row = (warp & 3) * 32 + lane, team = (warp - 4) >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    int ib = 0;
+    int ib = 0, ia = 0;      // blocks and stages so far
     bool ok = true;
     for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
       int rt, tt;
@@ -428,19 +434,23 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         zn[1] = one ? zn[0] : zero_of(kb * 4 + 2 * team + 1);
       };
       zeros_of(kb0);
-      for (int kb = kb0; kb < kb1; ++kb, ++ib) {
+      for (int kb = kb0; kb < kb1; kb += S::BPS, ib += S::BPS, ++ia) {
         z[0] = zn[0];
         z[1] = zn[1];
         if (L.G > 1 && kb + 1 < kb1) zeros_of(kb + 1);
-        if (S::X8 && (ib & 1) != team) continue;
-        const int sw = ib % S::NW, ia = S::X8 ? ib : 2 * ib + team, sa = ia % S::NA;
-        if (!wait(&wF[sw], (uint32_t)(ib / S::NW) & 1u) || (ia >= S::NA && !wait_stage(ia - S::NA))) {
+        const int block = S::X8 ? ib + team : ib, sw = block % S::NW, sa = ia % S::NA;
+        if (S::X8 && kb + team >= kb1) {       // half a stage: nothing for this team
+          __syncwarp();
+          if (lead) mbar_arrive(&aF[sa]);
+          continue;
+        }
+        if (!wait(&wF[sw], (uint32_t)(block / S::NW) & 1u) || (ia >= S::NA && !wait_stage(ia - S::NA))) {
           ok = false;
           break;
         }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint4* u = reinterpret_cast<const uint4*>(wring + sw * S::WS) + row;
-        const uint32_t to = tmem_a + sa * 32 + lanes;
+        const uint32_t to = tmem_a + sa * 64 + team * 32 + lanes;
         uint32_t a[16];
         if constexpr (S::X8) {
           uint4 q[4];
@@ -489,6 +499,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           mbar_arrive(&wE[sw]);
         }
       }
+      if (S::X8 && ((kb1 - kb0) & 1)) --ib;      // the half stage had one block
     }
   } else {
     if constexpr (S::SPLIT_REGS) regs_up<S::R_SUM>();
@@ -547,20 +558,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
         for (int i = 0; i < S::COLS; ++i) ((float*)xring)[(ch * S::COLS + i) * 128 + q * 32 + lane] = acc[i];
       } else {
-        float* mine = stage + (warp - 12) * 16 * STAGE_LD;
-        const int row0 = rt * LIN_BLOCK + q * 32 + (lane & 1) * 16;
+        float* mine = stage + (warp - 12) * 8 * STAGE_LD;
+        const int row0 = rt * LIN_BLOCK + q * 32 + (lane & 3) * 8;
 #pragma unroll 1
-        for (int b = 0; b < S::COLS / 16; ++b) {
+        for (int b = 0; b < S::COLS / 8; ++b) {
           __syncwarp();
 #pragma unroll
-          for (int c = 0; c < S::COLS / 16; ++c)
+          for (int c = 0; c < S::COLS / 8; ++c)
             if (b == c) {     // registers: no index that is not constant
 #pragma unroll
-              for (int i = 0; i < 16; ++i) mine[i * STAGE_LD + lane] = acc[16 * c + i];
+              for (int i = 0; i < 8; ++i) mine[i * STAGE_LD + lane] = acc[8 * c + i];
             }
           __syncwarp();
-          const int64_t tok = (int64_t)tt * S::BN + ch * S::COLS + b * 16 + (lane >> 1);
-          if (tok < L.rows) linear_store16(L, mine + (lane >> 1) * STAGE_LD + (lane & 1) * 16, tok, row0);
+          const int64_t tok = (int64_t)tt * S::BN + ch * S::COLS + b * 8 + (lane >> 2);
+          if (tok < L.rows) linear_store8(L, mine + (lane >> 2) * STAGE_LD + (lane & 3) * 8, tok, row0);
         }
       }
     }
