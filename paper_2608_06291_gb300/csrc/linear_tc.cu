@@ -10,11 +10,11 @@
 //     and the second part is a product with the sum of a token's values, formed once per
 //     grid by k_token_sums.  (From c and z by table it took 15 instructions of the integer
 //     pipe for 8 codes, which bound the whole kernel; this takes 9.)
-// A grid's sum (a segment; 1024 columns where a row has one grid) accumulates in TMEM
+// A grid's sum (a segment; 64 MMAs' columns where a row has one grid) accumulates in TMEM
 // from zero; the epilogue warps multiply it by the grid's scale and add it in fp32
 // registers while the next one is formed.
 //
-// Roles: warp 0 loads tokens, warp 2 codes, warp 1 issues the MMAs, warps 4-7 and 8-11
+// Roles: warp 0 loads tokens, warp 2 codes, warp 3 what a grid needs, warp 1 issues the MMAs, warps 4-7 and 8-11
 // expand (every other stage each), warps 12-19 (two per lane quarter of TMEM) sum and write
 // out.  CTAs are persistent, or, where there are fewer tiles than SMs, up to 8 CTAs of a
 // cluster share a tile's columns and add their parts through each other's shared memory,
@@ -34,7 +34,7 @@ namespace bakron {
 namespace {
 
 constexpr int TC_THREADS = 640;
-constexpr int SEG_CHUNKS = 32;           // a segment where a row has one grid: 1024 columns
+constexpr int SEG_MMAS = 64;             // MMAs of a segment where a row has one grid: 1024 (2048) columns
 constexpr int TOKEN_GROUP = 16;          // token tiles that share a pass over the weight
 
 // The way out: an epilogue warp's 32 rows of 8 tokens at a time, token by token.
@@ -59,11 +59,15 @@ struct TcShape {
   static constexpr int NX = BN > 128 ? 3 : 4;
   static constexpr int NW = W8 ? (BN > 64 ? 4 : 6) : BN > 64 ? 8 : 12;
   static constexpr int COLS = BN / 2;                    // columns an epilogue warp sums
-  static constexpr uint32_t SMEM_USED = 2 * NX * BOX + NW * WS + STAGE_BYTES + 1024 /*align*/ + 512 /*barriers*/;
+  // what the epilogue needs of a grid: the tokens' sums, the rows' scales and zeros
+  static constexpr uint32_t GS_SCALES = X8 ? BN * 4 : 0, GS_ZEROS = GS_SCALES + LIN_BLOCK * 4;
+  static constexpr uint32_t GS = GS_ZEROS + LIN_BLOCK;
+  static constexpr int NG = 4;
+  static constexpr uint32_t SMEM_USED = 2 * NX * BOX + NW * WS + STAGE_BYTES + NG * GS + 1024 /*align*/ + 512 /*barriers*/;
   static constexpr uint32_t SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA an SM
   // registers a thread of each warpgroup, out of 5 x 96 as launched
   static constexpr bool SPLIT_REGS = BN >= 128;
-  static constexpr int R_LOAD = 56, R_EXPAND = 72, R_SUM = 136;
+  static constexpr int R_LOAD = 56, R_EXPAND = 64, R_SUM = 144;
   static constexpr int ND = 4;                           // barriers of "the stage's MMAs are done"
   static_assert((ND & (ND - 1)) == 0 && (NACC & (NACC - 1)) == 0, "masks");
   static_assert(ND >= NX && ND >= NA, "a barrier's phase is waited for before the next one can end");
@@ -222,11 +226,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   unsigned char* xring = (unsigned char*)(((uintptr_t)tc_smem + 1023) & ~(uintptr_t)1023);
   unsigned char* wring = xring + 2 * S::NX * S::BOX;
   float* stage = (float*)(wring + S::NW * S::WS);
-  uint64_t* bars = (uint64_t*)((unsigned char*)stage + STAGE_BYTES);
-  // full: xF tokens, wF codes, aF expanded codes, cF sums; free again: sD tokens and expanded
-  // codes of a stage, wE codes, cE sums
+  unsigned char* gring = (unsigned char*)stage + STAGE_BYTES;
+  uint64_t* bars = (uint64_t*)(gring + S::NG * S::GS);
+  // full: xF tokens, wF codes, aF expanded codes, cF sums, gF grids; free again: sD tokens and
+  // expanded codes of a stage, wE codes, cE sums, gE grids
   uint64_t *xF = bars, *sD = xF + S::NX, *wF = sD + S::ND, *wE = wF + S::NW, *aF = wE + S::NW, *cF = aF + S::NA,
-           *cE = cF + S::NACC, *done = cE + S::NACC;
+           *cE = cF + S::NACC, *gF = cE + S::NACC, *gE = gF + S::NG, *done = gE + S::NG;
   uint32_t* tmem_slot = (uint32_t*)(done + 1);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -238,6 +243,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], S::X8 ? 4 : 8);   // the teams that read it
 
     for (int i = 0; i < S::NACC; ++i) mbar_init(&cF[i], 1), mbar_init(&cE[i], 8);
+    for (int i = 0; i < S::NG; ++i) mbar_init(&gF[i], 1), mbar_init(&gE[i], 8);
     mbar_init(done, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -326,6 +332,40 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       }
       for (int j = it > S::NW ? it - S::NW : 0; j < it; ++j)
         if (!mbar_wait(&wF[j % S::NW], (uint32_t)(j / S::NW) & 1u, drain)) timed_out();
+    } else if (warp == 3) {
+      int it = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+        int rt, tt;
+        place(tile, rt, tt);
+        Segments seg(P, kb0 * 4);
+        // one for each segment, or one for the tile
+        for (int chunk = kb0 * 4; chunk < kb1 * 4; ++it) {
+          const int s = it % S::NG, grid = L.G == 1 ? 0 : seg.seg;
+          if (it >= S::NG && !wait(&gE[s], (uint32_t)(it / S::NG - 1) & 1u)) {
+            ok = false;
+            break;
+          }
+          if (lead) {
+            unsigned char* to = gring + s * S::GS;
+            mbar_expect_tx(&gF[s], S::GS);
+            const int64_t at = grid * L.mp + (int64_t)rt * LIN_BLOCK;
+            if (S::X8)
+              bulk_load(to, P.sums + (int64_t)(L.G == 1 ? part : grid) * P.sums_ld + tt * S::BN, S::BN * 4, &gF[s]);
+            bulk_load(to + S::GS_SCALES, L.scales + at, LIN_BLOCK * 4, &gF[s]);
+            bulk_load(to + S::GS_ZEROS, L.zeros + at, LIN_BLOCK, &gF[s]);
+          }
+          __syncwarp();
+          if (L.G == 1 || seg.left == INT_MAX) {
+            ++it;
+            break;
+          }
+          chunk += seg.left;
+          seg.next();
+        }
+      }
+      for (int j = it > S::NG ? it - S::NG : 0; j < it; ++j)
+        if (!mbar_wait(&gF[j % S::NG], (uint32_t)(j / S::NG) & 1u, drain)) timed_out();
     } else if (warp == 1) {
       // The warp goes through the loop together and an elected lane issues.  Cycles an MMA
       // (128 x 32, four a stage with two barrier tests, fence and commit) beside warps busy
@@ -380,13 +420,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 ok = sum_free();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               }
-              const int run = seg.left < (nk - k) / S::MPC ? seg.left * S::MPC : nk - k;
+              const int room = min(nk, (k / 4 + 1) * 4) - k;      // of this box
+              const int run = seg.left < room / S::MPC ? seg.left * S::MPC : room;
               if (seg.left != INT_MAX) seg.left -= run / S::MPC;
               const bool ends = seg.left == 0 || (st == stages - 1 && k + run == nk);
               const uint32_t d = tmem + (g & (S::NACC - 1)) * S::BN;
               if (elected()) {
-                for (int j = k; ok && j < k + run; ++j)
-                  mma_ts<S::X8>(d, a + 8 * j, b + (j / 4) * (S::BOX >> 4) + 2 * (j % 4), idesc, j > k ? 1u : more);
+                const uint64_t bk = b + (k / 4) * (S::BOX >> 4);
+                if (run == 4 && k % 4 == 0 && ok) {     // a box
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) mma_ts<S::X8>(d, a + 8 * (k + j), bk + 2 * j, idesc, j ? 1u : more);
+                } else {
+                  for (int j = k; ok && j < k + run; ++j)
+                    mma_ts<S::X8>(d, a + 8 * j, b + (j / 4) * (S::BOX >> 4) + 2 * (j % 4), idesc, j > k ? 1u : more);
+                }
                 if (k + run == nk) mma_commit(&sD[ds]);
                 if (ends) mma_commit(&cF[g & (S::NACC - 1)]);
               }
@@ -505,51 +552,69 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if constexpr (S::SPLIT_REGS) regs_up<S::R_SUM>();
     const int q = warp & 3, ch = (warp - 12) >> 2;      // lane quarter, half of the columns
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
-    int g = 0;
+    int g = 0, ig = 0;
     bool ok = true;
     for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
       int rt, tt;
       place(tile, rt, tt);
-      const int row = rt * LIN_BLOCK + q * 32 + lane;
       float acc[S::COLS];
 #pragma unroll
       for (int i = 0; i < S::COLS; ++i) acc[i] = 0.f;
       Segments seg(P, kb0 * 4);
+      float s = 0.f;
+      const unsigned char* grid = nullptr;
       for (int chunk = kb0 * 4; chunk < kb1 * 4; ++g) {
-        const int grid = L.G == 1 ? 0 : seg.seg;
-        const float s = L.scales[grid * L.mp + row] * (S::X8 ? 256.f : 1.f);
-        const int buf = g % S::NACC;
+        if (L.G > 1 || chunk == kb0 * 4) {       // the next grid
+          if (!wait(&gF[ig % S::NG], (uint32_t)(ig / S::NG) & 1u)) {
+            ok = false;
+            break;
+          }
+          grid = gring + (ig % S::NG) * S::GS;
+          s = reinterpret_cast<const float*>(grid + S::GS_SCALES)[q * 32 + lane] * (S::X8 ? 256.f : 1.f);
+        }
+        const int buf = g & (S::NACC - 1);
         if (!wait(&cF[buf], (uint32_t)(g / S::NACC) & 1u)) {
           ok = false;
           break;
         }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t at = tmem + lanes + buf * S::BN + ch * S::COLS;
+        constexpr int LD = S::COLS % 32 == 0 ? 32 : 16;
 #pragma unroll
-        for (int c = 0; c < S::COLS; c += 16) {
-          uint32_t r[16];
-          tmem_ld16(at + c, r);
+        for (int c = 0; c < S::COLS; c += LD) {
+          uint32_t r[LD];
+          if constexpr (LD == 32)
+            tmem_ld32(at + c, r);
+          else
+            tmem_ld16(at + c, r);
           tmem_wait_ld();
+          if (c + LD == S::COLS) {      // all read: the next segment's MMAs may have it
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lead) mbar_arrive(&cE[buf]);
+          }
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[c + i] = fmaf(s, __uint_as_float(r[i]), acc[c + i]);
+          for (int i = 0; i < LD; ++i) acc[c + i] = fmaf(s, __uint_as_float(r[i]), acc[c + i]);
         }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lead) mbar_arrive(&cE[buf]);
         chunk = seg.left == INT_MAX ? INT_MAX : chunk + seg.left;
         seg.next();
-        if (S::X8 && (L.G > 1 || chunk >= kb1 * 4)) {
-          // the rest of c - z, 7.5 - z, with the sum of the grid's (of this part's) tokens
-          const float c = s * (1.f / 256.f) * (7.5f - (float)L.zeros[grid * L.mp + row]);
-          const float* sums = P.sums + (int64_t)(L.G == 1 ? part : grid) * P.sums_ld + tt * S::BN + ch * S::COLS;
+        if (L.G > 1 || chunk >= kb1 * 4) {
+          if constexpr (S::X8) {
+            // the rest of c - z, 7.5 - z, with the sum of the grid's (of this part's) tokens
+            const float c = s * (1.f / 256.f) * (7.5f - (float)grid[S::GS_ZEROS + q * 32 + lane]);
+            const float4* sums = reinterpret_cast<const float4*>(grid) + ch * (S::COLS / 4);
 #pragma unroll
-          for (int i = 0; i < S::COLS; i += 4) {
-            const float4 x = __ldg(reinterpret_cast<const float4*>(sums + i));
-            acc[i] = fmaf(c, x.x, acc[i]);
-            acc[i + 1] = fmaf(c, x.y, acc[i + 1]);
-            acc[i + 2] = fmaf(c, x.z, acc[i + 2]);
-            acc[i + 3] = fmaf(c, x.w, acc[i + 3]);
+            for (int i = 0; i < S::COLS; i += 4) {
+              const float4 x = sums[i / 4];
+              acc[i] = fmaf(c, x.x, acc[i]);
+              acc[i + 1] = fmaf(c, x.y, acc[i + 1]);
+              acc[i + 2] = fmaf(c, x.z, acc[i + 2]);
+              acc[i + 3] = fmaf(c, x.w, acc[i + 3]);
+            }
           }
+          __syncwarp();
+          if (lead) mbar_arrive(&gE[ig % S::NG]);
+          ++ig;
         }
       }
       if (!ok) break;
@@ -753,8 +818,8 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
   TcParams P{};
   P.L = L;
   P.row_tiles = (int)(L.mp / LIN_BLOCK);
-  P.seg_chunks = L.G == 1 ? SEG_CHUNKS : L.chunks;
-  P.segs = L.G == 1 ? INT_MAX / SEG_CHUNKS - 1 : L.G;
+  P.seg_chunks = L.G > 1 ? L.chunks : x8 && !bytes8 ? SEG_MMAS : SEG_MMAS / 2;
+  P.segs = L.G > 1 ? L.G : INT_MAX / SEG_MMAS - 1;
   P.status = (int*)workspace;
   P.spin_cycles = spin_cycles_from_env();
   const TcWorkspace W(L.x, x8, L.rows, L.ldx, L.n, bytes8, L.G);
