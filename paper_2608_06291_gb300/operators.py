@@ -4,75 +4,80 @@ probabilities of given tokens, and the gradients of the last two.
 
 Tensors may have any number of leading dimensions where their rows are evenly
 spaced (or else are copied); the last dimension is contiguous.  Work is enqueued on
-``stream`` (default: the current one).
+``stream`` (default: the current one), and what a call allocates or copies belongs to it.
+A decoding step's kernels take a few microseconds, less than a careless binding, so the
+usual case (contiguous tensors, one GPU) goes through few Python operations.
 """
 from __future__ import annotations
-
-import functools
 
 import torch
 
 from .bakron import BF16, E4M3, F32, OK, BakronError, lib
 
-_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+_F32, _BF16, _E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+_DTYPES = {_F32: F32, _BF16: BF16, _E4M3: E4M3}
 _ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
+_empty = torch.empty
+
+try:     # the stream's handle without a Stream object around it
+    from torch._C import _cuda_getCurrentRawStream as _raw_stream
+except ImportError:
+    def _raw_stream(index):
+        return torch.cuda.current_stream(index).cuda_stream
 
 
-def _check(rc, what):
-    if rc != OK:
-        raise BakronError(rc, what)
+def _names(dtypes):
+    return " or ".join(str(d)[6:] for d in dtypes)
 
 
-def _rows(t, name, dtypes, device=None):
-    """t as rows x d: (tensor, number of rows, row stride in elements)."""
+def _rows(t, name, dtypes, device):
+    """t as rows x d: (tensor, number of rows, row stride in elements).  device: an index."""
     if t.dtype not in dtypes:
-        raise ValueError(f"{name} must be {' or '.join(str(d)[6:] for d in dtypes)}")
-    if not t.is_cuda or t.dim() < 1 or (device is not None and t.device != device):
-        raise ValueError(f"{name} must be a CUDA tensor" + ("" if device is None else f" on {device}"))
+        raise ValueError(f"{name} must be {_names(dtypes)}")
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{name} must be a CUDA tensor" + (f" on cuda:{device}" if device >= 0 else ""))
     d = t.shape[-1]
-    if t.dim() != 2:
-        t = t.reshape(-1, d) if d else t.reshape(0, 0)
+    if t.is_contiguous():
+        return t, t.numel() // d if d else 0, d
+    t = t.reshape(-1, d)
     if t.stride(1) != 1 and d > 1 or t.shape[0] > 1 and t.stride(0) < d:
         t = t.contiguous()
     return t, t.shape[0], max(t.stride(0), d)
 
 
-def _vector(t, n, name, dtypes, device):
-    if t is None:
-        return None
-    if t.device != device or t.dtype not in dtypes or t.numel() != n:
-        raise ValueError(f"{name} must be {n} values of {' or '.join(str(d)[6:] for d in dtypes)} on {device}")
-    return t.contiguous()
-
-
 def _like(t, shape, name, dtype, device):
     """A tensor of the shape and type asked for, as rows."""
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}")
     return _rows(t, name, (dtype,), device)
 
 
-def _p(t):
-    return None if t is None else t.data_ptr()
+def _result(t, shape, name, dtype, device):
+    r, _, ld = _like(t, shape, name, dtype, device)
+    if r.data_ptr() != t.data_ptr():
+        raise ValueError(f"{name} must have evenly spaced rows and a contiguous last dimension")
+    return ld
 
 
-def _placed(fn):
-    """Runs fn on the device of its first argument and on ``stream``: also what fn copies
-    and allocates belongs to that stream."""
-    @functools.wraps(fn)
-    def call(t, *args, stream=None, **kwargs):
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return call(t, *args, **kwargs)
-        if t.is_cuda and t.device.index != torch.cuda.current_device():
-            with torch.cuda.device(t.device):
-                return fn(t, *args, **kwargs)
-        return fn(t, *args, **kwargs)
-    return call
+def _vector(t, n, name, dtypes, device):
+    if t.dtype not in dtypes or t.numel() != n or t.get_device() != device:
+        raise ValueError(f"{name} must be {n} values of {_names(dtypes)} on cuda:{device}")
+    return t if t.is_contiguous() else t.contiguous()
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+_gpus = 0
+
+
+def _elsewhere(t, stream):
+    """Whether a call has to be made again on another stream or device: the context."""
+    global _gpus
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    if not _gpus:
+        _gpus = torch.cuda.device_count()
+    if _gpus > 1 and t.is_cuda and t.get_device() != torch.cuda.current_device():
+        return torch.cuda.device(t.get_device())
+    return None
 
 
 class PackedWeight:
@@ -86,169 +91,216 @@ class PackedWeight:
         return self.buf.device
 
 
-@_placed
-def bakron_pack_weight(codes, scales, zeros, qmax: int, group_size: int = 0) -> PackedWeight:
+def bakron_pack_weight(codes, scales, zeros, qmax: int, group_size: int = 0, stream=None) -> PackedWeight:
     """Lay out codes (m x n uint8, 0..qmax), scales and zeros (m x G fp32) as the solve
     leaves them: code c of row i, group g stands for s[i, g] (c - z[i, g]).  group_size 0
     or a multiple of 32.  4 bits a code up to qmax 15, else 8.  Synchronous."""
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(codes, stream)
+        if there is not None:
+            with there:
+                return bakron_pack_weight(codes, scales, zeros, qmax, group_size)
     if codes.dim() != 2:
         raise ValueError("codes must be m x n")
-    codes, m, ldc = _rows(codes, "codes", (torch.uint8,))
-    n, group_size = codes.shape[1], int(group_size)
+    dev = codes.get_device()
+    codes, m, ldc = _rows(codes, "codes", (torch.uint8,), dev)
+    n, group_size, qmax = codes.shape[1], int(group_size), int(qmax)
     G = 1 if group_size <= 0 else n // group_size
-    dev = codes.device
-    scales = _like(scales, (m, G), "scales", torch.float32, dev)[0].contiguous()
-    zeros = _like(zeros, (m, G), "zeros", torch.float32, dev)[0].contiguous()
+    scales = _like(scales, (m, G), "scales", _F32, dev)[0].contiguous()
+    zeros = _like(zeros, (m, G), "zeros", _F32, dev)[0].contiguous()
     L = lib()
-    size = L.bakron_packed_bytes(m, n, int(qmax), group_size)
-    buf = torch.empty(size, dtype=torch.uint8, device=dev)
-    _check(L.bakron_pack_weight(codes.data_ptr(), ldc, scales.data_ptr(), zeros.data_ptr(), m, n, int(qmax),
-                                group_size, buf.data_ptr(), size, _stream(dev)), "bakron_pack_weight")
-    return PackedWeight(m, n, int(qmax), group_size, buf)
+    size = L.bakron_packed_bytes(m, n, qmax, group_size)
+    buf = _empty(size, dtype=torch.uint8, device=dev)
+    rc = L.bakron_pack_weight(codes.data_ptr(), ldc, scales.data_ptr(), zeros.data_ptr(), m, n, qmax, group_size,
+                              buf.data_ptr(), size, _raw_stream(dev))
+    if rc != OK:
+        raise BakronError(rc, "bakron_pack_weight")
+    return PackedWeight(m, n, qmax, group_size, buf)
 
 
-@_placed
 def bakron_linear(x, weight: PackedWeight, x_scales=None, bias=None, activation=None, residual=None,
-                  out_dtype=torch.bfloat16, out=None, workspace=None, sync: bool = False):
+                  out_dtype=_BF16, out=None, workspace=None, sync: bool = False, stream=None):
     """act(x What^T + bias) + residual for the tokens x (... x n, bfloat16 or
     float8_e4m3fn with ``x_scales``, one fp32 a token).  ``activation``: None, "relu",
     "silu" or "gelu".  ``bias``: m fp32; ``residual`` and the result (... x m): ``out_dtype``,
     bfloat16 or float32.  ``out`` may be ``residual``.  ``sync``: wait, and raise what the
     device reports (``bakron_read_status(workspace)`` tells it later)."""
-    shape, dev = x.shape, weight.buf.device
-    x, rows, ldx = _rows(x, "x", (torch.bfloat16, torch.float8_e4m3fn), dev)
-    m, n = weight.m, weight.n
-    if x.shape[1] != n:
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(x, stream)
+        if there is not None:
+            with there:
+                return bakron_linear(x, weight, x_scales, bias, activation, residual, out_dtype, out, workspace, sync)
+    m, n, dev = weight.m, weight.n, weight.buf.get_device()
+    shape = x.shape
+    x, rows, ldx = _rows(x, "x", (_BF16, _E4M3), dev)
+    if shape[-1] != n:
         raise ValueError(f"x must have {n} columns")
-    if activation not in _ACTIVATIONS:
+    act = _ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"activation must be one of {[a for a in _ACTIVATIONS if a]} or None")
     if out is not None:
         out_dtype = out.dtype
-    if out_dtype not in (torch.bfloat16, torch.float32):
+    if out_dtype is not _BF16 and out_dtype is not _F32:
         raise ValueError("the result must be bfloat16 or float32")
-    yshape = (*shape[:-1], m)
-    x_scales = _vector(x_scales, rows, "x_scales", (torch.float32,), dev)
-    bias = _vector(bias, m, "bias", (torch.float32,), dev)
-    ldr = 0
+    yshape = shape[:-1] + (m,)
+    xs = b = r = ws = None
+    ldr = size = 0
+    if x_scales is not None:
+        x_scales = _vector(x_scales, rows, "x_scales", (_F32,), dev)
+        xs = x_scales.data_ptr()
+    if bias is not None:
+        bias = _vector(bias, m, "bias", (_F32,), dev)
+        b = bias.data_ptr()
     if residual is not None:
         residual, _, ldr = _like(residual, yshape, "residual", out_dtype, dev)
-    L = lib()
+        r = residual.data_ptr()
     if out is None:
-        out = torch.empty(yshape, dtype=out_dtype, device=dev)
-    y, _, ldy = _like(out, yshape, "out", out_dtype, dev)
-    if y.data_ptr() != out.data_ptr():
-        raise ValueError("out must have evenly spaced rows and a contiguous last dimension")
-    dt = _DTYPES[x.dtype]
-    need = L.bakron_linear_workspace_bytes(x.data_ptr(), dt, rows, ldx, n, weight.qmax, weight.group_size)
-    if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    rc = L.bakron_linear(x.data_ptr(), dt, rows, ldx, _p(x_scales), weight.buf.data_ptr(), m, n, weight.qmax,
-                         weight.group_size, _p(bias), _ACTIVATIONS[activation], _p(residual), ldr,
-                         y.data_ptr(), _DTYPES[out_dtype], ldy, _p(workspace),
-                         0 if workspace is None else workspace.numel(), 1 if sync else 0, _stream(dev))
+        out, ldy = _empty(yshape, dtype=out_dtype, device=dev), m
+    else:
+        ldy = _result(out, yshape, "out", out_dtype, dev)
+    L = lib()
+    px, dt = x.data_ptr(), _DTYPES[x.dtype]
+    if workspace is None:
+        size = L.bakron_linear_workspace_bytes(px, dt, rows, ldx, n, weight.qmax, weight.group_size)
+        if size:
+            workspace = _empty(size, dtype=torch.uint8, device=dev)
+    if workspace is not None:
+        ws, size = workspace.data_ptr(), workspace.numel()
+    rc = L.bakron_linear(px, dt, rows, ldx, xs, weight.buf.data_ptr(), m, n, weight.qmax, weight.group_size, b, act, r,
+                         ldr, out.data_ptr(), _DTYPES[out_dtype], ldy, ws, size, 1 if sync else 0,
+                         _raw_stream(dev))
     if rc != OK:
         raise BakronError(rc, "bakron_linear")
     return out
 
 
-@_placed
-def bakron_rmsnorm(x, weight, eps: float = 1e-6, residual=None, out_dtype=None):
+def bakron_rmsnorm(x, weight, eps: float = 1e-6, residual=None, out_dtype=None, stream=None):
     """h = x + residual, y = weight h / sqrt(mean(h^2) + eps) over the last dimension.
     Returns (y, scales, h): y of ``out_dtype`` (default x's; or float8_e4m3fn with
     ``scales``, one fp32 a row, else None), h of x's type (None without a residual)."""
-    shape, dev, dtype = x.shape, x.device, x.dtype
-    x, rows, ldx = _rows(x, "x", (torch.float32, torch.bfloat16))
-    d = x.shape[1]
-    weight = _vector(weight, d, "weight", (torch.float32, torch.bfloat16), dev)
-    out_dtype = out_dtype or dtype
-    if out_dtype not in (dtype, torch.float8_e4m3fn):
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(x, stream)
+        if there is not None:
+            with there:
+                return bakron_rmsnorm(x, weight, eps, residual, out_dtype)
+    shape, dev, dtype = x.shape, x.get_device(), x.dtype
+    x, rows, ldx = _rows(x, "x", (_F32, _BF16), dev)
+    d = shape[-1]
+    weight = _vector(weight, d, "weight", (_F32, _BF16), dev)
+    if out_dtype is None:
+        out_dtype = dtype
+    elif out_dtype is not dtype and out_dtype is not _E4M3:
         raise ValueError("out_dtype must be x's or float8_e4m3fn")
+    y = _empty(shape, dtype=out_dtype, device=dev)
+    scales = h = s = ph = r = None
     ldr = 0
     if residual is not None:
         residual, _, ldr = _like(residual, shape, "residual", dtype, dev)
-    L = lib()
-    y = torch.empty(shape, dtype=out_dtype, device=dev)
-    h = torch.empty(shape, dtype=dtype, device=dev) if residual is not None else None
-    scales = torch.empty(shape[:-1], dtype=torch.float32, device=dev) if out_dtype != dtype else None
-    rc = L.bakron_rmsnorm(x.data_ptr(), _DTYPES[dtype], rows, d, ldx, _p(residual), ldr, weight.data_ptr(),
-                          _DTYPES[weight.dtype], float(eps), _p(h), d, y.data_ptr(), _DTYPES[out_dtype], d,
-                          _p(scales), _stream(dev))
+        h = _empty(shape, dtype=dtype, device=dev)
+        ph, r = h.data_ptr(), residual.data_ptr()
+    if out_dtype is _E4M3:
+        scales = _empty(shape[:-1], dtype=_F32, device=dev)
+        s = scales.data_ptr()
+    rc = lib().bakron_rmsnorm(x.data_ptr(), _DTYPES[dtype], rows, d, ldx, r, ldr, weight.data_ptr(),
+                              _DTYPES[weight.dtype], eps, ph, d, y.data_ptr(), _DTYPES[out_dtype], d, s,
+                              _raw_stream(dev))
     if rc != OK:
         raise BakronError(rc, "bakron_rmsnorm")
     return y, scales, h
 
 
-@_placed
-def bakron_rmsnorm_backward(dy, h, weight, eps: float = 1e-6, dsum=None):
+def bakron_rmsnorm_backward(dy, h, weight, eps: float = 1e-6, dsum=None, stream=None):
     """Gradients of y = weight h / sqrt(mean(h^2) + eps), given dy and the gradient ``dsum``
     that reaches h past the norm.  Returns (dx of h's type, dweight fp32)."""
-    shape, dev, dtype = h.shape, h.device, h.dtype
-    h, rows, ldh = _rows(h, "h", (torch.float32, torch.bfloat16))
-    d = h.shape[1]
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(dy, stream)
+        if there is not None:
+            with there:
+                return bakron_rmsnorm_backward(dy, h, weight, eps, dsum)
+    shape, dev, dtype = h.shape, h.get_device(), h.dtype
+    h, rows, ldh = _rows(h, "h", (_F32, _BF16), dev)
+    d = shape[-1]
     dy, _, lddy = _like(dy, shape, "dy", dtype, dev)
-    weight = _vector(weight, d, "weight", (torch.float32, torch.bfloat16), dev)
-    ldds = 0
+    weight = _vector(weight, d, "weight", (_F32, _BF16), dev)
+    ps, ldds = None, 0
     if dsum is not None:
         dsum, _, ldds = _like(dsum, shape, "dsum", dtype, dev)
+        ps = dsum.data_ptr()
     L = lib()
-    dx = torch.empty(shape, dtype=dtype, device=dev)
-    dw = torch.empty(d, dtype=torch.float32, device=dev)
+    dx = _empty(shape, dtype=dtype, device=dev)
+    dw = _empty(d, dtype=_F32, device=dev)
     size = L.bakron_rmsnorm_backward_workspace_bytes(rows, d)
-    ws = torch.empty(size, dtype=torch.uint8, device=dev)
+    ws = _empty(size, dtype=torch.uint8, device=dev)
     rc = L.bakron_rmsnorm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, _DTYPES[dtype], rows, d,
-                                   weight.data_ptr(), _DTYPES[weight.dtype], float(eps), _p(dsum), ldds,
-                                   dx.data_ptr(), d, dw.data_ptr(), ws.data_ptr(), size, _stream(dev))
+                                   weight.data_ptr(), _DTYPES[weight.dtype], eps, ps, ldds, dx.data_ptr(), d,
+                                   dw.data_ptr(), ws.data_ptr(), size, _raw_stream(dev))
     if rc != OK:
         raise BakronError(rc, "bakron_rmsnorm_backward")
     return dx, dw
 
 
-@_placed
-def bakron_token_logprobs(logits, targets=None, top: int = 0):
+def bakron_token_logprobs(logits, targets=None, top: int = 0, stream=None):
     """Log probabilities of the tokens ``targets`` (int64; outside 0..v-1: not scored, 0)
     under logits (... x v, float32 or bfloat16).  Returns (logp, entropy, lse, top_logp,
     top_ids): logp None without targets, the last two (... x top; fp32 and int32; the
     larger first, then the lower index) None without ``top``."""
-    shape, dev = logits.shape, logits.device
-    logits, rows, ldl = _rows(logits, "logits", (torch.float32, torch.bfloat16))
-    v, top = logits.shape[1], int(top)
-    targets = _vector(targets, rows, "targets", (torch.int64,), dev)
-    L = lib()
-    scalars = torch.empty((3, *shape[:-1]), dtype=torch.float32, device=dev)
-    logp, entropy, lse = scalars
-    top_logp = torch.empty((*shape[:-1], top), dtype=torch.float32, device=dev) if top > 0 else None
-    top_ids = torch.empty((*shape[:-1], top), dtype=torch.int32, device=dev) if top > 0 else None
-    if targets is None:
-        logp = None
-    rc = L.bakron_token_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], rows, v, ldl, _p(targets), top,
-                                 _p(logp), entropy.data_ptr(), lse.data_ptr(), _p(top_logp), _p(top_ids),
-                                 _stream(dev))
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(logits, stream)
+        if there is not None:
+            with there:
+                return bakron_token_logprobs(logits, targets, top)
+    shape, dev = logits.shape, logits.get_device()
+    logits, rows, ldl = _rows(logits, "logits", (_F32, _BF16), dev)
+    lead = shape[:-1]
+    t = pl = logp = top_logp = top_ids = pv = pi = None
+    if targets is not None:
+        targets = _vector(targets, rows, "targets", (torch.int64,), dev)
+        logp = _empty(lead, dtype=_F32, device=dev)
+        t, pl = targets.data_ptr(), logp.data_ptr()
+    entropy, lse = _empty(lead, dtype=_F32, device=dev), _empty(lead, dtype=_F32, device=dev)
+    if top > 0:
+        top_logp = _empty(lead + (top,), dtype=_F32, device=dev)
+        top_ids = _empty(lead + (top,), dtype=torch.int32, device=dev)
+        pv, pi = top_logp.data_ptr(), top_ids.data_ptr()
+    rc = lib().bakron_token_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], rows, shape[-1], ldl, t, top, pl,
+                                     entropy.data_ptr(), lse.data_ptr(), pv, pi, _raw_stream(dev))
     if rc != OK:
         raise BakronError(rc, "bakron_token_logprobs")
     return logp, entropy, lse, top_logp, top_ids
 
 
-@_placed
-def bakron_token_logprobs_backward(logits, targets, lse, dlogp, entropy=None, dentropy=None, out=None):
+def bakron_token_logprobs_backward(logits, targets, lse, dlogp, entropy=None, dentropy=None, out=None, stream=None):
     """The gradient at the logits of sum(dlogp logp + dentropy entropy), in their type;
     ``lse`` and ``entropy`` from ``bakron_token_logprobs``.  Either gradient may be None;
     ``out`` may be ``logits``."""
-    shape, dev, dtype = logits.shape, logits.device, logits.dtype
-    logits, rows, ldl = _rows(logits, "logits", (torch.float32, torch.bfloat16))
-    v = logits.shape[1]
-    f32 = (torch.float32,)
-    targets = _vector(targets, rows, "targets", (torch.int64,), dev)
-    lse, dlogp = _vector(lse, rows, "lse", f32, dev), _vector(dlogp, rows, "dlogp", f32, dev)
-    entropy, dentropy = _vector(entropy, rows, "entropy", f32, dev), _vector(dentropy, rows, "dentropy", f32, dev)
-    L = lib()
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(logits, stream)
+        if there is not None:
+            with there:
+                return bakron_token_logprobs_backward(logits, targets, lse, dlogp, entropy, dentropy, out)
+    shape, dev, dtype = logits.shape, logits.get_device(), logits.dtype
+    logits, rows, ldl = _rows(logits, "logits", (_F32, _BF16), dev)
+    v, f32 = shape[-1], (_F32,)
+    t = g = e = u = None
+    if targets is not None:
+        targets = _vector(targets, rows, "targets", (torch.int64,), dev)
+        t = targets.data_ptr()
+    lse = _vector(lse, rows, "lse", f32, dev)
+    if dlogp is not None:
+        dlogp = _vector(dlogp, rows, "dlogp", f32, dev)
+        g = dlogp.data_ptr()
+    if entropy is not None:
+        entropy = _vector(entropy, rows, "entropy", f32, dev)
+        e = entropy.data_ptr()
+    if dentropy is not None:
+        dentropy = _vector(dentropy, rows, "dentropy", f32, dev)
+        u = dentropy.data_ptr()
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=dev)
-    d, _, ldd = _like(out, shape, "out", dtype, dev)
-    if d.data_ptr() != out.data_ptr():
-        raise ValueError("out must have evenly spaced rows and a contiguous last dimension")
-    rc = L.bakron_token_logprobs_backward(logits.data_ptr(), _DTYPES[dtype], rows, v, ldl, _p(targets),
-                                          _p(lse), _p(dlogp), _p(entropy), _p(dentropy), d.data_ptr(), ldd,
-                                          _stream(dev))
+        out, ldd = _empty(shape, dtype=dtype, device=dev), v
+    else:
+        ldd = _result(out, shape, "out", dtype, dev)
+    rc = lib().bakron_token_logprobs_backward(logits.data_ptr(), _DTYPES[dtype], rows, v, ldl, t, lse.data_ptr(), g,
+                                              e, u, out.data_ptr(), ldd, _raw_stream(dev))
     if rc != OK:
         raise BakronError(rc, "bakron_token_logprobs_backward")
     return out
