@@ -672,7 +672,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 template <bool X8, bool WIDEN>
 __global__ void __launch_bounds__(256) k_linear_rows(const void* x, int64_t ldx, int rows, int n, void* out, int64_t ldo) {
   const int64_t row = blockIdx.x;
-  for (int k = threadIdx.x; k < n; k += 256) {
+  for (int k = blockIdx.y * 1024 + threadIdx.x; k < min(n, (int)(blockIdx.y + 1) * 1024); k += 256) {
     if constexpr (!X8) {
       ((uint16_t*)out)[row * ldo + k] = ((const uint16_t*)x)[row * ldx + k];
     } else {
@@ -830,13 +830,14 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
   int64_t ldx = L.ldx;
   if (!rows_in_place(x, x8, ldx, bytes8)) {
     void* out = (char*)workspace + W.off_copy;
+    const dim3 grid((unsigned)L.rows, (unsigned)ceil_div(L.n, 1024));
     ldx = round_up(L.n, 16);
     if (!x8)
-      k_linear_rows<false, false><<<L.rows, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+      k_linear_rows<false, false><<<grid, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
     else if (bytes8)
-      k_linear_rows<true, true><<<L.rows, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+      k_linear_rows<true, true><<<grid, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
     else
-      k_linear_rows<true, false><<<L.rows, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+      k_linear_rows<true, false><<<grid, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
     BK_CUDA_OK(cudaGetLastError());
     x = out;
   }

@@ -24,41 +24,48 @@ struct NormParams {
   float* scales;
   int rows, d;
   int wbf16;
-  int vec;       // every row of x, res, h, y and w starts on 16 bytes (y: 8 for e4m3)
+  int vec;       // d % 8 is 0, and every row of x, res, h, y and w starts on 16 bytes (y: 8 for e4m3)
   float eps;
 };
 
-// Element (i, j) of a thread's VPT groups of 8: 8 neighbours where vectors can be used,
-// else one every `nt` elements, so that a warp's loads stay together.
-__device__ __forceinline__ int elem(bool vec, int i, int j, int t, int nt) {
-  return vec ? (t + i * nt) * 8 + j : (i * 8 + j) * nt + t;
+// Element (i, j) of a thread's VPT groups of 8: 8 neighbours where vectors can be used (VEC:
+// d is a multiple of 8 and every row starts on 16 bytes), else one every `nt` elements, so
+// that a warp's loads stay together.
+template <bool VEC>
+__device__ __forceinline__ int elem(int i, int j, int t, int nt) {
+  return VEC ? (t + i * nt) * 8 + j : (i * 8 + j) * nt + t;
 }
 
-template <typename T>
-__device__ __forceinline__ void row_load(const T* p, bool vec, int i, int t, int nt, int d, float (&v)[8]) {
-  const int e0 = elem(true, i, 0, t, nt);
-  if (vec && e0 + 8 <= d) {
-    load8(p + e0, v);
-    return;
-  }
+template <bool VEC, typename T>
+__device__ __forceinline__ void row_load(const T* p, int i, int t, int nt, int d, float (&v)[8]) {
+  if constexpr (VEC) {
+    const int e0 = elem<true>(i, 0, t, nt);
+    if (e0 < d) {
+      load8(p + e0, v);
+    } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int e = elem(vec, i, j, t, nt);
-    v[j] = e < d ? to_f32(p[e]) : 0.f;
+      for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int e = elem<false>(i, j, t, nt);
+      v[j] = e < d ? to_f32(p[e]) : 0.f;
+    }
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void row_store(T* p, bool vec, int i, int t, int nt, int d, const float (&v)[8]) {
-  const int e0 = elem(true, i, 0, t, nt);
-  if (vec && e0 + 8 <= d) {
-    store8(p + e0, v);
-    return;
-  }
+template <bool VEC, typename T>
+__device__ __forceinline__ void row_store(T* p, int i, int t, int nt, int d, const float (&v)[8]) {
+  if constexpr (VEC) {
+    const int e0 = elem<true>(i, 0, t, nt);
+    if (e0 < d) store8(p + e0, v);
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int e = elem(vec, i, j, t, nt);
-    if (e < d) p[e] = from_f32<T>(v[j]);
+    for (int j = 0; j < 8; ++j) {
+      const int e = elem<false>(i, j, t, nt);
+      if (e < d) p[e] = from_f32<T>(v[j]);
+    }
   }
 }
 
@@ -66,29 +73,80 @@ __device__ __forceinline__ uint8_t e4m3(float v) {
   return (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3);
 }
 
-__device__ __forceinline__ void row_store_e4m3(uint8_t* p, bool vec, int i, int t, int nt, int d,
-                                               const float (&v)[8]) {
-  const int e0 = elem(true, i, 0, t, nt);
-  if (vec && e0 + 8 <= d) {
+template <bool VEC>
+__device__ __forceinline__ void row_store_e4m3(uint8_t* p, int i, int t, int nt, int d, const float (&v)[8]) {
+  if constexpr (VEC) {
+    const int e0 = elem<true>(i, 0, t, nt);
+    if (e0 >= d) return;
     uint32_t q[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       q[j] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * j], v[2 * j + 1]), __NV_SATFINITE, __NV_E4M3);
     *reinterpret_cast<uint2*>(p + e0) = make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int e = elem(vec, i, j, t, nt);
-    if (e < d) p[e] = e4m3(v[j]);
+    for (int j = 0; j < 8; ++j) {
+      const int e = elem<false>(i, j, t, nt);
+      if (e < d) p[e] = e4m3(v[j]);
+    }
   }
 }
 
-__device__ __forceinline__ void load_w(const NormParams& P, int i, int t, int nt, float (&v)[8]) {
-  if (P.wbf16)
-    row_load((const __nv_bfloat16*)P.w, P.vec, i, t, nt, P.d, v);
+// 8 elements as they are stored.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    a = make_float4(v[0], v[1], v[2], v[3]);
+    b = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+};
+template <>
+struct Raw8<__nv_bfloat16> {
+  uint4 a;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    a = make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7]));
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = bf16_lo(a.x); v[1] = bf16_hi(a.x); v[2] = bf16_lo(a.y); v[3] = bf16_hi(a.y);
+    v[4] = bf16_lo(a.z); v[5] = bf16_hi(a.z); v[6] = bf16_lo(a.w); v[7] = bf16_hi(a.w);
+  }
+};
+
+template <bool VEC, typename T>
+__device__ __forceinline__ void raw_load(const T* p, int i, int t, int nt, int d, Raw8<T>& r) {
+  if (VEC && elem<true>(i, 0, t, nt) < d) {
+    r.load(p + elem<true>(i, 0, t, nt));
+  } else {
+    float v[8];
+    if constexpr (VEC) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    } else {
+      row_load<false>(p, i, t, nt, d, v);
+    }
+    r.set(v);
+  }
+}
+
+// The weight, fp32 or bf16.
+template <bool VEC>
+__device__ __forceinline__ void load_w(const void* w, int bf16, int i, int t, int nt, int d, float (&v)[8]) {
+  if (bf16)
+    row_load<VEC>((const __nv_bfloat16*)w, i, t, nt, d, v);
   else
-    row_load((const float*)P.w, P.vec, i, t, nt, P.d, v);
+    row_load<VEC>((const float*)w, i, t, nt, d, v);
 }
 
 // A row's scale, and its values over it: a product with the reciprocal, or a quotient
@@ -105,55 +163,74 @@ struct RowScale {
   __device__ __forceinline__ float operator()(float y) const { return small ? y / s : y * inv; }
 };
 
-// One row per CTA, VPT groups of 8 elements per thread in registers.
-template <typename T, bool E4M3, int VPT>
-__global__ void __launch_bounds__(1024) k_rmsnorm(const NormParams P) {
-  __shared__ float slots[2][32];
+// VPT groups of 8 elements of a row per thread in registers.  Bound by memory: what counts is
+// that loads stay in flight.  Long rows (AHEAD): a CTA takes the rows blockIdx.x,
+// + gridDim.x, ..., with the next one on its way while this one is summed and written
+// (16381 x 8192 bf16 with a residual 178 us, 6.0 TB/s; a row per CTA 197).  Shorter ones: a row
+// per CTA, with fewer registers and more CTAs at once (16384 x 1000 bf16 28 us, ahead 45).
+template <typename T, bool E4M3, int VPT, bool AHEAD, bool VEC>
+__global__ void __launch_bounds__(AHEAD || VPT > 1 ? 512 : 1024, AHEAD && VPT * sizeof(T) <= 4 ? 2 : 1)
+    k_rmsnorm(const NormParams P) {
+  __shared__ float slots[2][2][32];
   const int t = threadIdx.x, nt = blockDim.x;
-  const int64_t row = blockIdx.x;
-  const T* x = (const T*)P.x + row * P.ldx;
-  const T* res = P.res ? (const T*)P.res + row * P.ldr : nullptr;
-  float h[VPT][8];
-  float ss = 0.f;
+  struct Row {
+    Raw8<T> x[VPT], r[VPT];
+  };
+  auto load_row = [&](int64_t row, Row& o) {
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    row_load(x, P.vec, i, t, nt, P.d, h[i]);
-    if (res) {
-      float r[8];
-      row_load(res, P.vec, i, t, nt, P.d, r);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[i][j] += r[j];
+    for (int i = 0; i < VPT; ++i) {
+      raw_load<VEC>((const T*)P.x + row * P.ldx, i, t, nt, P.d, o.x[i]);
+      if (P.res) raw_load<VEC>((const T*)P.res + row * P.ldr, i, t, nt, P.d, o.r[i]);
     }
+  };
+  Row next;
+  if (blockIdx.x < P.rows) load_row(blockIdx.x, next);
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x, turn ^= 1) {
+    float h[VPT][8];
+    float ss = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fmaf(h[i][j], h[i][j], ss);
-  }
-  if (P.h) {
+    for (int i = 0; i < VPT; ++i) {
+      next.x[i].get(h[i]);
+      if (P.res) {
+        float r[8];
+        next.r[i].get(r);
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) row_store((T*)P.h + row * P.ldh, P.vec, i, t, nt, P.d, h[i]);
-  }
-  ss = cta_all(ss, AddOp(), slots[0]);
-  const float rho = 1.f / sqrtf(ss / (float)P.d + P.eps);
-  float amax = 0.f;
-#pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    float w[8];
-    load_w(P, i, t, nt, w);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      h[i][j] = h[i][j] * rho * w[j];
-      if (E4M3) amax = max_nan(amax, fabsf(h[i][j]));
+        for (int j = 0; j < 8; ++j) h[i][j] += r[j];
+      }
     }
-    if (!E4M3) row_store((T*)P.y + row * P.ldy, P.vec, i, t, nt, P.d, h[i]);
-  }
-  if constexpr (E4M3) {
-    const RowScale sc(cta_all(amax, MaxNanOp(), slots[1]));
-    if (t == 0) P.scales[row] = sc.s;
+    if (AHEAD && row + gridDim.x < P.rows) load_row(row + gridDim.x, next);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[i][j] = sc(h[i][j]);
-      row_store_e4m3((uint8_t*)P.y + row * P.ldy, P.vec, i, t, nt, P.d, h[i]);
+      for (int j = 0; j < 8; ++j) ss = fmaf(h[i][j], h[i][j], ss);
+      if (P.h) row_store<VEC>((T*)P.h + row * P.ldh, i, t, nt, P.d, h[i]);
     }
+    ss = cta_all(ss, AddOp(), slots[turn][0]);
+    const float rho = 1.f / sqrtf(ss / (float)P.d + P.eps);
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float w[8];
+      load_w<VEC>(P.w, P.wbf16, i, t, nt, P.d, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[i][j] = h[i][j] * rho * w[j];
+        if (E4M3) amax = max_nan(amax, fabsf(h[i][j]));
+      }
+      if (!E4M3) row_store<VEC>((T*)P.y + row * P.ldy, i, t, nt, P.d, h[i]);
+    }
+    if constexpr (E4M3) {
+      const RowScale sc(cta_all(amax, MaxNanOp(), slots[turn][1]));
+      if (t == 0) P.scales[row] = sc.s;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[i][j] = sc(h[i][j]);
+        row_store_e4m3<VEC>((uint8_t*)P.y + row * P.ldy, i, t, nt, P.d, h[i]);
+      }
+    }
+    if (!AHEAD) break;
   }
 }
 
@@ -200,10 +277,96 @@ struct NormBackParams {
   void* dx;
   float *rho, *part;   // [rows]; [parts][d]
   int rows, d, wbf16, parts;
+  int vec;             // as for the norm
   float eps;
 };
 
-// dx of a row, and its rho for the weight's gradient.
+// A CTA takes the rows blockIdx.x, + gridDim.x, ...: each is read once and held as it is
+// stored while its two sums are formed; the weight's gradient stays in registers from row
+// to row and leaves as one part per CTA.  Four groups of 8 a thread: what a row costs beside
+// its elements (two sums over the CTA, addresses, rho) is shared by 32 of them (with 8 a
+// thread the kernel was bound by instructions, 45 an element).
+constexpr int BACK_VPT = 4;
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(512) k_rmsnorm_back(const NormBackParams P) {
+  constexpr int VPT = BACK_VPT;
+  constexpr bool HOLD = sizeof(T) == 2;      // dsum too
+  __shared__ float2 slots[2][16];
+  const int t = threadIdx.x, nt = blockDim.x, warp = t >> 5, lane = t & 31, warps = nt >> 5;
+  float dw[VPT][8] = {};
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x, turn ^= 1) {
+    Raw8<T> h[VPT], dy[VPT], ds[HOLD ? VPT : 1];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      raw_load<VEC>((const T*)P.h + row * P.ldh, i, t, nt, P.d, h[i]);
+      raw_load<VEC>((const T*)P.dy + row * P.lddy, i, t, nt, P.d, dy[i]);
+      if (HOLD && P.dsum) raw_load<VEC>((const T*)P.dsum + row * P.ldds, i, t, nt, P.d, ds[HOLD ? i : 0]);
+    }
+    float ss = 0.f, c = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float a[8], b[8], w[8];
+      h[i].get(a);
+      dy[i].get(b);
+      load_w<VEC>(P.w, P.wbf16, i, t, nt, P.d, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        ss = fmaf(a[j], a[j], ss);
+        c = fmaf(w[j] * b[j], a[j], c);
+      }
+    }
+    // both sums in one butterfly: the lower half warp goes on with ss, the upper with c
+    const bool up = lane & 16;
+    float v = (up ? c : ss) + __shfl_xor_sync(0xffffffffu, up ? ss : c, 16);
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((lane & 15) == 0) (up ? slots[turn][warp].y : slots[turn][warp].x) = v;
+    if (warps > 1)
+      __syncthreads();      // (the other turn's slots were read before this)
+    else
+      __syncwarp();
+    ss = c = 0.f;
+    for (int w = 0; w < warps; ++w) {
+      const float2 s = slots[turn][w];
+      ss += s.x;
+      c += s.y;
+    }
+    const float rho = rsqrtf(ss / (float)P.d + P.eps), k = rho * rho * (c / (float)P.d);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float a[8], b[8], w[8], o[8];
+      h[i].get(a);
+      dy[i].get(b);
+      load_w<VEC>(P.w, P.wbf16, i, t, nt, P.d, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dw[i][j] = fmaf(b[j] * a[j], rho, dw[i][j]);
+        o[j] = rho * (w[j] * b[j] - a[j] * k);
+      }
+      if (P.dsum) {
+        if (HOLD)
+          ds[HOLD ? i : 0].get(a);
+        else
+          row_load<VEC>((const T*)P.dsum + row * P.ldds, i, t, nt, P.d, a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] += a[j];
+      }
+      row_store<VEC>((T*)P.dx + row * P.lddx, i, t, nt, P.d, o);
+    }
+  }
+  float* part = P.part + (int64_t)blockIdx.x * P.d;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int e = elem<VEC>(i, j, t, nt);
+      if (e < P.d) part[e] = dw[i][j];
+    }
+}
+
+// Rows too long for that: dx of a row, and its rho for the weight's gradient.
 template <typename T>
 __global__ void __launch_bounds__(256) k_rmsnorm_dx(const NormBackParams P) {
   __shared__ float slots[2][32];
@@ -259,21 +422,52 @@ __global__ void __launch_bounds__(1024) k_sum_parts(const float* part, int parts
   }
 }
 
-// Rows share their parts of dw among this many CTAs.
-int back_parts(int rows) { return std::min(rows, 4 * ROW_SMS); }
+// Threads of a CTA (0: rows too long), and CTAs, each with its part of dw: 16 warps an SM.
+int back_threads(int d) {
+  const int nt = (int)round_up(ceil_div(ceil_div(d, 8), BACK_VPT), 32);
+  return nt <= 512 ? nt : 0;
+}
+int back_parts(int rows, int d) {
+  const int nt = back_threads(d);
+  return std::min(rows, ROW_SMS * (nt ? std::max(1, 512 / nt) : 4));
+}
 
-template <typename T, bool E4M3>
+template <typename T>
+void back_launch(const NormBackParams& P, cudaStream_t s) {
+  if (const int nt = back_threads(P.d)) {
+    P.vec ? k_rmsnorm_back<T, true><<<P.parts, nt, 0, s>>>(P) : k_rmsnorm_back<T, false><<<P.parts, nt, 0, s>>>(P);
+  } else {
+    k_rmsnorm_dx<T><<<P.rows, 256, 0, s>>>(P);
+    k_rmsnorm_dw<T><<<dim3((unsigned)ceil_div(P.d, 256), (unsigned)P.parts), 256, 0, s>>>(P);
+  }
+}
+
+template <typename T, bool E4M3, bool VEC>
 int norm_launch(const NormParams& P, cudaStream_t s) {
   const int groups = ceil_div(P.d, 8);
-  if (groups > 2 * 1024) {
+  const bool many = P.rows > 2 * ROW_SMS;
+  if (groups > 2048) {
     k_rmsnorm_long<T, E4M3><<<P.rows, 1024, 0, s>>>(P);
-  } else if (groups <= 1024) {
-    k_rmsnorm<T, E4M3, 1><<<P.rows, (unsigned)round_up(groups, 32), 0, s>>>(P);
+  } else if (groups > 1024 || (many && groups > 512)) {
+    const int vpt = groups > 1024 ? 4 : 2, nt = (int)round_up(ceil_div(groups, vpt), 32);
+    const int ctas = std::min(P.rows, ROW_SMS * ((vpt * (int)sizeof(T) <= 4 ? 1024 : 512) / nt));
+    if (vpt == 4)
+      k_rmsnorm<T, E4M3, 4, true, VEC><<<ctas, nt, 0, s>>>(P);
+    else
+      k_rmsnorm<T, E4M3, 2, true, VEC><<<ctas, nt, 0, s>>>(P);
+  } else if (many && groups > 256) {
+    k_rmsnorm<T, E4M3, 2, false, VEC><<<P.rows, (unsigned)round_up(ceil_div(groups, 2), 32), 0, s>>>(P);
   } else {
-    k_rmsnorm<T, E4M3, 2><<<P.rows, (unsigned)round_up(ceil_div(groups, 2), 32), 0, s>>>(P);
+    k_rmsnorm<T, E4M3, 1, false, VEC><<<P.rows, (unsigned)round_up(groups, 32), 0, s>>>(P);
   }
   BK_CUDA_OK(cudaGetLastError());
   return BAKRON_OK;
+}
+
+template <typename T>
+int norm_kinds(const NormParams& P, bool q, cudaStream_t s) {
+  if (q) return P.vec ? norm_launch<T, true, true>(P, s) : norm_launch<T, true, false>(P, s);
+  return P.vec ? norm_launch<T, false, true>(P, s) : norm_launch<T, false, false>(P, s);
 }
 
 bool float_dtype(int t) { return t == BAKRON_F32 || t == BAKRON_BF16; }
@@ -300,17 +494,16 @@ extern "C" int bakron_rmsnorm(const void* x, int dtype, int rows, int d, int64_t
   P.x = x; P.res = residual; P.w = weight; P.h = sum; P.y = y; P.scales = scales;
   P.ldx = ldx; P.ldr = ldr; P.ldh = lds; P.ldy = ldy;
   P.rows = rows; P.d = d; P.wbf16 = wdtype == BAKRON_BF16; P.eps = eps;
-  P.vec = aligned16(x, ldx * es) && (!residual || aligned16(residual, ldr * es)) &&
+  P.vec = d % 8 == 0 && aligned16(x, ldx * es) && (!residual || aligned16(residual, ldr * es)) &&
           (!sum || aligned16(sum, lds * es)) && aligned16(weight, 0) &&
           (q ? ((uintptr_t)y | (uintptr_t)ldy) % 8 == 0 : aligned16(y, ldy * es));
   cudaStream_t s = (cudaStream_t)stream;
-  if (dtype == BAKRON_F32) return q ? norm_launch<float, true>(P, s) : norm_launch<float, false>(P, s);
-  return q ? norm_launch<__nv_bfloat16, true>(P, s) : norm_launch<__nv_bfloat16, false>(P, s);
+  return dtype == BAKRON_F32 ? norm_kinds<float>(P, q, s) : norm_kinds<__nv_bfloat16>(P, q, s);
 }
 
 extern "C" size_t bakron_rmsnorm_backward_workspace_bytes(int rows, int d) {
   if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
-  return align256((size_t)rows * 4) + (size_t)back_parts(rows) * d * 4 + 256;
+  return align256((size_t)rows * 4) + (size_t)back_parts(rows, d) * d * 4 + 256;
 }
 
 extern "C" int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh,
@@ -328,18 +521,17 @@ extern "C" int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void*
   NormBackParams P{};
   P.dy = dy; P.h = h; P.w = weight; P.dsum = dsum; P.dx = dx;
   P.lddy = lddy; P.ldh = ldh; P.ldds = ldds; P.lddx = lddx;
-  P.rows = rows; P.d = d; P.wbf16 = wdtype == BAKRON_BF16; P.parts = back_parts(rows); P.eps = eps;
+  P.rows = rows; P.d = d; P.wbf16 = wdtype == BAKRON_BF16; P.parts = back_parts(rows, d); P.eps = eps;
   P.rho = (float*)workspace;
   P.part = (float*)((char*)workspace + align256((size_t)rows * 4));
   if (rows > 0) {
-    const dim3 gw((unsigned)ceil_div(d, 256), (unsigned)P.parts);
-    if (dtype == BAKRON_F32) {
-      k_rmsnorm_dx<float><<<rows, 256, 0, s>>>(P);
-      k_rmsnorm_dw<float><<<gw, 256, 0, s>>>(P);
-    } else {
-      k_rmsnorm_dx<__nv_bfloat16><<<rows, 256, 0, s>>>(P);
-      k_rmsnorm_dw<__nv_bfloat16><<<gw, 256, 0, s>>>(P);
-    }
+    const int es = dtype == BAKRON_F32 ? 4 : 2;
+    P.vec = d % 8 == 0 && aligned16(dy, lddy * es) && aligned16(h, ldh * es) && (!dsum || aligned16(dsum, ldds * es)) &&
+            aligned16(dx, lddx * es) && aligned16(weight, 0);
+    if (dtype == BAKRON_F32)
+      back_launch<float>(P, s);
+    else
+      back_launch<__nv_bfloat16>(P, s);
     BK_CUDA_OK(cudaGetLastError());
   }
   k_sum_parts<<<(unsigned)ceil_div(d, 32), dim3(32, 32), 0, s>>>(P.part, P.parts, d, dw);
