@@ -127,16 +127,6 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<uint32_t*>(&r);
 }
 
-// 16 bytes of global memory to shared memory, without a register: in flight until the
-// lane's copies_left() allows no more than that many later groups.
-__device__ __forceinline__ void copy16(uint4* to, const uint4* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from)
-               : "memory");
-}
-__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_left() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // A lane's 32 elements of a tile, as loaded: U vectors, 32 apart.
 template <typename T>
 struct Tile {

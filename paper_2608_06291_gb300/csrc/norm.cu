@@ -281,35 +281,76 @@ struct NormBackParams {
   float eps;
 };
 
-// A CTA takes the rows blockIdx.x, + gridDim.x, ...: each is read once and held as it is
-// stored while its two sums are formed; the weight's gradient stays in registers from row
-// to row and leaves as one part per CTA.  Four groups of 8 a thread: what a row costs beside
-// its elements (two sums over the CTA, addresses, rho) is shared by 32 of them (with 8 a
-// thread the kernel was bound by instructions, 45 an element).
+// A CTA takes the rows blockIdx.x, + gridDim.x, ...: each is read once while its two sums are
+// formed and used again for dx; the weight's gradient stays in registers from row to row
+// and leaves as one part per CTA.  Four groups of 8 a thread: what a row costs beside its
+// elements (two sums over the CTA, addresses, rho) is shared by 32 of them (with 8 a
+// thread the kernel was bound by instructions).  Rows that vectors can be used for wait in a
+// ring of RING rows in shared memory, copied there without registers, so that loads stay
+// in flight (RING 0: held in registers, 8192 x 4096 in bf16 69 us).
 constexpr int BACK_VPT = 4;
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, int RING>
 __global__ void __launch_bounds__(512) k_rmsnorm_back(const NormBackParams P) {
   constexpr int VPT = BACK_VPT;
-  constexpr bool HOLD = sizeof(T) == 2;      // dsum too
+  constexpr bool HOLD = sizeof(T) == 2 && RING == 0;      // dsum too
+  static_assert(VEC || RING == 0, "whole vectors");
   __shared__ float2 slots[2][16];
+  extern __shared__ __align__(16) unsigned char nb_ring[];   // [RING][h, dy, dsum][d]
   const int t = threadIdx.x, nt = blockDim.x, warp = t >> 5, lane = t & 31, warps = nt >> 5;
   float dw[VPT][8] = {};
-  int turn = 0;
-  for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x, turn ^= 1) {
-    Raw8<T> h[VPT], dy[VPT], ds[HOLD ? VPT : 1];
+  int turn = 0, slot = 0;
+  T* ring = reinterpret_cast<T*>(nb_ring);
+  auto fetch = [&](int64_t row, int to) {      // each thread its own groups
+    if (row < P.rows) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      raw_load<VEC>((const T*)P.h + row * P.ldh, i, t, nt, P.d, h[i]);
-      raw_load<VEC>((const T*)P.dy + row * P.lddy, i, t, nt, P.d, dy[i]);
-      if (HOLD && P.dsum) raw_load<VEC>((const T*)P.dsum + row * P.ldds, i, t, nt, P.d, ds[HOLD ? i : 0]);
+      for (int i = 0; i < VPT; ++i) {
+        const int e0 = elem<true>(i, 0, t, nt);
+        if (e0 >= P.d) continue;
+        T* at = ring + (int64_t)to * 3 * P.d + e0;
+#pragma unroll
+        for (int k = 0; k < 8; k += 16 / (int)sizeof(T)) {
+          copy16(at + k, (const T*)P.h + row * P.ldh + e0 + k);
+          copy16(at + P.d + k, (const T*)P.dy + row * P.lddy + e0 + k);
+          if (P.dsum) copy16(at + 2 * P.d + k, (const T*)P.dsum + row * P.ldds + e0 + k);
+        }
+      }
     }
+    copies_group();
+  };
+  if constexpr (RING > 0) {
+#pragma unroll
+    for (int s = 0; s < RING - 1; ++s) fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+  }
+  for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x, turn ^= 1) {
+    Raw8<T> h[RING ? 1 : VPT], dy[RING ? 1 : VPT], ds[HOLD ? VPT : 1];
+    const T* here = ring + (int64_t)slot * 3 * P.d;
+    if constexpr (RING > 0) {
+      copies_left<(RING > 1 ? RING - 2 : 0)>();
+      fetch(row + (int64_t)(RING - 1) * gridDim.x, slot == 0 ? RING - 1 : slot - 1);
+      slot = slot == RING - 1 ? 0 : slot + 1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        raw_load<VEC>((const T*)P.h + row * P.ldh, i, t, nt, P.d, h[i]);
+        raw_load<VEC>((const T*)P.dy + row * P.lddy, i, t, nt, P.d, dy[i]);
+        if (HOLD && P.dsum) raw_load<VEC>((const T*)P.dsum + row * P.ldds, i, t, nt, P.d, ds[HOLD ? i : 0]);
+      }
+    }
+    auto get = [&](int i, float (&a)[8], float (&b)[8]) {
+      if constexpr (RING > 0) {
+        row_load<true>(here, i, t, nt, P.d, a);
+        row_load<true>(here + P.d, i, t, nt, P.d, b);
+      } else {
+        h[i].get(a);
+        dy[i].get(b);
+      }
+    };
     float ss = 0.f, c = 0.f;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       float a[8], b[8], w[8];
-      h[i].get(a);
-      dy[i].get(b);
+      get(i, a, b);
       load_w<VEC>(P.w, P.wbf16, i, t, nt, P.d, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -337,8 +378,7 @@ __global__ void __launch_bounds__(512) k_rmsnorm_back(const NormBackParams P) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       float a[8], b[8], w[8], o[8];
-      h[i].get(a);
-      dy[i].get(b);
+      get(i, a, b);
       load_w<VEC>(P.w, P.wbf16, i, t, nt, P.d, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -348,6 +388,8 @@ __global__ void __launch_bounds__(512) k_rmsnorm_back(const NormBackParams P) {
       if (P.dsum) {
         if (HOLD)
           ds[HOLD ? i : 0].get(a);
+        else if (RING > 0)
+          row_load<true>(here + 2 * P.d, i, t, nt, P.d, a);
         else
           row_load<VEC>((const T*)P.dsum + row * P.ldds, i, t, nt, P.d, a);
 #pragma unroll
@@ -422,24 +464,46 @@ __global__ void __launch_bounds__(1024) k_sum_parts(const float* part, int parts
   }
 }
 
-// Threads of a CTA (0: rows too long), and CTAs, each with its part of dw: 16 warps an SM.
+// Threads of a CTA (0: rows too long), and CTAs, each with its part of dw: what an SM holds.
+constexpr int NB_SMEM = 220 * 1024;      // of an SM's, beside each CTA's kilobyte
 int back_threads(int d) {
   const int nt = (int)round_up(ceil_div(ceil_div(d, 8), BACK_VPT), 32);
   return nt <= 512 ? nt : 0;
 }
-int back_parts(int rows, int d) {
-  const int nt = back_threads(d);
-  return std::min(rows, ROW_SMS * (nt ? std::max(1, 512 / nt) : 4));
+struct BackPlan {
+  int ring, ctas;      // rows of the ring, CTAs of an SM
+  BackPlan(int d, int es, bool vec) {
+    const int nt = back_threads(d), row = 3 * d * es;
+    ring = !nt || !vec || 2 * row > NB_SMEM ? 0 : 2 * 3 * row > NB_SMEM ? 2 : 3;
+    ctas = nt ? std::max(1, 512 / nt) : 4;
+    if (ring) ctas = std::min(640 / nt, NB_SMEM / (ring * row + 1024));
+  }
+};
+int back_parts(int rows, int d, int es, bool vec) {
+  return std::min(rows, ROW_SMS * BackPlan(d, es, vec).ctas);
 }
 
 template <typename T>
-void back_launch(const NormBackParams& P, cudaStream_t s) {
-  if (const int nt = back_threads(P.d)) {
-    P.vec ? k_rmsnorm_back<T, true><<<P.parts, nt, 0, s>>>(P) : k_rmsnorm_back<T, false><<<P.parts, nt, 0, s>>>(P);
-  } else {
+cudaError_t back_launch(const NormBackParams& P, cudaStream_t s) {
+  const int nt = back_threads(P.d), ring = BackPlan(P.d, sizeof(T), P.vec).ring;
+  if (!nt) {
     k_rmsnorm_dx<T><<<P.rows, 256, 0, s>>>(P);
     k_rmsnorm_dw<T><<<dim3((unsigned)ceil_div(P.d, 256), (unsigned)P.parts), 256, 0, s>>>(P);
+    return cudaGetLastError();
   }
+  static OncePerDevice once;
+  const cudaError_t e = once([] {
+    const cudaError_t a = cudaFuncSetAttribute(k_rmsnorm_back<T, true, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, NB_SMEM);
+    return a != cudaSuccess
+               ? a
+               : cudaFuncSetAttribute(k_rmsnorm_back<T, true, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize, NB_SMEM);
+  });
+  if (e != cudaSuccess) return e;
+  const size_t smem = (size_t)ring * 3 * P.d * sizeof(T);
+  const auto kernel = ring == 3 ? k_rmsnorm_back<T, true, 3> : ring == 2 ? k_rmsnorm_back<T, true, 2>
+                      : P.vec   ? k_rmsnorm_back<T, true, 0> : k_rmsnorm_back<T, false, 0>;
+  kernel<<<P.parts, nt, smem, s>>>(P);
+  return cudaGetLastError();
 }
 
 template <typename T, bool E4M3, bool VEC>
@@ -503,7 +567,10 @@ extern "C" int bakron_rmsnorm(const void* x, int dtype, int rows, int d, int64_t
 
 extern "C" size_t bakron_rmsnorm_backward_workspace_bytes(int rows, int d) {
   if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
-  return align256((size_t)rows * 4) + (size_t)back_parts(rows, d) * d * 4 + 256;
+  int parts = 0;      // whichever way the call goes
+  for (int es : {2, 4})
+    for (bool vec : {false, true}) parts = std::max(parts, back_parts(rows, d, es, vec));
+  return align256((size_t)rows * 4) + (size_t)parts * d * 4 + 256;
 }
 
 extern "C" int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh,
@@ -521,18 +588,15 @@ extern "C" int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void*
   NormBackParams P{};
   P.dy = dy; P.h = h; P.w = weight; P.dsum = dsum; P.dx = dx;
   P.lddy = lddy; P.ldh = ldh; P.ldds = ldds; P.lddx = lddx;
-  P.rows = rows; P.d = d; P.wbf16 = wdtype == BAKRON_BF16; P.parts = back_parts(rows, d); P.eps = eps;
+  P.rows = rows; P.d = d; P.wbf16 = wdtype == BAKRON_BF16; P.eps = eps;
   P.rho = (float*)workspace;
   P.part = (float*)((char*)workspace + align256((size_t)rows * 4));
   if (rows > 0) {
     const int es = dtype == BAKRON_F32 ? 4 : 2;
     P.vec = d % 8 == 0 && aligned16(dy, lddy * es) && aligned16(h, ldh * es) && (!dsum || aligned16(dsum, ldds * es)) &&
             aligned16(dx, lddx * es) && aligned16(weight, 0);
-    if (dtype == BAKRON_F32)
-      back_launch<float>(P, s);
-    else
-      back_launch<__nv_bfloat16>(P, s);
-    BK_CUDA_OK(cudaGetLastError());
+    P.parts = back_parts(rows, d, es, P.vec);
+    BK_CUDA_OK(dtype == BAKRON_F32 ? back_launch<float>(P, s) : back_launch<__nv_bfloat16>(P, s));
   }
   k_sum_parts<<<(unsigned)ceil_div(d, 32), dim3(32, 32), 0, s>>>(P.part, P.parts, d, dw);
   BK_CUDA_OK(cudaGetLastError());

@@ -87,6 +87,16 @@ __device__ __forceinline__ float cta_all(float v, Op op, float* slots) {
   return warp_all(lane < warps ? slots[lane] : Op::none, op);
 }
 
+// 16 bytes of global memory to shared memory, without a register: in flight until the
+// lane's copies_left() allows no more than that many later groups.
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from)
+               : "memory");
+}
+__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_left() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 inline bool aligned16(const void* p, int64_t row_bytes) {
   return ((uintptr_t)p | (uintptr_t)row_bytes) % 16 == 0;
 }
