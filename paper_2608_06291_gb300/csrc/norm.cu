@@ -290,14 +290,27 @@ struct NormBackParams {
 // in flight (RING 0: held in registers, 8192 x 4096 in bf16 69 us).
 constexpr int BACK_VPT = 4;
 
-template <typename T, bool VEC, int RING>
-__global__ void __launch_bounds__(512) k_rmsnorm_back(const NormBackParams P) {
+template <typename T, typename W, bool VEC, int RING, int MAXT>
+__global__ void __launch_bounds__(MAXT) k_rmsnorm_back(const NormBackParams P) {
   constexpr int VPT = BACK_VPT;
   constexpr bool HOLD = sizeof(T) == 2 && RING == 0;      // dsum too
+  // The rings leave little of the SM's memory to its cache: the weight stays in registers.
+  constexpr bool KEEP_W = RING > 0 && MAXT == 256;
   static_assert(VEC || RING == 0, "whole vectors");
   __shared__ float2 slots[2][16];
   extern __shared__ __align__(16) unsigned char nb_ring[];   // [RING][h, dy, dsum][d]
   const int t = threadIdx.x, nt = blockDim.x, warp = t >> 5, lane = t & 31, warps = nt >> 5;
+  Raw8<W> weight[KEEP_W ? VPT : 1];
+  if constexpr (KEEP_W) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) raw_load<VEC>((const W*)P.w, i, t, nt, P.d, weight[i]);
+  }
+  auto get_w = [&](int i, float (&w)[8]) {
+    if constexpr (KEEP_W)
+      weight[i].get(w);
+    else
+      row_load<VEC>((const W*)P.w, i, t, nt, P.d, w);
+  };
   float dw[VPT][8] = {};
   int turn = 0, slot = 0;
   T* ring = reinterpret_cast<T*>(nb_ring);
@@ -351,7 +364,7 @@ __global__ void __launch_bounds__(512) k_rmsnorm_back(const NormBackParams P) {
     for (int i = 0; i < VPT; ++i) {
       float a[8], b[8], w[8];
       get(i, a, b);
-      load_w<VEC>(P.w, P.wbf16, i, t, nt, P.d, w);
+      get_w(i, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         ss = fmaf(a[j], a[j], ss);
@@ -379,11 +392,11 @@ __global__ void __launch_bounds__(512) k_rmsnorm_back(const NormBackParams P) {
     for (int i = 0; i < VPT; ++i) {
       float a[8], b[8], w[8], o[8];
       get(i, a, b);
-      load_w<VEC>(P.w, P.wbf16, i, t, nt, P.d, w);
+      get_w(i, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         dw[i][j] = fmaf(b[j] * a[j], rho, dw[i][j]);
-        o[j] = rho * (w[j] * b[j] - a[j] * k);
+        o[j] = fmaf(rho, w[j] * b[j], -(rho * k) * a[j]);
       }
       if (P.dsum) {
         if (HOLD)
@@ -474,7 +487,7 @@ struct BackPlan {
   int ring, ctas;      // rows of the ring, CTAs of an SM
   BackPlan(int d, int es, bool vec) {
     const int nt = back_threads(d), row = 3 * d * es;
-    ring = !nt || !vec || 2 * row > NB_SMEM ? 0 : 2 * 3 * row > NB_SMEM ? 2 : 3;
+    ring = !nt || !vec || 2 * row > NB_SMEM ? 0 : nt > 256 || 2 * 3 * row > NB_SMEM ? 2 : 3;
     ctas = nt ? std::max(1, 512 / nt) : 4;
     if (ring) ctas = std::min(640 / nt, NB_SMEM / (ring * row + 1024));
   }
@@ -483,7 +496,12 @@ int back_parts(int rows, int d, int es, bool vec) {
   return std::min(rows, ROW_SMS * BackPlan(d, es, vec).ctas);
 }
 
-template <typename T>
+template <typename K>
+cudaError_t back_attr(K kernel) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NB_SMEM);
+}
+
+template <typename T, typename W>
 cudaError_t back_launch(const NormBackParams& P, cudaStream_t s) {
   const int nt = back_threads(P.d), ring = BackPlan(P.d, sizeof(T), P.vec).ring;
   if (!nt) {
@@ -493,16 +511,16 @@ cudaError_t back_launch(const NormBackParams& P, cudaStream_t s) {
   }
   static OncePerDevice once;
   const cudaError_t e = once([] {
-    const cudaError_t a = cudaFuncSetAttribute(k_rmsnorm_back<T, true, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, NB_SMEM);
-    return a != cudaSuccess
-               ? a
-               : cudaFuncSetAttribute(k_rmsnorm_back<T, true, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize, NB_SMEM);
+    cudaError_t a = back_attr(k_rmsnorm_back<T, W, true, 2, 256>);
+    if (a == cudaSuccess) a = back_attr(k_rmsnorm_back<T, W, true, 3, 256>);
+    if (a == cudaSuccess) a = back_attr(k_rmsnorm_back<T, W, true, 2, 512>);
+    return a;
   });
   if (e != cudaSuccess) return e;
-  const size_t smem = (size_t)ring * 3 * P.d * sizeof(T);
-  const auto kernel = ring == 3 ? k_rmsnorm_back<T, true, 3> : ring == 2 ? k_rmsnorm_back<T, true, 2>
-                      : P.vec   ? k_rmsnorm_back<T, true, 0> : k_rmsnorm_back<T, false, 0>;
-  kernel<<<P.parts, nt, smem, s>>>(P);
+  const auto kernel = ring == 0  ? (P.vec ? k_rmsnorm_back<T, W, true, 0, 512> : k_rmsnorm_back<T, W, false, 0, 512>)
+                      : nt > 256 ? k_rmsnorm_back<T, W, true, 2, 512>
+                      : ring == 2 ? k_rmsnorm_back<T, W, true, 2, 256> : k_rmsnorm_back<T, W, true, 3, 256>;
+  kernel<<<P.parts, nt, (size_t)ring * 3 * P.d * sizeof(T), s>>>(P);
   return cudaGetLastError();
 }
 
@@ -596,7 +614,10 @@ extern "C" int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void*
     P.vec = d % 8 == 0 && aligned16(dy, lddy * es) && aligned16(h, ldh * es) && (!dsum || aligned16(dsum, ldds * es)) &&
             aligned16(dx, lddx * es) && aligned16(weight, 0);
     P.parts = back_parts(rows, d, es, P.vec);
-    BK_CUDA_OK(dtype == BAKRON_F32 ? back_launch<float>(P, s) : back_launch<__nv_bfloat16>(P, s));
+    const auto launch = dtype == BAKRON_F32 ? (P.wbf16 ? back_launch<float, __nv_bfloat16> : back_launch<float, float>)
+                                            : (P.wbf16 ? back_launch<__nv_bfloat16, __nv_bfloat16>
+                                                       : back_launch<__nv_bfloat16, float>);
+    BK_CUDA_OK(launch(P, s));
   }
   k_sum_parts<<<(unsigned)ceil_div(d, 32), dim3(32, 32), 0, s>>>(P.part, P.parts, d, dw);
   BK_CUDA_OK(cudaGetLastError());
