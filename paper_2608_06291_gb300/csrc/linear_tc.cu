@@ -15,8 +15,7 @@
 // registers while the next one is formed.
 //
 // Roles: warp 0 loads tokens, warp 2 codes, warp 3 what a grid needs, warp 1 issues the MMAs, warps 4-7 and 8-11
-// expand (every other stage each), warps 12-19 (two per lane quarter of TMEM) sum and write
-// out.  CTAs are persistent, or, where there are fewer tiles than SMs, up to 8 CTAs of a
+// expand (half of a stage each), warps 12-19 (two per lane quarter of TMEM) sum and write out.  CTAs are persistent, or, where there are fewer tiles than SMs, up to 8 CTAs of a
 // cluster share a tile's columns and add their parts through each other's shared memory,
 // always in the same order.
 #include <cooperative_groups.h>
@@ -33,13 +32,11 @@ namespace cg = cooperative_groups;
 namespace bakron {
 namespace {
 
-constexpr int TC_THREADS = 640;
 constexpr int SEG_MMAS = 64;             // MMAs of a segment where a row has one grid: 1024 (2048) columns
 constexpr int TOKEN_GROUP = 16;          // token tiles that share a pass over the weight
 
 // The way out: an epilogue warp's 32 rows of 8 tokens at a time, token by token.
 constexpr int STAGE_LD = 36;             // floats of a token: 16-byte reads of 8 lanes meet no bank twice
-constexpr uint32_t STAGE_BYTES = 8 * 8 * STAGE_LD * 4;
 
 // A stage is 256 bytes of a token (two boxes of 128): 128 bf16 columns or 256 e4m3 columns,
 // eight MMAs.  What an iteration of the issuing warp costs beside its MMAs (barriers,
@@ -49,6 +46,9 @@ template <int BN_, bool W8_, bool X8_>
 struct TcShape {
   static constexpr int BN = BN_;
   static constexpr bool W8 = W8_, X8 = X8_;
+  static constexpr int EW = 2;                           // warpgroups that sum
+  static constexpr int THREADS = 128 * (3 + EW);
+  static constexpr int LAUNCH_REGS = 96;                 // of a thread: 65536 / THREADS, in steps of 8
   static constexpr int NACC = 2;                         // accumulators of BN columns
   static constexpr int NA = BN > 128 ? 2 : 4;            // A stages, 64 TMEM columns each
   static constexpr int ACC_COLS = NACC * BN;
@@ -58,14 +58,15 @@ struct TcShape {
   static constexpr uint32_t WS = W8 ? 16384 : 8192;      // bytes of a block's codes
   static constexpr int NX = BN > 128 ? 3 : 4;
   static constexpr int NW = W8 ? (BN > 64 ? 4 : 6) : BN > 64 ? 8 : 12;
-  static constexpr int COLS = BN / 2;                    // columns an epilogue warp sums
+  static constexpr int COLS = BN / EW;                   // columns an epilogue warp sums
+  static constexpr uint32_t STAGE_BYTES = 4 * EW * 8 * STAGE_LD * 4;
   // what the epilogue needs of a grid: the tokens' sums, the rows' scales and zeros
   static constexpr uint32_t GS_SCALES = X8 ? BN * 4 : 0, GS_ZEROS = GS_SCALES + LIN_BLOCK * 4;
   static constexpr uint32_t GS = GS_ZEROS + LIN_BLOCK;
   static constexpr int NG = 4;
   static constexpr uint32_t SMEM_USED = 2 * NX * BOX + NW * WS + STAGE_BYTES + NG * GS + 1024 /*align*/ + 512 /*barriers*/;
   static constexpr uint32_t SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA an SM
-  // registers a thread of each warpgroup, out of 5 x 96 as launched
+  // registers a thread of each warpgroup, out of those launched with
   static constexpr bool SPLIT_REGS = BN >= 128;
   static constexpr int R_LOAD = 56, R_EXPAND = 64, R_SUM = 144;
   static constexpr int ND = 4;                           // barriers of "the stage's MMAs are done"
@@ -73,7 +74,7 @@ struct TcShape {
   static_assert(ND >= NX && ND >= NA, "a barrier's phase is waited for before the next one can end");
   static_assert(ACC_COLS + NA * 64 <= 512, "TMEM");
   static_assert(SMEM <= 232448, "shared memory");
-  static_assert(R_LOAD + 2 * R_EXPAND + 2 * R_SUM <= 5 * 96, "registers");
+  static_assert(R_LOAD + 2 * R_EXPAND + EW * R_SUM <= (3 + EW) * LAUNCH_REGS, "registers");
   static_assert((uint32_t)BN * 128 * 4 <= 2 * NX * BOX || BN > 128, "parts of a split tile");
 };
 
@@ -220,13 +221,13 @@ __device__ __forceinline__ void linear_store8(const LinearParams& L, const float
 }
 
 template <class S>
-__global__ void __launch_bounds__(TC_THREADS, 1)
+__global__ void __launch_bounds__(S::THREADS, 1)
     k_linear_tc(const __grid_constant__ CUtensorMap xmap, const TcParams P) {
   extern __shared__ __align__(1024) unsigned char tc_smem[];
   unsigned char* xring = (unsigned char*)(((uintptr_t)tc_smem + 1023) & ~(uintptr_t)1023);
   unsigned char* wring = xring + 2 * S::NX * S::BOX;
   float* stage = (float*)(wring + S::NW * S::WS);
-  unsigned char* gring = (unsigned char*)stage + STAGE_BYTES;
+  unsigned char* gring = (unsigned char*)stage + S::STAGE_BYTES;
   uint64_t* bars = (uint64_t*)(gring + S::NG * S::GS);
   // full: xF tokens, wF codes, aF expanded codes, cF sums, gF grids; free again: sD tokens and
   // expanded codes of a stage, wE codes, cE sums, gE grids
@@ -242,8 +243,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     for (int i = 0; i < S::NA; ++i) mbar_init(&aF[i], 8);
     for (int i = 0; i < S::NW; ++i) mbar_init(&wF[i], 1), mbar_init(&wE[i], S::X8 ? 4 : 8);   // the teams that read it
 
-    for (int i = 0; i < S::NACC; ++i) mbar_init(&cF[i], 1), mbar_init(&cE[i], 8);
-    for (int i = 0; i < S::NG; ++i) mbar_init(&gF[i], 1), mbar_init(&gE[i], 8);
+    for (int i = 0; i < S::NACC; ++i) mbar_init(&cF[i], 1), mbar_init(&cE[i], 4 * S::EW);
+    for (int i = 0; i < S::NG; ++i) mbar_init(&gF[i], 1), mbar_init(&gE[i], 4 * S::EW);
     mbar_init(done, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -271,6 +272,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     tt = group * TOKEN_GROUP + in % wide;
   };
   auto timed_out = [&]() {
+    pdl_wait();        // the status is cleared by the kernel before
     if (!*abort_flag) raise_status(P.status, BAKRON_ERR_TIMEOUT);
     *abort_flag = 1;
   };
@@ -284,6 +286,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   if (warp < 4) {
     if constexpr (S::SPLIT_REGS) regs_down<S::R_LOAD>();
     if (warp == 0) {
+      pdl_wait();      // the tokens' copy
       int it = 0;
       bool ok = true;
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
@@ -333,6 +336,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       for (int j = it > S::NW ? it - S::NW : 0; j < it; ++j)
         if (!mbar_wait(&wF[j % S::NW], (uint32_t)(j / S::NW) & 1u, drain)) timed_out();
     } else if (warp == 3) {
+      pdl_wait();      // the tokens' sums
       int it = 0;
       bool ok = true;
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
@@ -550,16 +554,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     }
   } else {
     if constexpr (S::SPLIT_REGS) regs_up<S::R_SUM>();
-    const int q = warp & 3, ch = (warp - 12) >> 2;      // lane quarter, half of the columns
+    const int q = warp & 3, ch = (warp - 12) >> 2;      // lane quarter, part of the columns
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     int g = 0, ig = 0;
     bool ok = true;
     for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
       int rt, tt;
       place(tile, rt, tt);
-      float acc[S::COLS];
+      Two acc[S::COLS / 2];       // in pairs: half the instructions (issue slots are what is short)
 #pragma unroll
-      for (int i = 0; i < S::COLS; ++i) acc[i] = 0.f;
+      for (int i = 0; i < S::COLS / 2; ++i) acc[i] = Two(0.f, 0.f);
       Segments seg(P, kb0 * 4);
       float s = 0.f;
       const unsigned char* grid = nullptr;
@@ -594,7 +598,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             if (lead) mbar_arrive(&cE[buf]);
           }
 #pragma unroll
-          for (int i = 0; i < LD; ++i) acc[c + i] = fmaf(s, __uint_as_float(r[i]), acc[c + i]);
+          for (int i = 0; i < LD; i += 2)
+            acc[(c + i) / 2] = Two::fma(Two(s, s), Two(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), acc[(c + i) / 2]);
         }
         chunk = seg.left == INT_MAX ? INT_MAX : chunk + seg.left;
         seg.next();
@@ -606,10 +611,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
             for (int i = 0; i < S::COLS; i += 4) {
               const float4 x = sums[i / 4];
-              acc[i] = fmaf(c, x.x, acc[i]);
-              acc[i + 1] = fmaf(c, x.y, acc[i + 1]);
-              acc[i + 2] = fmaf(c, x.z, acc[i + 2]);
-              acc[i + 3] = fmaf(c, x.w, acc[i + 3]);
+              acc[i / 2] = Two::fma(Two(c, c), Two(x.x, x.y), acc[i / 2]);
+              acc[i / 2 + 1] = Two::fma(Two(c, c), Two(x.z, x.w), acc[i / 2 + 1]);
             }
           }
           __syncwarp();
@@ -621,7 +624,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       if (S::BN <= 128 && P.splits > 1) {
         // [token][128 rows] over the tokens' ring: every MMA that read it is complete
 #pragma unroll
-        for (int i = 0; i < S::COLS; ++i) ((float*)xring)[(ch * S::COLS + i) * 128 + q * 32 + lane] = acc[i];
+        for (int i = 0; i < S::COLS; i += 2) {
+          float* to = (float*)xring + (ch * S::COLS + i) * 128 + q * 32 + lane;
+          acc[i / 2].get(to[0], to[128]);
+        }
       } else {
         float* mine = stage + (warp - 12) * 8 * STAGE_LD;
         const int row0 = rt * LIN_BLOCK + q * 32 + (lane & 3) * 8;
@@ -632,7 +638,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           for (int c = 0; c < S::COLS / 8; ++c)
             if (b == c) {     // registers: no index that is not constant
 #pragma unroll
-              for (int i = 0; i < 8; ++i) mine[i * STAGE_LD + lane] = acc[8 * c + i];
+              for (int i = 0; i < 8; i += 2)
+                acc[4 * c + i / 2].get(mine[i * STAGE_LD + lane], mine[(i + 1) * STAGE_LD + lane]);
             }
           __syncwarp();
           const int64_t tok = (int64_t)tt * S::BN + ch * S::COLS + b * 8 + (lane >> 2);
@@ -649,7 +656,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       int rt, tt;
       place(tile0, rt, tt);
       const int row = rt * LIN_BLOCK + (threadIdx.x & 127);
-      for (int t = part * 5 + (threadIdx.x >> 7); t < S::BN; t += 5 * P.splits) {
+      for (int t = part * (3 + S::EW) + (threadIdx.x >> 7); t < S::BN; t += (3 + S::EW) * P.splits) {
         const int64_t tok = (int64_t)tt * S::BN + t;
         if (tok >= L.rows) break;
         float v = 0.f;
@@ -669,8 +676,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 
 // Tokens as TMA can read them: rows of 16-byte multiples, e4m3 widened to bf16 (exact)
 // where the codes have 8 bits.
+// Clears the status, too.
 template <bool X8, bool WIDEN>
-__global__ void __launch_bounds__(256) k_linear_rows(const void* x, int64_t ldx, int rows, int n, void* out, int64_t ldo) {
+__global__ void __launch_bounds__(256)
+    k_linear_rows(const void* x, int64_t ldx, int n, void* out, int64_t ldo, int* status) {
+  pdl_trigger();
+  if (blockIdx.x + blockIdx.y + threadIdx.x == 0) *status = 0;
   const int64_t row = blockIdx.x;
   for (int k = blockIdx.y * 1024 + threadIdx.x; k < min(n, (int)(blockIdx.y + 1) * 1024); k += 256) {
     if constexpr (!X8) {
@@ -690,6 +701,7 @@ __global__ void __launch_bounds__(256) k_linear_rows(const void* x, int64_t ldx,
 // token (zeros for the padding tokens up to ld); the status word cleared beside.
 __global__ void __launch_bounds__(256)
     k_token_sums(const uint8_t* x, int64_t ldx, int rows, int n, int pieces, int width, float* sums, int64_t ld, int* status) {
+  pdl_trigger();
   if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
   const int64_t tok = blockIdx.x * 8 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
@@ -715,6 +727,11 @@ __global__ void __launch_bounds__(256)
   }
 }
 
+__global__ void k_clear_status(int* status) {
+  pdl_trigger();
+  *status = 0;
+}
+
 template <class S>
 int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   static OncePerDevice once;
@@ -722,7 +739,7 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
     cudaFuncAttributes a;
     cudaError_t e = cudaFuncGetAttributes(&a, k_linear_tc<S>);
     // the warpgroups' shares (setmaxnreg) are taken from what the block is launched with
-    if (e == cudaSuccess && S::SPLIT_REGS && a.numRegs != 96) e = cudaErrorInvalidConfiguration;
+    if (e == cudaSuccess && S::SPLIT_REGS && a.numRegs != S::LAUNCH_REGS) e = cudaErrorInvalidConfiguration;
     return e != cudaSuccess
                ? e
                : cudaFuncSetAttribute(k_linear_tc<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
@@ -756,15 +773,19 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
     return BAKRON_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(P.splits > 1 ? tiles * P.splits : std::min<int64_t>(tiles, ROW_SMS)));
-  cfg.blockDim = dim3(TC_THREADS);
+  cfg.blockDim = dim3(S::THREADS);
   cfg.dynamicSmemBytes = S::SMEM;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = P.splits;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  // Starts beside the kernel before (which clears the status and makes the tokens' copy or
+  // sums): barriers, TMEM and the first codes are ready when that is done.
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = P.splits;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = P.splits > 1 ? 1 : 0;
+  cfg.numAttrs = P.splits > 1 ? 2 : 1;
   BK_CUDA_OK(cudaLaunchKernelEx(&cfg, k_linear_tc<S>, map, P));
   return BAKRON_OK;
 }
@@ -825,7 +846,6 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
   const TcWorkspace W(L.x, x8, L.rows, L.ldx, L.n, bytes8, L.G);
   P.sums = (const float*)((char*)workspace + 256);
   P.sums_ld = W.sums_ld;
-  if (!x8 || bytes8) BK_CUDA_OK(cudaMemsetAsync(workspace, 0, 4, s));
   const void* x = L.x;
   int64_t ldx = L.ldx;
   if (!rows_in_place(x, x8, ldx, bytes8)) {
@@ -833,13 +853,16 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
     const dim3 grid((unsigned)L.rows, (unsigned)ceil_div(L.n, 1024));
     ldx = round_up(L.n, 16);
     if (!x8)
-      k_linear_rows<false, false><<<grid, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+      k_linear_rows<false, false><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, P.status);
     else if (bytes8)
-      k_linear_rows<true, true><<<grid, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+      k_linear_rows<true, true><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, P.status);
     else
-      k_linear_rows<true, false><<<grid, 256, 0, s>>>(x, L.ldx, L.rows, L.n, out, ldx);
+      k_linear_rows<true, false><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, P.status);
     BK_CUDA_OK(cudaGetLastError());
     x = out;
+  } else if (!x8 || bytes8) {
+    k_clear_status<<<1, 1, 0, s>>>(P.status);
+    BK_CUDA_OK(cudaGetLastError());
   }
   if (bytes8) return launch_bn<true, false>(x, ldx, P, s);
   return x8 ? launch_bn<false, true>(x, ldx, P, s) : launch_bn<false, false>(x, ldx, P, s);

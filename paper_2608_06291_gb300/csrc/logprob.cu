@@ -87,23 +87,6 @@ struct Sums {
   }
 };
 
-// Two fp32 operations in one instruction.
-struct Two {
-  uint64_t v;
-  __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-  __device__ __forceinline__ static Two fma(const Two& a, const Two& b, const Two& c) {
-    Two r(0.f, 0.f);
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-  }
-  __device__ __forceinline__ static Two add(const Two& a, const Two& b) {
-    Two r(0.f, 0.f);
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-  }
-};
-
 // A row as aligned 16-byte vectors of PER elements: vector 0 starts `off` elements before
 // the row.
 template <typename T>
