@@ -57,13 +57,13 @@ struct TcShape {
   static constexpr uint32_t BOX = BN * 128;              // bytes of a box of tokens
   static constexpr uint32_t WS = W8 ? 16384 : 8192;      // bytes of a block's codes
   static constexpr int NX = BN > 128 ? 3 : 4;
-  static constexpr int NW = W8 ? (BN > 64 ? 4 : 6) : BN > 64 ? 8 : 12;
+  static constexpr int NW = W8 ? (BN > 128 ? 3 : BN > 64 ? 4 : 6) : BN > 128 ? 7 : BN > 64 ? 8 : 12;
   static constexpr int COLS = BN / EW;                   // columns an epilogue warp sums
   static constexpr uint32_t STAGE_BYTES = 4 * EW * 8 * STAGE_LD * 4;
   // what the epilogue needs of a grid: the tokens' sums, the rows' scales and zeros
   static constexpr uint32_t GS_SCALES = X8 ? BN * 4 : 0, GS_ZEROS = GS_SCALES + LIN_BLOCK * 4;
   static constexpr uint32_t GS = GS_ZEROS + LIN_BLOCK;
-  static constexpr int NG = 4;
+  static constexpr int NG = BN > 128 ? 8 : 16;           // enough for a load's way from memory
   static constexpr uint32_t SMEM_USED = 2 * NX * BOX + NW * WS + STAGE_BYTES + NG * GS + 1024 /*align*/ + 512 /*barriers*/;
   static constexpr uint32_t SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA an SM
   // registers a thread of each warpgroup, out of those launched with
@@ -88,13 +88,18 @@ struct TcParams {
   long long spin_cycles;
 };
 
-// A warp's wait, every lane testing (the vote keeps the control flow uniform); gives up
-// after `limit` cycles, or once another role has.
-__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, long long limit, volatile int* abort_flag) {
-  if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+// A warp's wait for two barriers, every lane testing (the vote keeps the control flow
+// uniform); gives up after `limit` cycles, or once another role has.
+__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, uint64_t* bar2, uint32_t parity2, long long limit,
+                                        volatile int* abort_flag) {
+  auto both = [&]() {
+    const bool a = mbar_test(bar, parity), b = bar2 == bar || mbar_test(bar2, parity2);
+    return __all_sync(0xffffffffu, a && b) != 0;
+  };
+  if (both()) return true;
   const long long t0 = clock64();
   while (true) {
-    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+    if (both()) return true;
     if (__any_sync(0xffffffffu, *abort_flag || clock64() - t0 > limit)) return false;
   }
 }
@@ -276,11 +281,12 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     if (!*abort_flag) raise_status(P.status, BAKRON_ERR_TIMEOUT);
     *abort_flag = 1;
   };
-  auto wait = [&](uint64_t* bar, uint32_t parity) {      // a warp
-    if (tc_wait(bar, parity, P.spin_cycles, abort_flag)) return true;
+  auto wait2 = [&](uint64_t* bar, uint32_t parity, uint64_t* bar2, uint32_t parity2) {      // a warp
+    if (tc_wait(bar, parity, bar2, parity2, P.spin_cycles, abort_flag)) return true;
     timed_out();
     return false;
   };
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return wait2(bar, parity, bar, parity); };
   auto wait_stage = [&](int it) { return wait(&sD[it % S::ND], (uint32_t)(it / S::ND) & 1u); };
   const uint32_t lead = lane == 0;
   if (warp < 4) {
@@ -386,14 +392,12 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         Segments seg(P, kb0 * 4);
         uint32_t more = 0;       // the segment has begun
         for (int st = 0; st < stages; ++st) {
-          if ((!here && (!wait(&xF[xs], xp) || !wait(&aF[as], ap))) || (!more && !sum_free())) {
+          if (!here && (!wait2(&xF[xs], xp, &aF[as], ap) || (!more && !sum_free()))) {
             ok = false;
             break;
           }
-          // a look at the next stage's barriers, of no consequence until then
           const uint32_t nxs = xs + 1 == S::NX ? 0 : xs + 1, nas = as + 1 == S::NA ? 0 : as + 1;
           const uint32_t nxp = xp ^ (uint32_t)(nxs == 0), nap = ap ^ (uint32_t)(nas == 0);
-          const bool nx = mbar_test(&xF[nxs], nxp), na = mbar_test(&aF[nas], nap);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint64_t b = desc0 + (uint64_t)(xs * (2 * S::BOX >> 4));
           const uint32_t a = tmem_a + as * 64;
@@ -451,7 +455,11 @@ __global__ void __launch_bounds__(S::THREADS, 1)
               }
             }
           }
-          here = __all_sync(0xffffffffu, nx && na);
+          // A look at what the next stage waits for, while the last MMAs run: most often it is
+          // all there, and nothing is waited for one by one.
+          const bool nx = mbar_test(&xF[nxs], nxp), na = mbar_test(&aF[nas], nap);
+          const bool ns = more || g < S::NACC || mbar_test(&cE[g & (S::NACC - 1)], (uint32_t)(g / S::NACC - 1) & 1u);
+          here = __all_sync(0xffffffffu, nx && na && ns);
           xs = nxs;
           xp = nxp;
           as = nas;
@@ -478,17 +486,23 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       auto zero_of = [&](int chunk) { return (int)zeros[(L.G == 1 ? 0 : min(chunk / L.chunks, L.G - 1)) * L.mp]; };
       // the zeros of this team's two chunks of a block: one grid a block, or one a chunk
       const bool one = L.G == 1 || L.chunks % 4 == 0;
-      int z[2], zn[2];
-      auto zeros_of = [&](int kb) {
-        if (S::X8) return;
-        zn[0] = zero_of(kb * 4 + 2 * team);
-        zn[1] = one ? zn[0] : zero_of(kb * 4 + 2 * team + 1);
+      // (four blocks ahead: a load's way from memory)
+      auto zeros_of = [&](int kb) -> int {
+        if (S::X8 || kb >= kb1) return 0;
+        const int z = zero_of(kb * 4 + 2 * team);
+        return z | (one ? z : zero_of(kb * 4 + 2 * team + 1)) << 8;
       };
-      zeros_of(kb0);
+      int zq[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) zq[i] = zeros_of(i == 0 || L.G > 1 ? kb0 + i : kb1);
       for (int kb = kb0; kb < kb1; kb += S::BPS, ib += S::BPS, ++ia) {
-        z[0] = zn[0];
-        z[1] = zn[1];
-        if (L.G > 1 && kb + 1 < kb1) zeros_of(kb + 1);
+        const int z[2] = {zq[0] & 255, zq[0] >> 8};
+        if (L.G > 1) {
+          zq[0] = zq[1];
+          zq[1] = zq[2];
+          zq[2] = zq[3];
+          zq[3] = zeros_of(kb + 4);
+        }
         const int block = S::X8 ? ib + team : ib, sw = block % S::NW, sa = ia % S::NA;
         if (S::X8 && kb + team >= kb1) {       // half a stage: nothing for this team
           __syncwarp();
@@ -568,29 +582,27 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       float s = 0.f;
       const unsigned char* grid = nullptr;
       for (int chunk = kb0 * 4; chunk < kb1 * 4; ++g) {
-        if (L.G > 1 || chunk == kb0 * 4) {       // the next grid
-          if (!wait(&gF[ig % S::NG], (uint32_t)(ig / S::NG) & 1u)) {
-            ok = false;
-            break;
-          }
-          grid = gring + (ig % S::NG) * S::GS;
-          s = reinterpret_cast<const float*>(grid + S::GS_SCALES)[q * 32 + lane] * (S::X8 ? 256.f : 1.f);
-        }
         const int buf = g & (S::NACC - 1);
-        if (!wait(&cF[buf], (uint32_t)(g / S::NACC) & 1u)) {
+        const bool fresh = L.G > 1 || chunk == kb0 * 4;       // the next grid
+        uint64_t* gbar = &gF[ig % S::NG];
+        if (!(fresh ? wait2(&cF[buf], (uint32_t)(g / S::NACC) & 1u, gbar, (uint32_t)(ig / S::NG) & 1u)
+                    : wait(&cF[buf], (uint32_t)(g / S::NACC) & 1u))) {
           ok = false;
           break;
         }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (fresh) {
+          grid = gring + (ig % S::NG) * S::GS;
+          s = reinterpret_cast<const float*>(grid + S::GS_SCALES)[q * 32 + lane] * (S::X8 ? 256.f : 1.f);
+        }
+        // As much of the sums at once as registers allow: a warp's turn is a chain of waits.
         const uint32_t at = tmem + lanes + buf * S::BN + ch * S::COLS;
-        constexpr int LD = S::COLS % 32 == 0 ? 32 : 16;
+        constexpr int LD = S::COLS <= 64 ? S::COLS : 32;
 #pragma unroll
         for (int c = 0; c < S::COLS; c += LD) {
-          uint32_t r[LD];
-          if constexpr (LD == 32)
-            tmem_ld32(at + c, r);
-          else
-            tmem_ld16(at + c, r);
+          uint32_t r[LD / 16][16];
+#pragma unroll
+          for (int i = 0; i < LD / 16; ++i) tmem_ld16(at + c + 16 * i, r[i]);
           tmem_wait_ld();
           if (c + LD == S::COLS) {      // all read: the next segment's MMAs may have it
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -599,7 +611,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           }
 #pragma unroll
           for (int i = 0; i < LD; i += 2)
-            acc[(c + i) / 2] = Two::fma(Two(s, s), Two(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), acc[(c + i) / 2]);
+            acc[(c + i) / 2] = Two::fma(Two(s, s), Two(__uint_as_float(r[i / 16][i % 16]), __uint_as_float(r[i / 16][i % 16 + 1])),
+                                        acc[(c + i) / 2]);
         }
         chunk = seg.left == INT_MAX ? INT_MAX : chunk + seg.left;
         seg.next();
@@ -793,10 +806,13 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
 template <bool W8, bool X8>
 int launch_bn(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   // The token tile with the shortest schedule: rounds of tiles over the SMs, a tile costing
-  // its tokens and about 32 more (expanding the codes, the way out).
+  // its tokens and about 32 more (expanding the codes, the way out).  With grids along a row
+  // not 192, whose sums are not read in one go (4096 x 28672 x 8192 bf16 in groups of 128: 1.89 ms,
+  // 128: MS128 ms).
   int best = 32;
   double cost = 1e300;
   for (int bn : {192, 128, 64, 32}) {
+    if (bn == 192 && P.L.G > 1) continue;
     const double tiles = (double)P.row_tiles * ceil_div(P.L.rows, bn);
     const double c = tiles >= ROW_SMS ? ceil(tiles / ROW_SMS) * (bn + 32) : tiles / ROW_SMS * (bn + 32) + (bn > 128 ? bn : 0);
     if (c < 0.97 * cost) {
