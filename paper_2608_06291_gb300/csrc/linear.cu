@@ -161,22 +161,33 @@ __global__ void __launch_bounds__(FEW_WARPS * 32) k_linear_few(const LinearParam
           cur[mt][n][e] = 0.f;
         }
   };
-  for (int kb = warp; kb < P.kblocks; kb += FEW_WARPS) {
+  // the next block's codes and tokens are on their way while this one is multiplied
+  struct Block {
     uint4 u[2][2][UW];
+    uint32_t b[NT][4][4];
+  };
+  auto load = [&](int kb, Block& to) {
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
       for (int r = 0; r < 2; ++r)
 #pragma unroll
         for (int h = 0; h < UW; ++h)
-          u[mt][r][h] = *reinterpret_cast<const uint4*>(
-              base + ((int64_t)kb * 4 * UW + 4 * h) * 2048 + (mt * 16 + r * 8) * 16);
-    uint32_t b[NT][4][4];
+          to.u[mt][r][h] = __ldg(reinterpret_cast<const uint4*>(
+              base + ((int64_t)kb * 4 * UW + 4 * h) * 2048 + (mt * 16 + r * 8) * 16));
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        load_x8<X8>(P, tok0 + n * 8 + g, kb * LIN_BLOCK + 32 * j + 8 * t, b[n][j]);
+        load_x8<X8>(P, tok0 + n * 8 + g, kb * LIN_BLOCK + 32 * j + 8 * t, to.b[n][j]);
+  };
+  Block next;
+  if (warp < P.kblocks) load(warp, next);
+  for (int kb = warp; kb < P.kblocks; kb += FEW_WARPS) {
+    const Block now_ = next;
+    const auto& u = now_.u;
+    const auto& b = now_.b;
+    if (kb + FEW_WARPS < P.kblocks) load(kb + FEW_WARPS, next);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int now = P.G == 1 ? 0 : min((kb * 4 + j) / P.chunks, P.G - 1);
@@ -315,7 +326,8 @@ extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, c
   P.rows = rows; P.m = m; P.n = n; P.mp = L.mp; P.kblocks = (int)(L.np / LIN_BLOCK);
   P.chunks = L.G == 1 ? (int)(L.np / 32) : L.group / 32;
   P.G = (int)L.G; P.activation = activation; P.yf32 = ydtype == BAKRON_F32;
-  P.xvec = x8 ? ((uintptr_t)x | (uintptr_t)ldx) % 8 == 0 : aligned16(x, ldx * 2);
+  const int64_t step = rows > 1 ? ldx : 0;      // one row may have any stride
+  P.xvec = x8 ? ((uintptr_t)x | (uintptr_t)step) % 8 == 0 : aligned16(x, step * 2);
   const int ys = P.yf32 ? 4 : 2;
   P.yvec = aligned16(y, ldy * ys) && (!residual || aligned16(residual, ldr * ys));
   cudaStream_t s = (cudaStream_t)stream;

@@ -81,12 +81,26 @@ struct TcShape {
 struct TcParams {
   LinearParams L;
   int row_tiles, token_tiles, splits, per;   // per: 128-column blocks of a split's part
+  uint32_t by_chunks;     // 2^32 / (chunks of a grid), rounded up: chunk / chunks by a product; 0 for 1
   int seg_chunks, segs;   // chunks of a segment; how many there are (the last takes the rest)
   const float* sums;      // e4m3 tokens: [segment of a grid][token, padded] sum of the values
   int64_t sums_ld;
   int* status;
   long long spin_cycles;
 };
+
+// Whether a phase is over, without waiting (mbar_test's try_wait may hold the thread a while).
+__device__ __forceinline__ bool mbar_look(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 
 // A warp's wait for two barriers, every lane testing (the vote keeps the control flow
 // uniform); gives up after `limit` cycles, or once another role has.
@@ -457,8 +471,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           }
           // A look at what the next stage waits for, while the last MMAs run: most often it is
           // all there, and nothing is waited for one by one.
-          const bool nx = mbar_test(&xF[nxs], nxp), na = mbar_test(&aF[nas], nap);
-          const bool ns = more || g < S::NACC || mbar_test(&cE[g & (S::NACC - 1)], (uint32_t)(g / S::NACC - 1) & 1u);
+          const bool nx = mbar_look(&xF[nxs], nxp), na = mbar_look(&aF[nas], nap);
+          const bool ns = more || g < S::NACC || mbar_look(&cE[g & (S::NACC - 1)], (uint32_t)(g / S::NACC - 1) & 1u);
           here = __all_sync(0xffffffffu, nx && na && ns);
           xs = nxs;
           xp = nxp;
@@ -483,25 +497,27 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       int rt, tt;
       place(tile, rt, tt);
       const uint8_t* zeros = L.zeros + (int64_t)rt * LIN_BLOCK + row;
-      auto zero_of = [&](int chunk) { return (int)zeros[(L.G == 1 ? 0 : min(chunk / L.chunks, L.G - 1)) * L.mp]; };
-      // the zeros of this team's two chunks of a block: one grid a block, or one a chunk
-      const bool one = L.G == 1 || L.chunks % 4 == 0;
-      // (four blocks ahead: a load's way from memory)
-      auto zeros_of = [&](int kb) -> int {
-        if (S::X8 || kb >= kb1) return 0;
-        const int z = zero_of(kb * 4 + 2 * team);
-        return z | (one ? z : zero_of(kb * 4 + 2 * team + 1)) << 8;
+      auto zero_of = [&](int chunk) -> uint32_t {
+        const int grid = L.G == 1 ? 0 : min(P.by_chunks ? (int)__umulhi(chunk, P.by_chunks) : chunk, L.G - 1);
+        return zeros[grid * L.mp];
       };
-      int zq[4];
+      // the zeros of this team's two chunks of a block, asked for four blocks ahead (a load's way
+      // from memory) and not looked at before
+      uint32_t z0[4], z1[4];
+      auto zeros_of = [&](int kb, int i) {
+        z0[i] = z1[i] = 0;
+        if (S::X8 || kb >= kb1) return;
+        z0[i] = zero_of(kb * 4 + 2 * team);
+        z1[i] = zero_of(kb * 4 + 2 * team + 1);
+      };
 #pragma unroll
-      for (int i = 0; i < 4; ++i) zq[i] = zeros_of(i == 0 || L.G > 1 ? kb0 + i : kb1);
+      for (int i = 0; i < 4; ++i) zeros_of(i == 0 || L.G > 1 ? kb0 + i : kb1, i);
       for (int kb = kb0; kb < kb1; kb += S::BPS, ib += S::BPS, ++ia) {
-        const int z[2] = {zq[0] & 255, zq[0] >> 8};
-        if (L.G > 1) {
-          zq[0] = zq[1];
-          zq[1] = zq[2];
-          zq[2] = zq[3];
-          zq[3] = zeros_of(kb + 4);
+        const uint32_t z[2] = {z0[0], z1[0]};
+        if (!S::X8 && L.G > 1) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i) z0[i] = z0[i + 1], z1[i] = z1[i + 1];
+          zeros_of(kb + 4, 3);
         }
         const int block = S::X8 ? ib + team : ib, sw = block % S::NW, sa = ia % S::NA;
         if (S::X8 && kb + team >= kb1) {       // half a stage: nothing for this team
@@ -806,13 +822,10 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
 template <bool W8, bool X8>
 int launch_bn(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   // The token tile with the shortest schedule: rounds of tiles over the SMs, a tile costing
-  // its tokens and about 32 more (expanding the codes, the way out).  With grids along a row
-  // not 192, whose sums are not read in one go (4096 x 28672 x 8192 bf16 in groups of 128: 1.89 ms,
-  // 128: MS128 ms).
+  // its tokens and about 32 more (expanding the codes, the way out).
   int best = 32;
   double cost = 1e300;
   for (int bn : {192, 128, 64, 32}) {
-    if (bn == 192 && P.L.G > 1) continue;
     const double tiles = (double)P.row_tiles * ceil_div(P.L.rows, bn);
     const double c = tiles >= ROW_SMS ? ceil(tiles / ROW_SMS) * (bn + 32) : tiles / ROW_SMS * (bn + 32) + (bn > 128 ? bn : 0);
     if (c < 0.97 * cost) {
@@ -855,6 +868,7 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
   TcParams P{};
   P.L = L;
   P.row_tiles = (int)(L.mp / LIN_BLOCK);
+  P.by_chunks = L.chunks > 1 ? (uint32_t)((((uint64_t)1 << 32) + L.chunks - 1) / L.chunks) : 0;
   P.seg_chunks = L.G > 1 ? L.chunks : x8 && !bytes8 ? SEG_MMAS : SEG_MMAS / 2;
   P.segs = L.G > 1 ? L.G : INT_MAX / SEG_MMAS - 1;
   P.status = (int*)workspace;
