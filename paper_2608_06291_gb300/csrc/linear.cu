@@ -138,8 +138,10 @@ constexpr int FEW_WARPS = 8;     // they share its columns, block by block
 
 // 32 rows x 8 NT tokens per CTA.  What's rows are the rows of mma.sync's first operand,
 // read straight from the packed units into its registers; the tokens are its columns.
+// Bound by the codes' way from memory and, per call, by the launch: 1 token x 28672 x 8192,
+// 118 MB of codes, 48 us (2.5 TB/s); 1 x 4096 x 4096 about 11 us a call.
 template <int NT, bool W8, bool X8>
-__global__ void __launch_bounds__(FEW_WARPS * 32) k_linear_few(const LinearParams P) {
+__global__ void __launch_bounds__(FEW_WARPS * 32, NT == 1 && !W8 ? 3 : 2) k_linear_few(const LinearParams P) {
   constexpr int UW = W8 ? 2 : 1;     // units of a row a lane reads per block
   __shared__ float red[FEW_WARPS][8 * NT][FEW_ROWS + 1];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -161,10 +163,10 @@ __global__ void __launch_bounds__(FEW_WARPS * 32) k_linear_few(const LinearParam
           cur[mt][n][e] = 0.f;
         }
   };
-  // the next block's codes and tokens are on their way while this one is multiplied
+  // the next block's codes are on their way while this one is multiplied (the tokens too took
+  // so many registers that 16 tokens x 28672 x 8192 went from 86 to 156 us)
   struct Block {
     uint4 u[2][2][UW];
-    uint32_t b[NT][4][4];
   };
   auto load = [&](int kb, Block& to) {
 #pragma unroll
@@ -175,18 +177,18 @@ __global__ void __launch_bounds__(FEW_WARPS * 32) k_linear_few(const LinearParam
         for (int h = 0; h < UW; ++h)
           to.u[mt][r][h] = __ldg(reinterpret_cast<const uint4*>(
               base + ((int64_t)kb * 4 * UW + 4 * h) * 2048 + (mt * 16 + r * 8) * 16));
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        load_x8<X8>(P, tok0 + n * 8 + g, kb * LIN_BLOCK + 32 * j + 8 * t, to.b[n][j]);
   };
   Block next;
   if (warp < P.kblocks) load(warp, next);
   for (int kb = warp; kb < P.kblocks; kb += FEW_WARPS) {
-    const Block now_ = next;
-    const auto& u = now_.u;
-    const auto& b = now_.b;
+    const Block here = next;
+    const auto& u = here.u;
+    uint32_t b[NT][4][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        load_x8<X8>(P, tok0 + n * 8 + g, kb * LIN_BLOCK + 32 * j + 8 * t, b[n][j]);
     if (kb + FEW_WARPS < P.kblocks) load(kb + FEW_WARPS, next);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -257,6 +259,8 @@ void launch_few(const LinearParams& P, bool w8, bool x8, cudaStream_t s) {
 }
 
 constexpr int LIN_MAX_DIM = 1 << 17;
+// Up to here the codes' reading is all there is, and mma.sync is enough (16 tokens x 11008 x 4096:
+// 19 us, by the tensor-memory kernel 25).
 constexpr int FEW_TOKENS = 16;
 
 bool weight_ok(int m, int n, int qmax, int group_size) {

@@ -65,11 +65,22 @@ struct LinearParams {
   int yvec;                 // y and the residual 16 bytes at a time, from columns that are multiples of 8
 };
 
+// erf to 1.5e-7 (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26).  An fp32
+// erf of the usual accuracy cost the epilogue of a 4096 x 28672 product 100 us.
+__device__ __forceinline__ float erf_short(float v) {
+  const float x = fabsf(v), t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f) * t;
+  return copysignf(fmaf(-p, __expf(-x * x), 1.f), v);
+}
+
 __device__ __forceinline__ float activate(float v, int a) {
   switch (a) {
-    case BAKRON_RELU: return v < 0.f ? 0.f : v;     // NaN stays
-    case BAKRON_SILU: return v / (1.f + expf(-v));
-    case BAKRON_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678f));
+    case BAKRON_RELU: return v < 0.f ? 0.f : v;                  // NaN stays
+    case BAKRON_SILU: return __fdividef(v, 1.f + __expf(-v));    // the divisor's overflow gives 0, as it should
+    case BAKRON_GELU: return 0.5f * v * (1.f + erf_short(v * 0.70710678f));
     default: return v;
   }
 }

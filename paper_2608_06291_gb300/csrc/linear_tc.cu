@@ -106,15 +106,13 @@ __device__ __forceinline__ bool mbar_look(uint64_t* bar, uint32_t parity) {
 // uniform); gives up after `limit` cycles, or once another role has.
 __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, uint64_t* bar2, uint32_t parity2, long long limit,
                                         volatile int* abort_flag) {
-  auto both = [&]() {
-    const bool a = mbar_test(bar, parity), b = bar2 == bar || mbar_test(bar2, parity2);
-    return __all_sync(0xffffffffu, a && b) != 0;
-  };
-  if (both()) return true;
+  const bool now = mbar_look(bar, parity) && (bar2 == bar || mbar_look(bar2, parity2));
+  if (__all_sync(0xffffffffu, now)) return true;
   const long long t0 = clock64();
   while (true) {
-    if (both()) return true;
     if (__any_sync(0xffffffffu, *abort_flag || clock64() - t0 > limit)) return false;
+    const bool a = mbar_test(bar, parity), b = bar2 == bar || mbar_test(bar2, parity2);
+    if (__all_sync(0xffffffffu, a && b)) return true;
   }
 }
 
