@@ -501,7 +501,8 @@ typedef enum {
 /*
  * bakron_linear -- y = act(x What^T + bias) + residual for `rows` tokens, What the m x n
  * weight of a packed buffer.
- *   x        device, rows x n, BAKRON_BF16 or BAKRON_E4M3, row stride ldx (>= n)
+ *   x        device, rows (at most 2^30) x n, BAKRON_BF16 or BAKRON_E4M3, row stride ldx
+ *            (>= n)
  *   xscales  device, `rows` fp32: token t stands for xscales[t] x[t], as
  *            bakron_rmsnorm leaves it; NULL: 1
  *   packed, m, n, qmax, group_size  the weight, as given to bakron_pack_weight

@@ -258,7 +258,7 @@ void launch_few(const LinearParams& P, bool w8, bool x8, cudaStream_t s) {
        : k_linear_few<NT, false, false><<<grid, FEW_WARPS * 32, 0, s>>>(P);
 }
 
-constexpr int LIN_MAX_DIM = 1 << 17;
+constexpr int LIN_MAX_DIM = 1 << 17, LIN_MAX_ROWS = 1 << 30;
 // Up to here the codes' reading is all there is, and mma.sync is enough (16 tokens x 11008 x 4096:
 // 19 us, by the tensor-memory kernel 25).
 constexpr int FEW_TOKENS = 16;
@@ -310,7 +310,7 @@ extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, c
                              const float* bias, int activation, const void* residual, int64_t ldr,
                              void* y, int ydtype, int64_t ldy, void* workspace,
                              size_t workspace_bytes, int sync, void* stream) {
-  if (rows < 0 || !weight_ok(m, n, qmax, group_size) || (xdtype != BAKRON_BF16 && xdtype != BAKRON_E4M3) ||
+  if (rows < 0 || rows > LIN_MAX_ROWS || !weight_ok(m, n, qmax, group_size) || (xdtype != BAKRON_BF16 && xdtype != BAKRON_E4M3) ||
       (ydtype != BAKRON_BF16 && ydtype != BAKRON_F32) || activation < BAKRON_NO_ACTIVATION ||
       activation > BAKRON_GELU)
     return BAKRON_ERR_INVALID_ARG;

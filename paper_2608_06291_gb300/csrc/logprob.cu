@@ -428,8 +428,8 @@ cudaError_t launch_logprob(const LogprobParams& P, cudaStream_t s) {
                                 (int)lp_ring_bytes<T>(LP_WARPS));
   });
   if (e != cudaSuccess) return e;
-  // Warps a row is shared by: as many as the GPU holds for all rows, but four (their tiles in
-  // flight together; 4095 rows of 128256 bf16, top 20: 1 warp 241 us, 2: 218, 4: 214, 8: 238) and
+  // Warps a row is shared by: as many as the GPU holds for all rows, at least four (their tiles
+  // are in flight together; 4095 rows of 128256 bf16, top 20: 1 warp 241 us, 2: 218, 4: 214, 8: 238) and
   // no more than there are tiles.
   const int tiles = ceil_div(P.v, LP_TILE) + (P.v % 8 ? 1 : 0);
   const int want = std::min(tiles, std::max(4, ROW_SMS * 32 / P.rows));

@@ -38,7 +38,7 @@ def test_pack_weight(L):
 def test_linear(L):
     ok = dict(x=FAKE, xdtype=BF16, rows=4, ldx=64, xscales=None, packed=FAKE, m=8, n=64, qmax=15, group=32, bias=None,
               activation=0, residual=None, ldr=0, y=FAKE, ydtype=BF16, ldy=8, ws=None, ws_bytes=0, sync=0, stream=None)
-    for bad in (dict(x=None), dict(xdtype=F32), dict(rows=-1), dict(ldx=63), dict(packed=None), dict(m=0), dict(n=0),
+    for bad in (dict(x=None), dict(xdtype=F32), dict(rows=-1), dict(rows=(1 << 30) + 1), dict(ldx=63), dict(packed=None), dict(m=0), dict(n=0),
                 dict(qmax=0), dict(group=16), dict(activation=4), dict(activation=-1), dict(residual=FAKE, ldr=7),
                 dict(y=None), dict(ydtype=E4M3), dict(ldy=7), dict(packed=ctypes.c_void_p(0x1008))):
         assert L.bakron_linear(*_with(ok, **bad)) == 1, bad
