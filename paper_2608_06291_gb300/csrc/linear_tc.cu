@@ -724,8 +724,31 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// Sums of e4m3 tokens' values over each of `pieces` ranges of `width` columns, a warp per
-// token (zeros for the padding tokens up to ld); the status word cleared beside.
+// The sum of up to 16 e4m3 values of a row, from column k (a multiple of 16) on.
+__device__ __forceinline__ float sum16(const uint8_t* row, int64_t k, int64_t end) {
+  if (k >= end) return 0.f;
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+  if (k + 16 <= end) {
+    const uint4 q = *reinterpret_cast<const uint4*>(row + k);
+    w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (k + j < end) w[j / 4] |= (uint32_t)row[k + j] << (8 * (j % 4));
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const auto two = (__nv_fp8x2_storage_t)(w[j / 2] >> (16 * (j % 2)) & 0xFFFFu);
+    const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3)));
+    s += f.x + f.y;
+  }
+  return s;
+}
+
+// Sums of e4m3 tokens' values over each of `pieces` ranges of `width` columns (multiples of 32),
+// a warp per token (zeros for the padding tokens up to ld); the status word cleared beside.
+// Rows start on 16 bytes.
 __global__ void __launch_bounds__(256)
     k_token_sums(const uint8_t* x, int64_t ldx, int rows, int n, int pieces, int width, float* sums, int64_t ld, int* status) {
   pdl_trigger();
@@ -733,23 +756,25 @@ __global__ void __launch_bounds__(256)
   const int64_t tok = blockIdx.x * 8 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (tok >= ld) return;
-  for (int p = 0; p < pieces; ++p) {
-    float s = 0.f;
-    if (tok < rows) {
-      const int64_t end = min((int64_t)n, (int64_t)(p + 1) * width);
-      for (int64_t k = (int64_t)p * width + 4 * lane; k < end; k += 128) {
-        uint32_t w = 0u;
-        if (k + 4 <= end) {      // rows start on 16 bytes, ranges on 32
-          w = *reinterpret_cast<const uint32_t*>(x + tok * ldx + k);
-        } else {
-          for (int j = 0; k + j < end; ++j) w |= (uint32_t)x[tok * ldx + k + j] << (8 * j);
-        }
-        const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3)));
-        const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3)));
-        s += (a.x + a.y) + (b.x + b.y);
-      }
-      s = warp_all(s, AddOp());
+  const int64_t end = tok < rows ? n : 0;
+  const uint8_t* row = x + (tok < rows ? tok : 0) * ldx;
+  if (width <= 512 && 512 % width == 0) {
+    // whole pieces in 512 columns: lanes of a piece add up, its first one writes
+    const int lanes = width / 16;
+#pragma unroll 4
+    for (int64_t k = 16 * lane; k < (int64_t)round_up((int64_t)pieces * width, 512); k += 512) {
+      float s = sum16(row, k, end);
+      for (int o = 1; o < lanes; o *= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (lane % lanes == 0 && k / width < pieces) sums[k / width * ld + tok] = s;
     }
+    return;
+  }
+  for (int p = 0; p < pieces; ++p) {
+    const int64_t to = min(end, (int64_t)(p + 1) * width);
+    float s = 0.f;
+#pragma unroll 4
+    for (int64_t k = (int64_t)p * width + 16 * lane; k < to; k += 512) s += sum16(row, k, to);
+    s = warp_all(s, AddOp());
     if (lane == 0) sums[p * ld + tok] = s;
   }
 }

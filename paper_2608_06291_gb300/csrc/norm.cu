@@ -300,6 +300,7 @@ __global__ void __launch_bounds__(MAXT) k_rmsnorm_back(const NormBackParams P) {
   __shared__ float2 slots[2][16];
   extern __shared__ __align__(16) unsigned char nb_ring[];   // [RING][h, dy, dsum][d]
   const int t = threadIdx.x, nt = blockDim.x, warp = t >> 5, lane = t & 31, warps = nt >> 5;
+  pdl_trigger();      // the parts' sum may get ready; it waits for this grid's end
   Raw8<W> weight[KEEP_W ? VPT : 1];
   if constexpr (KEEP_W) {
 #pragma unroll
@@ -464,6 +465,7 @@ __global__ void __launch_bounds__(256) k_rmsnorm_dw(const NormBackParams P) {
 __global__ void __launch_bounds__(1024) k_sum_parts(const float* part, int parts, int d, float* dw) {
   __shared__ float s[32][33];
   const int c = blockIdx.x * 32 + threadIdx.x;
+  pdl_wait();
   float v = 0.f;
   if (c < d)
     for (int p = threadIdx.y; p < parts; p += 32) v += part[(int64_t)p * d + c];
@@ -619,7 +621,6 @@ extern "C" int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void*
                                                        : back_launch<__nv_bfloat16, float>);
     BK_CUDA_OK(launch(P, s));
   }
-  k_sum_parts<<<(unsigned)ceil_div(d, 32), dim3(32, 32), 0, s>>>(P.part, P.parts, d, dw);
-  BK_CUDA_OK(cudaGetLastError());
+  BK_CUDA_OK(launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(d, 32)), dim3(32, 32), 0, s, P.part, P.parts, d, dw));
   return BAKRON_OK;
 }
