@@ -518,7 +518,13 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           zeros_of(kb + 4, 3);
         }
         const int block = S::X8 ? ib + team : ib, sw = block % S::NW, sa = ia % S::NA;
-        if (S::X8 && kb + team >= kb1) {       // half a stage: nothing for this team
+        if (S::X8 && kb + team >= kb1) {
+          // Half a stage: nothing for this team, but its arrival is this stage's, and may not come
+          // while the slot still counts those of the stage NA before.
+          if (ia >= S::NA && !wait_stage(ia - S::NA)) {
+            ok = false;
+            break;
+          }
           __syncwarp();
           if (lead) mbar_arrive(&aF[sa]);
           continue;
