@@ -64,16 +64,20 @@ struct TcShape {
   static constexpr uint32_t GS_SCALES = X8 ? BN * 4 : 0, GS_ZEROS = GS_SCALES + LIN_BLOCK * 4;
   static constexpr uint32_t GS = GS_ZEROS + LIN_BLOCK;
   static constexpr int NG = BN > 128 ? 8 : 16;           // enough for a load's way from memory
-  static constexpr uint32_t SMEM_USED = 2 * NX * BOX + NW * WS + STAGE_BYTES + NG * GS + 1024 /*align*/ + 512 /*barriers*/;
+  static constexpr int ND = 4;                           // barriers of "the stage's MMAs are done"
+  // behind the rings: the barriers, then TMEM's address and the abort flag
+  static constexpr int BARRIERS = NX + ND + 2 * NW + NA + 2 * NACC + 2 * NG + 1;
+  static constexpr uint32_t RINGS = 2 * NX * BOX + NW * WS + STAGE_BYTES + NG * GS;
+  static constexpr uint32_t SMEM_USED = 1024 /*align*/ + RINGS + BARRIERS * 8 + 8;
   static constexpr uint32_t SMEM = SMEM_USED < 120 * 1024 ? 120 * 1024 : SMEM_USED;   // one CTA an SM
   // registers a thread of each warpgroup, out of those launched with
   static constexpr bool SPLIT_REGS = BN >= 128;
   static constexpr int R_LOAD = 56, R_EXPAND = 64, R_SUM = 144;
-  static constexpr int ND = 4;                           // barriers of "the stage's MMAs are done"
   static_assert((ND & (ND - 1)) == 0 && (NACC & (NACC - 1)) == 0, "masks");
   static_assert(ND >= NX && ND >= NA, "a barrier's phase is waited for before the next one can end");
   static_assert(ACC_COLS + NA * 64 <= 512, "TMEM");
   static_assert(SMEM <= 232448, "shared memory");
+  static_assert(RINGS % 8 == 0 && (NW * WS) % 16 == 0 && GS % 16 == 0, "barriers and bulk copies are aligned");
   static_assert(R_LOAD + 2 * R_EXPAND + EW * R_SUM <= (3 + EW) * LAUNCH_REGS, "registers");
   static_assert((uint32_t)BN * 128 * 4 <= 2 * NX * BOX || BN > 128, "parts of a split tile");
 };
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
   // expanded codes of a stage, wE codes, cE sums, gE grids
   uint64_t *xF = bars, *sD = xF + S::NX, *wF = sD + S::ND, *wE = wF + S::NW, *aF = wE + S::NW, *cF = aF + S::NA,
            *cE = cF + S::NACC, *gF = cE + S::NACC, *gE = gF + S::NG, *done = gE + S::NG;
-  uint32_t* tmem_slot = (uint32_t*)(done + 1);
+  uint32_t* tmem_slot = (uint32_t*)(bars + S::BARRIERS);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
