@@ -491,7 +491,8 @@ struct BackPlan {
     const int nt = back_threads(d), row = 3 * d * es;
     ring = !nt || !vec || 2 * row > NB_SMEM ? 0 : nt > 256 || 2 * 3 * row > NB_SMEM ? 2 : 3;
     ctas = nt ? std::max(1, 512 / nt) : 4;
-    if (ring) ctas = std::min(640 / nt, NB_SMEM / (ring * row + 1024));
+    // (one CTA fits wherever its ring does: NB_SMEM leaves 8 KB of the SM's)
+    if (ring) ctas = std::max(1, std::min(640 / nt, NB_SMEM / (ring * row + 1024)));
   }
 };
 int back_parts(int rows, int d, int es, bool vec) {
