@@ -302,8 +302,7 @@ extern "C" int bakron_pack_weight(const uint8_t* codes, int64_t ldc, const float
 extern "C" size_t bakron_linear_workspace_bytes(const void* x, int xdtype, int rows, int64_t ldx,
                                                 int n, int qmax, int group_size) {
   if (rows <= FEW_TOKENS || !weight_ok(1, n, qmax, group_size)) return 0;
-  return linear_tc_workspace(x, xdtype == BAKRON_E4M3, rows, ldx, n, qmax > 15,
-                             group_size ? n / group_size : 1);
+  return linear_tc_workspace(x, xdtype == BAKRON_E4M3, rows, ldx, n, qmax > 15);
 }
 
 extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float* xscales,

@@ -121,9 +121,9 @@ __device__ __forceinline__ uint32_t pair8(uint32_t w0, uint32_t w1, int p, __nv_
   return *reinterpret_cast<uint32_t*>(&r);
 }
 
-// Many tokens (linear_tc.cu): the bytes of workspace its call needs (the status, sums of e4m3
-// tokens, the tokens' copy where they cannot be read as they are), and the call.
-size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8, int G);
+// Many tokens (linear_tc.cu): the bytes of workspace its call needs (the status, the tokens'
+// copy where they cannot be read as they are), and the call.
+size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8);
 int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cudaStream_t s);
 
 }  // namespace bakron

@@ -5,11 +5,12 @@
 // in shared memory as TMA leaves it (K-major, 128-byte swizzle).  So a code is read once
 // as 4 or 8 bits and never goes through shared memory in its expanded form.
 //   bf16 tokens: kind::f16, c - z in bf16 (|c - z| <= 255: exact).
-//   e4m3 tokens: kind::f8f6f4.  e4m3 is linear up to 16 2^-9 (byte i is i 2^-9), so the odd
-//     integer 2 c - 15 is a sign and its own four bits; c - z = (2 c - 15) / 2 + (7.5 - z),
-//     and the second part is a product with the sum of a token's values, formed once per
-//     grid by k_token_sums.  (From c and z by table it took 15 instructions of the integer
-//     pipe for 8 codes, which bound the whole kernel; this takes 9.)
+//   e4m3 tokens: kind::f8f6f4, c - z in e4m3 (|c - z| <= 15: exact).  e4m3 is linear up to
+//     16 2^-9 (byte i is i 2^-9), so c - z is a sign and |c - z| itself, four codes at a time.
+//     (The odd integer 2 c - 15, with 7.5 - z times the sum of a token's values, is cheaper to
+//     form, 830 us for 845 at 4096 x 28672 x 8192 with GELU, but its two parts cancel: a row with
+//     few codes beside its zero loses most of its bits.  In groups of 128, without GELU, it took
+//     2.19 ms, this 1.60.)
 // A grid's sum (a segment; 64 MMAs' columns where a row has one grid) accumulates in TMEM
 // from zero; the epilogue warps multiply it by the grid's scale and add it in fp32
 // registers while the next one is formed.
@@ -60,9 +61,7 @@ struct TcShape {
   static constexpr int NW = W8 ? (BN > 128 ? 3 : BN > 64 ? 4 : 6) : BN > 128 ? 7 : BN > 64 ? 8 : 12;
   static constexpr int COLS = BN / EW;                   // columns an epilogue warp sums
   static constexpr uint32_t STAGE_BYTES = 4 * EW * 8 * STAGE_LD * 4;
-  // what the epilogue needs of a grid: the tokens' sums, the rows' scales and zeros
-  static constexpr uint32_t GS_SCALES = X8 ? BN * 4 : 0, GS_ZEROS = GS_SCALES + LIN_BLOCK * 4;
-  static constexpr uint32_t GS = GS_ZEROS + LIN_BLOCK;
+  static constexpr uint32_t GS = LIN_BLOCK * 4;          // what the epilogue needs of a grid: the rows' scales
   static constexpr int NG = BN > 128 ? 8 : 16;           // enough for a load's way from memory
   static constexpr int ND = 4;                           // barriers of "the stage's MMAs are done"
   // behind the rings: the barriers, then TMEM's address and the abort flag
@@ -87,8 +86,6 @@ struct TcParams {
   int row_tiles, token_tiles, splits, per;   // per: 128-column blocks of a split's part
   uint32_t by_chunks;     // 2^32 / (chunks of a grid), rounded up: chunk / chunks by a product; 0 for 1
   int seg_chunks, segs;   // chunks of a segment; how many there are (the last takes the rest)
-  const float* sums;      // e4m3 tokens: [segment of a grid][token, padded] sum of the values
-  int64_t sums_ld;
   int* status;
   long long spin_cycles;
 };
@@ -197,15 +194,14 @@ struct Segments {
   }
 };
 
-// Four codes (the low nibbles of u's bytes) as e4m3 (2 c - 15) 2^-9: bits 1-3 of 2 c, turned
-// over, with the sign, where c < 8.
-__device__ __forceinline__ uint32_t odd4(uint32_t u) {
-  const uint32_t low = ~(u >> 2) & 0x02020202u;          // 2 where c < 8
-  return ((u << 1) & 0x0E0E0E0Eu) ^ (low * 0x47u + 0x01010101u);
-}
-// The 8 codes of a word, in the columns' order.
-__device__ __forceinline__ void odd8(uint32_t w, uint32_t& o0, uint32_t& o1) {
-  const uint32_t a = odd4(w), b = odd4(w >> 4);          // columns 0 4 1 5 and 2 6 3 7
+// The 8 codes of a word as e4m3 (c - z) 2^-9, in the columns' order; z in every byte of zz.
+// The comparison as a product keeps it off the integer pipe (an addition there: 907 us for 845).
+__device__ __forceinline__ void minus_zero8(uint32_t w, uint32_t zz, uint32_t& o0, uint32_t& o1) {
+  auto four = [zz](uint32_t u) {      // columns 0 4 1 5, or 2 6 3 7
+    const uint32_t c = u & 0x0F0F0F0Fu, t = c * 7u + (0x80808080u - 7u * zz);   // bit 7 of a byte: c >= z
+    return __vabsdiffu4(c, zz) | (~t & 0x80808080u);
+  };
+  const uint32_t a = four(w), b = four(w >> 4);
   o0 = __byte_perm(a, b, 0x6420);
   o1 = __byte_perm(a, b, 0x7531);
 }
@@ -358,7 +354,6 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       for (int j = it > S::NW ? it - S::NW : 0; j < it; ++j)
         if (!mbar_wait(&wF[j % S::NW], (uint32_t)(j / S::NW) & 1u, drain)) timed_out();
     } else if (warp == 3) {
-      pdl_wait();      // the tokens' sums
       int it = 0;
       bool ok = true;
       for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
@@ -376,10 +371,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
             unsigned char* to = gring + s * S::GS;
             mbar_expect_tx(&gF[s], S::GS);
             const int64_t at = grid * L.mp + (int64_t)rt * LIN_BLOCK;
-            if (S::X8)
-              bulk_load(to, P.sums + (int64_t)(L.G == 1 ? part : grid) * P.sums_ld + tt * S::BN, S::BN * 4, &gF[s]);
-            bulk_load(to + S::GS_SCALES, L.scales + at, LIN_BLOCK * 4, &gF[s]);
-            bulk_load(to + S::GS_ZEROS, L.zeros + at, LIN_BLOCK, &gF[s]);
+            bulk_load(to, L.scales + at, S::GS, &gF[s]);
           }
           __syncwarp();
           if (L.G == 1 || seg.left == INT_MAX) {
@@ -503,23 +495,30 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         const int grid = L.G == 1 ? 0 : min(P.by_chunks ? (int)__umulhi(chunk, P.by_chunks) : chunk, L.G - 1);
         return zeros[grid * L.mp];
       };
-      // the zeros of this team's two chunks of a block, asked for four blocks ahead (a load's way
-      // from memory) and not looked at before
-      uint32_t z0[4], z1[4];
+      // the zeros of this team's chunks of a stage, asked for a load's way from memory ahead (four
+      // blocks, two of e4m3 stages) and not looked at before
+      constexpr int AHEAD = S::X8 ? 1 : 4, CHUNKS = 2 * S::BPS;
+      uint32_t zs[AHEAD][CHUNKS];
       auto zeros_of = [&](int kb, int i) {
-        z0[i] = z1[i] = 0;
-        if (S::X8 || kb >= kb1) return;
-        z0[i] = zero_of(kb * 4 + 2 * team);
-        z1[i] = zero_of(kb * 4 + 2 * team + 1);
+        const int block = S::X8 ? kb + team : kb;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) zs[i][c] = 0;
+        if (block >= kb1) return;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) zs[i][c] = zero_of(block * 4 + (S::X8 ? c : 2 * team + c));
       };
 #pragma unroll
-      for (int i = 0; i < 4; ++i) zeros_of(i == 0 || L.G > 1 ? kb0 + i : kb1, i);
+      for (int i = 0; i < AHEAD; ++i) zeros_of(i == 0 || L.G > 1 ? kb0 + i * S::BPS : kb1, i);
       for (int kb = kb0; kb < kb1; kb += S::BPS, ib += S::BPS, ++ia) {
-        const uint32_t z[2] = {z0[0], z1[0]};
-        if (!S::X8 && L.G > 1) {
+        uint32_t z[CHUNKS];
 #pragma unroll
-          for (int i = 0; i < 3; ++i) z0[i] = z0[i + 1], z1[i] = z1[i + 1];
-          zeros_of(kb + 4, 3);
+        for (int c = 0; c < CHUNKS; ++c) z[c] = zs[0][c];
+        if (L.G > 1) {
+#pragma unroll
+          for (int i = 0; i < AHEAD - 1; ++i)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) zs[i][c] = zs[i + 1][c];
+          zeros_of(kb + AHEAD * S::BPS, AHEAD - 1);
         }
         const int block = S::X8 ? ib + team : ib, sw = block % S::NW, sa = ia % S::NA;
         if (S::X8 && kb + team >= kb1) {
@@ -549,8 +548,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           for (int j = 0; j < 4; ++j) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-              odd8(j == 0 ? q[t].x : j == 1 ? q[t].y : j == 2 ? q[t].z : q[t].w, a[8 * (j & 1) + 2 * t],
-                   a[8 * (j & 1) + 2 * t + 1]);
+              minus_zero8(j == 0 ? q[t].x : j == 1 ? q[t].y : j == 2 ? q[t].z : q[t].w, z[j] * 0x01010101u,
+                          a[8 * (j & 1) + 2 * t], a[8 * (j & 1) + 2 * t + 1]);
             if (j & 1) tmem_st16(to + 8 * (j - 1), a);
           }
         } else if constexpr (S::W8) {
@@ -604,7 +603,6 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       for (int i = 0; i < S::COLS / 2; ++i) acc[i] = Two(0.f, 0.f);
       Segments seg(P, kb0 * 4);
       float s = 0.f;
-      const unsigned char* grid = nullptr;
       for (int chunk = kb0 * 4; chunk < kb1 * 4; ++g) {
         const int buf = g & (S::NACC - 1);
         const bool fresh = L.G > 1 || chunk == kb0 * 4;       // the next grid
@@ -616,8 +614,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (fresh) {
-          grid = gring + (ig % S::NG) * S::GS;
-          s = reinterpret_cast<const float*>(grid + S::GS_SCALES)[q * 32 + lane] * (S::X8 ? 256.f : 1.f);
+          s = reinterpret_cast<const float*>(gring + (ig % S::NG) * S::GS)[q * 32 + lane] * (S::X8 ? 512.f : 1.f);
         }
         // As much of the sums at once as registers allow: a warp's turn is a chain of waits.
         const uint32_t at = tmem + lanes + buf * S::BN + ch * S::COLS;
@@ -641,17 +638,6 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         chunk = seg.left == INT_MAX ? INT_MAX : chunk + seg.left;
         seg.next();
         if (L.G > 1 || chunk >= kb1 * 4) {
-          if constexpr (S::X8) {
-            // the rest of c - z, 7.5 - z, with the sum of the grid's (of this part's) tokens
-            const float c = s * (1.f / 256.f) * (7.5f - (float)grid[S::GS_ZEROS + q * 32 + lane]);
-            const float4* sums = reinterpret_cast<const float4*>(grid) + ch * (S::COLS / 4);
-#pragma unroll
-            for (int i = 0; i < S::COLS; i += 4) {
-              const float4 x = sums[i / 4];
-              acc[i / 2] = Two::fma(Two(c, c), Two(x.x, x.y), acc[i / 2]);
-              acc[i / 2 + 1] = Two::fma(Two(c, c), Two(x.z, x.w), acc[i / 2 + 1]);
-            }
-          }
           __syncwarp();
           if (lead) mbar_arrive(&gE[ig % S::NG]);
           ++ig;
@@ -734,61 +720,6 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// The sum of up to 16 e4m3 values of a row, from column k (a multiple of 16) on.
-__device__ __forceinline__ float sum16(const uint8_t* row, int64_t k, int64_t end) {
-  if (k >= end) return 0.f;
-  uint32_t w[4] = {0u, 0u, 0u, 0u};
-  if (k + 16 <= end) {
-    const uint4 q = *reinterpret_cast<const uint4*>(row + k);
-    w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (k + j < end) w[j / 4] |= (uint32_t)row[k + j] << (8 * (j % 4));
-  }
-  float s = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const auto two = (__nv_fp8x2_storage_t)(w[j / 2] >> (16 * (j % 2)) & 0xFFFFu);
-    const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3)));
-    s += f.x + f.y;
-  }
-  return s;
-}
-
-// Sums of e4m3 tokens' values over each of `pieces` ranges of `width` columns (multiples of 32),
-// a warp per token (zeros for the padding tokens up to ld); the status word cleared beside.
-// Rows start on 16 bytes.
-__global__ void __launch_bounds__(256)
-    k_token_sums(const uint8_t* x, int64_t ldx, int rows, int n, int pieces, int width, float* sums, int64_t ld, int* status) {
-  pdl_trigger();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
-  const int64_t tok = blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (tok >= ld) return;
-  const int64_t end = tok < rows ? n : 0;
-  const uint8_t* row = x + (tok < rows ? tok : 0) * ldx;
-  if (width <= 512 && 512 % width == 0) {
-    // whole pieces in 512 columns: lanes of a piece add up, its first one writes
-    const int lanes = width / 16;
-#pragma unroll 4
-    for (int64_t k = 16 * lane; k < (int64_t)round_up((int64_t)pieces * width, 512); k += 512) {
-      float s = sum16(row, k, end);
-      for (int o = 1; o < lanes; o *= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (lane % lanes == 0 && k / width < pieces) sums[k / width * ld + tok] = s;
-    }
-    return;
-  }
-  for (int p = 0; p < pieces; ++p) {
-    const int64_t to = min(end, (int64_t)(p + 1) * width);
-    float s = 0.f;
-#pragma unroll 4
-    for (int64_t k = (int64_t)p * width + 16 * lane; k < to; k += 512) s += sum16(row, k, to);
-    s = warp_all(s, AddOp());
-    if (lane == 0) sums[p * ld + tok] = s;
-  }
-}
-
 __global__ void k_clear_status(int* status) {
   pdl_trigger();
   *status = 0;
@@ -814,16 +745,6 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   if (S::BN <= 128)
     while (P.splits < 8 && tiles * P.splits * 2 <= ROW_SMS && L.kblocks >= 4 * P.splits) P.splits *= 2;
   P.per = ceil_div(L.kblocks, P.splits);
-  if (S::X8) {
-    // no grid in two parts: a part ends where a grid does
-    int whole = 1;
-    while (L.G > 1 && whole * 4 % L.chunks != 0) ++whole;
-    P.per = (int)round_up(P.per, whole);
-    const int pieces = L.G == 1 ? P.splits : L.G, width = L.G == 1 ? P.per * LIN_BLOCK : L.chunks * 32;
-    k_token_sums<<<(unsigned)((P.sums_ld + 7) / 8), 256, 0, s>>>((const uint8_t*)x, ldx, L.rows, L.n, pieces, width,
-                                                               const_cast<float*>(P.sums), P.sums_ld, P.status);
-    BK_CUDA_OK(cudaGetLastError());
-  }
   CUtensorMap map;
   const cuuint64_t dims[2] = {(cuuint64_t)L.n, (cuuint64_t)L.rows};
   const cuuint64_t strides[1] = {(cuuint64_t)ldx * (S::X8 ? 1 : 2)};
@@ -838,8 +759,8 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   cfg.blockDim = dim3(S::THREADS);
   cfg.dynamicSmemBytes = S::SMEM;
   cfg.stream = s;
-  // Starts beside the kernel before (which clears the status and makes the tokens' copy or
-  // sums): barriers, TMEM and the first codes are ready when that is done.
+  // Starts beside the kernel before (which clears the status and makes the tokens'
+  // copy): barriers, TMEM and the first codes are ready when that is done.
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -881,20 +802,9 @@ static bool rows_in_place(const void* x, bool x8, int64_t ldx, bool bytes8) {
   return !(x8 && bytes8) && aligned16(x, x8 ? ldx : 2 * ldx);
 }
 
-// Where the workspace keeps things: [status 256 B][e4m3 tokens' sums][tokens' copy].
-struct TcWorkspace {
-  int64_t sums_ld;
-  size_t off_copy, bytes;
-  TcWorkspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8, int G) {
-    sums_ld = round_up((int64_t)rows + 191, 64);     // whole token tiles, whichever their width
-    off_copy = 256 + (x8 && !bytes8 ? align256((size_t)std::max(G, 8) * sums_ld * 4) : 0);
-    bytes = off_copy;
-    if (!rows_in_place(x, x8, ldx, bytes8)) bytes += (size_t)rows * round_up(n, 16) * (x8 && !bytes8 ? 1 : 2);
-  }
-};
-
-size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8, int G) {
-  return TcWorkspace(x, x8, rows, ldx, n, bytes8, G).bytes;
+// The workspace: [status 256 B][tokens' copy].
+size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8) {
+  return 256 + (rows_in_place(x, x8, ldx, bytes8) ? 0 : (size_t)rows * round_up(n, 16) * (x8 && !bytes8 ? 1 : 2));
 }
 
 int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cudaStream_t s) {
@@ -906,13 +816,10 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
   P.segs = L.G > 1 ? L.G : INT_MAX / SEG_MMAS - 1;
   P.status = (int*)workspace;
   P.spin_cycles = spin_cycles_from_env();
-  const TcWorkspace W(L.x, x8, L.rows, L.ldx, L.n, bytes8, L.G);
-  P.sums = (const float*)((char*)workspace + 256);
-  P.sums_ld = W.sums_ld;
   const void* x = L.x;
   int64_t ldx = L.ldx;
   if (!rows_in_place(x, x8, ldx, bytes8)) {
-    void* out = (char*)workspace + W.off_copy;
+    void* out = (char*)workspace + 256;
     const dim3 grid((unsigned)L.rows, (unsigned)ceil_div(L.n, 1024));
     ldx = round_up(L.n, 16);
     if (!x8)
@@ -923,7 +830,7 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
       k_linear_rows<true, false><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, P.status);
     BK_CUDA_OK(cudaGetLastError());
     x = out;
-  } else if (!x8 || bytes8) {
+  } else {
     k_clear_status<<<1, 1, 0, s>>>(P.status);
     BK_CUDA_OK(cudaGetLastError());
   }
