@@ -496,7 +496,8 @@ typedef enum {
   BAKRON_RELU = 1,   /* max(v, 0) */
   BAKRON_SILU = 2,   /* v / (1 + exp(-v)) */
   BAKRON_GELU = 3    /* v (1 + erf(v / sqrt(2))) / 2 */
-} bakron_activation;
+} bakron_activation;  /* fp32 results: within (v^2 + 8) 2^-23 of themselves; bf16 results come from
+                         an erf within 1.5e-7, and a logistic function within (2 + |v|) 2^-21 */
 
 /*
  * bakron_linear -- y = act(x What^T + bias) + residual for `rows` tokens, What the m x n

@@ -65,8 +65,8 @@ struct LinearParams {
   int yvec;                 // y and the residual 16 bytes at a time, from columns that are multiples of 8
 };
 
-// erf to 1.5e-7 (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26).  An fp32
-// erf of the usual accuracy cost the epilogue of a 4096 x 28672 product 100 us.
+// erf to 1.5e-7 (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26), for bf16
+// results: erff cost the epilogue of a 4096 x 28672 product 100 us, erfcf in an fp32 one 150 (846 -> 996).
 __device__ __forceinline__ float erf_short(float v) {
   const float x = fabsf(v), t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
   float p = fmaf(1.061405429f, t, -1.453152027f);
@@ -76,31 +76,40 @@ __device__ __forceinline__ float erf_short(float v) {
   return copysignf(fmaf(-p, __expf(-x * x), 1.f), v);
 }
 
+// EXACT: for fp32 results, right but for a few of their last bits (erfc, as 1 + erf cancels where
+// v is negative).  Else for results that are rounded to bf16: what the short forms lose is far
+// below its 2^-9, but for GELU's tail (below -4, where it errs by up to 1e-7 |v|).
+template <bool EXACT>
 __device__ __forceinline__ float activate(float v, int a) {
   switch (a) {
-    case BAKRON_RELU: return v < 0.f ? 0.f : v;                  // NaN stays
-    case BAKRON_SILU: return __fdividef(v, 1.f + __expf(-v));    // the divisor's overflow gives 0, as it should
-    case BAKRON_GELU: return 0.5f * v * (1.f + erf_short(v * 0.70710678f));
+    case BAKRON_RELU: return v < 0.f ? 0.f : v;     // NaN stays
+    case BAKRON_SILU:      // the divisor's overflow gives 0, as it should
+      return EXACT ? v / (1.f + expf(-v)) : __fdividef(v, 1.f + __expf(-v));
+    case BAKRON_GELU:
+      return EXACT ? 0.5f * v * erfcf(v * -0.70710678f) : 0.5f * v * (1.f + erf_short(v * 0.70710678f));
     default: return v;
   }
 }
+__host__ __device__ __forceinline__ bool exact_activation(const LinearParams& P) {
+  return P.yf32 && P.activation >= BAKRON_SILU;
+}
 
-// What follows the product's sum for one entry, up to its store.
-__device__ __forceinline__ float linear_out(const LinearParams& P, float v, int64_t tok, int row) {
+// One entry from the product's sum to its store.
+template <bool EXACT>
+__device__ __forceinline__ void linear_store(const LinearParams& P, float v, int64_t tok, int row) {
   if (P.xscales) v *= P.xscales[tok];
   if (P.bias) v += P.bias[row];
-  v = activate(v, P.activation);
+  v = activate<EXACT>(v, P.activation);
   if (P.residual)
     v += P.yf32 ? ((const float*)P.residual)[tok * P.ldr + row]
                 : __bfloat162float(((const __nv_bfloat16*)P.residual)[tok * P.ldr + row]);
-  return v;
-}
-__device__ __forceinline__ void linear_store(const LinearParams& P, float v, int64_t tok, int row) {
-  v = linear_out(P, v, tok, row);
   if (P.yf32)
     ((float*)P.y)[tok * P.ldy + row] = v;
   else
     ((__nv_bfloat16*)P.y)[tok * P.ldy + row] = __float2bfloat16_rn(v);
+}
+__device__ __forceinline__ void linear_store(const LinearParams& P, float v, int64_t tok, int row) {
+  exact_activation(P) ? linear_store<true>(P, v, tok, row) : linear_store<false>(P, v, tok, row);
 }
 
 // Two codes of a pair as bf16 values c - z, exact: integers up to 255.

@@ -207,13 +207,14 @@ __device__ __forceinline__ void minus_zero8(uint32_t w, uint32_t zz, uint32_t& o
 }
 
 // 8 neighbouring rows' sums of one token (16-byte aligned in shared memory): epilogue and store.
+template <bool EXACT>
 __device__ __forceinline__ void linear_store8(const LinearParams& L, const float* sums, int64_t tok, int row0) {
   float v[8], r[8];
   load8(sums, v);
   if (row0 + 8 > L.m || !L.yvec) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (row0 + i < L.m) linear_store(L, v[i], tok, row0 + i);
+      if (row0 + i < L.m) linear_store<EXACT>(L, v[i], tok, row0 + i);
     return;
   }
   const float xs = L.xscales ? L.xscales[tok] : 1.f;
@@ -221,7 +222,7 @@ __device__ __forceinline__ void linear_store8(const LinearParams& L, const float
   for (int i = 0; i < 8; ++i) {
     v[i] *= xs;
     if (L.bias) v[i] += L.bias[row0 + i];
-    v[i] = activate(v[i], L.activation);
+    v[i] = activate<EXACT>(v[i], L.activation);
   }
   if (L.residual) {
     if (L.yf32)
@@ -237,7 +238,9 @@ __device__ __forceinline__ void linear_store8(const LinearParams& L, const float
     store8((__nv_bfloat16*)L.y + tok * L.ldy + row0, v);
 }
 
-template <class S>
+// EXACT: with the activations that fp32 results want.  A kernel of its own: beside the short
+// ones in one kernel they cost every call 8 to 12% (4096 x 28672 x 8192 in bf16 1.25 -> 1.35 ms).
+template <class S, bool EXACT>
 __global__ void __launch_bounds__(S::THREADS, 1)
     k_linear_tc(const __grid_constant__ CUtensorMap xmap, const TcParams P) {
   extern __shared__ __align__(1024) unsigned char tc_smem[];
@@ -666,7 +669,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
             }
           __syncwarp();
           const int64_t tok = (int64_t)tt * S::BN + ch * S::COLS + b * 8 + (lane >> 2);
-          if (tok < L.rows) linear_store8(L, mine + (lane >> 2) * STAGE_LD + (lane & 3) * 8, tok, row0);
+          if (tok < L.rows) linear_store8<EXACT>(L, mine + (lane >> 2) * STAGE_LD + (lane & 3) * 8, tok, row0);
         }
       }
     }
@@ -685,7 +688,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         float v = 0.f;
         for (int p = 0; p < P.splits; ++p)
           v += cluster.map_shared_rank(mine, p)[t * 128 + (threadIdx.x & 127)];
-        if (row < L.m) linear_store(L, v, tok, row);
+        if (row < L.m) linear_store<EXACT>(L, v, tok, row);
       }
       cluster.sync();          // nobody's shared memory goes before it is read
     }
@@ -725,17 +728,17 @@ __global__ void k_clear_status(int* status) {
   *status = 0;
 }
 
-template <class S>
+template <class S, bool EXACT>
 int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   static OncePerDevice once;
   BK_CUDA_OK(once([] {
     cudaFuncAttributes a;
-    cudaError_t e = cudaFuncGetAttributes(&a, k_linear_tc<S>);
+    cudaError_t e = cudaFuncGetAttributes(&a, k_linear_tc<S, EXACT>);
     // the warpgroups' shares (setmaxnreg) are taken from what the block is launched with
     if (e == cudaSuccess && S::SPLIT_REGS && a.numRegs != S::LAUNCH_REGS) e = cudaErrorInvalidConfiguration;
     return e != cudaSuccess
                ? e
-               : cudaFuncSetAttribute(k_linear_tc<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
+               : cudaFuncSetAttribute(k_linear_tc<S, EXACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
   }));
   const LinearParams& L = P.L;
   P.token_tiles = ceil_div(L.rows, S::BN);
@@ -769,11 +772,11 @@ int launch_tc(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = P.splits > 1 ? 2 : 1;
-  BK_CUDA_OK(cudaLaunchKernelEx(&cfg, k_linear_tc<S>, map, P));
+  BK_CUDA_OK(cudaLaunchKernelEx(&cfg, k_linear_tc<S, EXACT>, map, P));
   return BAKRON_OK;
 }
 
-template <bool W8, bool X8>
+template <bool W8, bool X8, bool EXACT>
 int launch_bn(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
   // The token tile with the shortest schedule: rounds of tiles over the SMs, a tile costing
   // its tokens and about 32 more (expanding the codes, the way out).
@@ -788,10 +791,10 @@ int launch_bn(const void* x, int64_t ldx, TcParams& P, cudaStream_t s) {
     }
   }
   switch (best) {
-    case 192: return launch_tc<TcShape<192, W8, X8>>(x, ldx, P, s);
-    case 128: return launch_tc<TcShape<128, W8, X8>>(x, ldx, P, s);
-    case 64: return launch_tc<TcShape<64, W8, X8>>(x, ldx, P, s);
-    default: return launch_tc<TcShape<32, W8, X8>>(x, ldx, P, s);
+    case 192: return launch_tc<TcShape<192, W8, X8>, EXACT>(x, ldx, P, s);
+    case 128: return launch_tc<TcShape<128, W8, X8>, EXACT>(x, ldx, P, s);
+    case 64: return launch_tc<TcShape<64, W8, X8>, EXACT>(x, ldx, P, s);
+    default: return launch_tc<TcShape<32, W8, X8>, EXACT>(x, ldx, P, s);
   }
 }
 
@@ -834,8 +837,10 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
     k_clear_status<<<1, 1, 0, s>>>(P.status);
     BK_CUDA_OK(cudaGetLastError());
   }
-  if (bytes8) return launch_bn<true, false>(x, ldx, P, s);
-  return x8 ? launch_bn<false, true>(x, ldx, P, s) : launch_bn<false, false>(x, ldx, P, s);
+  const bool exact = exact_activation(L);
+  if (bytes8) return exact ? launch_bn<true, false, true>(x, ldx, P, s) : launch_bn<true, false, false>(x, ldx, P, s);
+  if (x8) return exact ? launch_bn<false, true, true>(x, ldx, P, s) : launch_bn<false, true, false>(x, ldx, P, s);
+  return exact ? launch_bn<false, false, true>(x, ldx, P, s) : launch_bn<false, false, false>(x, ldx, P, s);
 }
 
 }  // namespace bakron
