@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(MAXT) k_rmsnorm_back(const NormBackParams P) {
       ss += s.x;
       c += s.y;
     }
-    const float rho = rsqrtf(ss / (float)P.d + P.eps), k = rho * rho * (c / (float)P.d);
+    const float rho = 1.f / sqrtf(ss / (float)P.d + P.eps), k = rho * rho * (c / (float)P.d);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       float a[8], b[8], w[8], o[8];
