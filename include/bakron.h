@@ -512,7 +512,8 @@ typedef enum {
  *   y        device, rows x m, BAKRON_BF16 or BAKRON_F32, row stride ldy (>= m); must not
  *            overlap x
  *   workspace device, >= bakron_linear_workspace_bytes(...) bytes, 16-byte aligned (may
- *            be NULL where that is 0); its first word is the status
+ *            be NULL where that is 0); where there is one, its first word is the status of
+ *            this call
  *   sync     nonzero: synchronise `stream` and return the device status
  *            (BAKRON_ERR_TIMEOUT: a bounded wait ran out, y is undefined); zero:
  *            bakron_read_status(workspace, stream) returns it later, where there is one

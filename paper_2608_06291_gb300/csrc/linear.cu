@@ -147,6 +147,7 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, W8 ? 3 - NT : 4 - NT) k_linear
   __shared__ float red[FEW_WARPS][8 * NT][FEW_ROWS + 1];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int64_t row0 = (int64_t)blockIdx.x * FEW_ROWS, tok0 = (int64_t)blockIdx.y * 8 * NT;
+  if (P.status && blockIdx.x + blockIdx.y + threadIdx.x == 0) *P.status = 0;      // nothing here can run out
   const unsigned char* base = P.codes + (row0 / LIN_BLOCK) * P.kblocks * (4 * UW) * 2048 +
                               (row0 % LIN_BLOCK + g) * 16 + t * 2048;
   float acc[2][NT][4] = {}, cur[2][NT][4] = {};
@@ -334,6 +335,7 @@ extern "C" int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, c
   P.xvec = x8 ? ((uintptr_t)x | (uintptr_t)step) % 8 == 0 : aligned16(x, step * 2);
   const int ys = P.yf32 ? 4 : 2;
   P.yvec = aligned16(y, ldy * ys) && (!residual || aligned16(residual, ldr * ys));
+  if (workspace && workspace_bytes >= sizeof(int) && (uintptr_t)workspace % 16 == 0) P.status = (int*)workspace;
   cudaStream_t s = (cudaStream_t)stream;
   if (rows > FEW_TOKENS) {
     const int rc = linear_tc(P, x8, L.bytes8, workspace, s);

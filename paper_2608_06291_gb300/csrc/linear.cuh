@@ -63,6 +63,7 @@ struct LinearParams {
   int activation, yf32;
   int xvec;                 // x can be read 8 elements at a time
   int yvec;                 // y and the residual 16 bytes at a time, from columns that are multiples of 8
+  int* status;              // the call's status word, or null
 };
 
 // erf to 1.5e-7 (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26), for bf16

@@ -86,7 +86,6 @@ struct TcParams {
   int row_tiles, token_tiles, splits, per;   // per: 128-column blocks of a split's part
   uint32_t by_chunks;     // 2^32 / (chunks of a grid), rounded up: chunk / chunks by a product; 0 for 1
   int seg_chunks, segs;   // chunks of a segment; how many there are (the last takes the rest)
-  int* status;
   long long spin_cycles;
 };
 
@@ -293,7 +292,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
   };
   auto timed_out = [&]() {
     pdl_wait();        // the status is cleared by the kernel before
-    if (!*abort_flag) raise_status(P.status, BAKRON_ERR_TIMEOUT);
+    if (!*abort_flag) raise_status(P.L.status, BAKRON_ERR_TIMEOUT);
     *abort_flag = 1;
   };
   auto wait2 = [&](uint64_t* bar, uint32_t parity, uint64_t* bar2, uint32_t parity2) {      // a warp
@@ -817,7 +816,6 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
   P.by_chunks = L.chunks > 1 ? (uint32_t)((((uint64_t)1 << 32) + L.chunks - 1) / L.chunks) : 0;
   P.seg_chunks = L.G > 1 ? L.chunks : x8 && !bytes8 ? SEG_MMAS : SEG_MMAS / 2;
   P.segs = L.G > 1 ? L.G : INT_MAX / SEG_MMAS - 1;
-  P.status = (int*)workspace;
   P.spin_cycles = spin_cycles_from_env();
   const void* x = L.x;
   int64_t ldx = L.ldx;
@@ -826,15 +824,15 @@ int linear_tc(const LinearParams& L, bool x8, bool bytes8, void* workspace, cuda
     const dim3 grid((unsigned)L.rows, (unsigned)ceil_div(L.n, 1024));
     ldx = round_up(L.n, 16);
     if (!x8)
-      k_linear_rows<false, false><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, P.status);
+      k_linear_rows<false, false><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, L.status);
     else if (bytes8)
-      k_linear_rows<true, true><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, P.status);
+      k_linear_rows<true, true><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, L.status);
     else
-      k_linear_rows<true, false><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, P.status);
+      k_linear_rows<true, false><<<grid, 256, 0, s>>>(x, L.ldx, L.n, out, ldx, L.status);
     BK_CUDA_OK(cudaGetLastError());
     x = out;
   } else {
-    k_clear_status<<<1, 1, 0, s>>>(P.status);
+    k_clear_status<<<1, 1, 0, s>>>(L.status);
     BK_CUDA_OK(cudaGetLastError());
   }
   const bool exact = exact_activation(L);
