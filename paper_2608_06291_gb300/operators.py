@@ -160,12 +160,15 @@ def bakron_linear(x, weight: PackedWeight, x_scales=None, bias=None, activation=
         ldy = _result(out, yshape, "out", out_dtype, dev)
     L = lib()
     px, dt = x.data_ptr(), _DTYPES[x.dtype]
-    if workspace is None:
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on cuda:{dev}")
+    else:
         size = L.bakron_linear_workspace_bytes(px, dt, rows, ldx, n, weight.qmax, weight.group_size)
         if size:
             workspace = _empty(size, dtype=torch.uint8, device=dev)
     if workspace is not None:
-        ws, size = workspace.data_ptr(), workspace.numel()
+        ws, size = workspace.data_ptr(), workspace.nbytes
     rc = L.bakron_linear(px, dt, rows, ldx, xs, weight.buf.data_ptr(), m, n, weight.qmax, weight.group_size, b, act, r,
                          ldr, out.data_ptr(), _DTYPES[out_dtype], ldy, ws, size, 1 if sync else 0,
                          _raw_stream(dev))
