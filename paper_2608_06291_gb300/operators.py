@@ -18,6 +18,7 @@ _F32, _BF16, _E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
 _DTYPES = {_F32: F32, _BF16: BF16, _E4M3: E4M3}
 _ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 _empty = torch.empty
+_MOST = 2 ** 31 - 1
 
 try:     # the stream's handle without a Stream object around it
     from torch._C import _cuda_getCurrentRawStream as _raw_stream
@@ -36,9 +37,11 @@ def _rows(t, name, dtypes, device):
         raise ValueError(f"{name} must be {_names(dtypes)}")
     if t.get_device() != device or device < 0:
         raise ValueError(f"{name} must be a CUDA tensor" + (f" on cuda:{device}" if device >= 0 else ""))
-    d = t.shape[-1]
+    d, count = t.shape[-1], t.numel()
+    if count > _MOST and max(d, count // d) > _MOST:     # counts are 32-bit integers below
+        raise ValueError(f"{name} must have at most 2^31 - 1 rows and columns")
     if t.is_contiguous():
-        return t, t.numel() // d if d else 0, d
+        return t, count // d if d else 0, d
     t = t.reshape(-1, d)
     if t.stride(1) != 1 and d > 1 or t.shape[0] > 1 and t.stride(0) < d:
         t = t.contiguous()
