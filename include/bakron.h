@@ -564,7 +564,8 @@ int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t
                             float* dw, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * bakron_token_logprobs -- of each row of logits l (rows x v, BAKRON_F32 or BAKRON_BF16):
+ * bakron_token_logprobs -- of each row of logits l (rows x v, BAKRON_F32 or BAKRON_BF16, v at
+ * most 2^31 - 1024):
  *   lse      rows fp32: log sum_j exp(l_j)
  *   logp     rows fp32: l[target] - lse; 0 where the target is outside 0..v-1 (a position
  *            that is not scored); NULL if targets is NULL

@@ -28,6 +28,7 @@ namespace bakron {
 namespace {
 
 constexpr int TOP_MAX = 32;
+constexpr int V_MAX = INT_MAX - 1023;  // an index, or a row's end rounded up to a tile, passes no 32 bits
 constexpr float LSE_EXACT = 1024.f;   // up to here lse's rounding is below 2^-14
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr double LN2 = 0.6931471805599453;
@@ -570,7 +571,7 @@ using namespace bakron;
 extern "C" int bakron_token_logprobs(const void* logits, int dtype, int rows, int v, int64_t ldl,
                                      const int64_t* targets, int top, float* logp, float* entropy,
                                      float* lse, float* top_logp, int* top_ids, void* stream) {
-  if ((dtype != BAKRON_F32 && dtype != BAKRON_BF16) || rows < 0 || v < 1 || top < 0 || top > TOP_MAX ||
+  if ((dtype != BAKRON_F32 && dtype != BAKRON_BF16) || rows < 0 || v < 1 || v > V_MAX || top < 0 || top > TOP_MAX ||
       top > v || (targets != nullptr) != (logp != nullptr))
     return BAKRON_ERR_INVALID_ARG;
   if (rows == 0) return BAKRON_OK;
@@ -590,7 +591,7 @@ extern "C" int bakron_token_logprobs_backward(const void* logits, int dtype, int
                                               const float* dlogp, const float* entropy,
                                               const float* dentropy, void* dlogits, int64_t ldd,
                                               void* stream) {
-  if ((dtype != BAKRON_F32 && dtype != BAKRON_BF16) || rows < 0 || v < 1) return BAKRON_ERR_INVALID_ARG;
+  if ((dtype != BAKRON_F32 && dtype != BAKRON_BF16) || rows < 0 || v < 1 || v > V_MAX) return BAKRON_ERR_INVALID_ARG;
   if (rows == 0) return BAKRON_OK;
   if (!logits || !lse || !dlogits || ldl < v || ldd < v || (!dlogp && !dentropy) ||
       (dlogp && !targets) || (dentropy && !entropy))
