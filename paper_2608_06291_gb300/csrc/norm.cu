@@ -461,7 +461,8 @@ __global__ void __launch_bounds__(256) k_rmsnorm_dw(const NormBackParams P) {
   P.part[(int64_t)blockIdx.y * P.d + e] = s;
 }
 
-// dw = the parts' sum, always in the same order: 32 columns a CTA, 32 ranges of parts.
+// dw = the parts' sum, always in the same order: 32 columns a CTA, 32 ranges of parts, whose
+// sums a warp joins pairwise (one after another they were the largest part of dw's error).
 __global__ void __launch_bounds__(1024) k_sum_parts(const float* part, int parts, int d, float* dw) {
   __shared__ float s[32][33];
   const int c = blockIdx.x * 32 + threadIdx.x;
@@ -471,12 +472,9 @@ __global__ void __launch_bounds__(1024) k_sum_parts(const float* part, int parts
     for (int p = threadIdx.y; p < parts; p += 32) v += part[(int64_t)p * d + c];
   s[threadIdx.y][threadIdx.x] = v;
   __syncthreads();
-  if (threadIdx.y == 0 && c < d) {
-    float t = 0.f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) t += s[i][threadIdx.x];
-    dw[c] = t;
-  }
+  v = warp_all(s[threadIdx.x][threadIdx.y], AddOp());
+  const int at = blockIdx.x * 32 + threadIdx.y;
+  if (threadIdx.x == 0 && at < d) dw[at] = v;
 }
 
 // Threads of a CTA (0: rows too long), and CTAs, each with its part of dw: what an SM holds.
