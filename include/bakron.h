@@ -538,8 +538,10 @@ int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float*
  *   scales   device, `rows` fp32: max |y| / 448 of the row (1 where that is 0); y then
  *            holds y / scale, rounded to nearest
  *   d        1..65536
- * All in fp32; y comes from the unrounded h.  A row that holds a NaN or an infinity
- * gives NaNs (in 8 bits: a NaN scale).
+ * All in fp32; y comes from the unrounded h.  A row that holds a NaN gives NaNs.  One that
+ * holds an infinity has an infinite mean: y is NaN at the infinity and 0 elsewhere.  In 8 bits
+ * either gives a NaN scale and NaNs.  A sum of squares beyond fp32's largest number (entries of
+ * some 1e19) counts as infinite too: y is 0.
  */
 int bakron_rmsnorm(const void* x, int dtype, int rows, int d, int64_t ldx,
                    const void* residual, int64_t ldr, const void* weight, int wdtype,
