@@ -138,9 +138,11 @@ constexpr int FEW_WARPS = 8;     // they share its columns, block by block
 
 // 32 rows x 8 NT tokens per CTA.  What's rows are the rows of mma.sync's first operand,
 // read straight from the packed units into its registers; the tokens are its columns.
-// Bound by the codes' way from memory and, per call, by the launch: 1 token x 28672 x 8192,
-// 118 MB of codes, 47 us (2.5 TB/s); 1 x 4096 x 4096 13 us a call.  CTAs an SM as registers
-// allow (two of 16 tokens x 8-bit codes spill: 29 us for 4099 x 11008, one 25).
+// Bound by its waits, not by memory (1 token x 8192 x 8192 in groups of 128: 28 us, DRAM 16% busy,
+// issue 34%): a new grid's scales and zeros and a block's tokens are loaded where they are
+// used, and codes are only one block ahead.  As graph replays: 1 x 28672 x 8192, 118 MB of codes, 58 us
+// in groups of 128 (2.2 TB/s with the grids), 41 with one grid a row; 1 x 4096 x 4096 10.  CTAs
+// an SM as registers allow (two of 16 tokens x 8-bit codes spill: 29 us for 4099 x 11008, one 25).
 template <int NT, bool W8, bool X8>
 __global__ void __launch_bounds__(FEW_WARPS * 32, W8 ? 3 - NT : 4 - NT) k_linear_few(const LinearParams P) {
   constexpr int UW = W8 ? 2 : 1;     // units of a row a lane reads per block

@@ -2,6 +2,9 @@
 the product with a quantised weight, the root-mean-square norm, the log
 probabilities of given tokens, and the gradients of the last two.
 
+Results carry no autograd graph, whatever their inputs ask for: a training step calls the
+``*_backward`` operators itself, and the product has none.
+
 Tensors may have any number of leading dimensions where their rows are evenly
 spaced (or else are copied); the last dimension is contiguous.  Work is enqueued on
 ``stream`` (default: the current one), and what a call allocates or copies belongs to it.
