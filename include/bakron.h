@@ -599,6 +599,49 @@ int bakron_token_logprobs_backward(const void* logits, int dtype, int rows, int 
                                    const float* dentropy, void* dlogits, int64_t ldd,
                                    void* stream);
 
+/*
+ * bakron_head_logprobs -- bakron_token_logprobs of the logits l = h W^T, which are not kept:
+ *   h        device, rows (at most 2^24) x d (at most 65536) BAKRON_BF16 values, row stride ldh (>= d)
+ *   weight   device, v (at most 2^24) x d BAKRON_BF16 values, row stride ldw (>= d)
+ *   targets, logp, entropy, lse  as for bakron_token_logprobs (logp is given where targets are)
+ *   workspace device, >= bakron_head_logprobs_workspace_bytes(...) bytes, 16-byte aligned; its
+ *            first word is the status of this call
+ *   sync     as for bakron_linear
+ * Products of bf16 values are exact and their sums fp32.  Rows and matrices that start on 16 bytes
+ * (base and stride) are read as they lie; others are copied into the workspace first.  A row of h
+ * that holds a NaN or an infinity affects its own results alone (they are then no finite numbers).
+ */
+size_t bakron_head_logprobs_workspace_bytes(const void* h, int64_t ldh, const void* weight,
+                                            int64_t ldw, int rows, int v, int d);
+int bakron_head_logprobs(const void* h, int64_t ldh, const void* weight, int64_t ldw, int rows,
+                         int v, int d, const int64_t* targets, float* logp, float* entropy,
+                         float* lse, void* workspace, size_t workspace_bytes, int sync,
+                         void* stream);
+
+/*
+ * bakron_head_logprobs_backward -- the gradients of sum_t (dlogp_t logp_t + dentropy_t entropy_t)
+ * at h and at the weight: dh = G W, dW = G^T h, with G as bakron_token_logprobs_backward gives it
+ * (formed again, a piece of the vocabulary at a time).
+ *   lse, entropy, dlogp, dentropy, targets  as for bakron_token_logprobs_backward
+ *   dh       device, rows x d BAKRON_BF16, row stride lddh (>= d); must not overlap h or weight
+ *   dweight  device, v x d BAKRON_BF16, row stride lddw (>= d), or NULL: not wanted; must not
+ *            overlap h or weight.  Zeros for no rows
+ *   workspace device, >= bakron_head_logprobs_backward_workspace_bytes(...) bytes (weight_grad:
+ *            whether dweight is given), 16-byte aligned; its first word is the status of this call
+ *   sync     as for bakron_linear
+ * G's entries are rounded to bf16 but for each token's own target, which stays in fp32; sums are
+ * fp32, in a fixed order, and each result is rounded once.
+ */
+size_t bakron_head_logprobs_backward_workspace_bytes(const void* h, int64_t ldh,
+                                                     const void* weight, int64_t ldw, int rows,
+                                                     int v, int d, int weight_grad);
+int bakron_head_logprobs_backward(const void* h, int64_t ldh, const void* weight, int64_t ldw,
+                                  int rows, int v, int d, const int64_t* targets,
+                                  const float* lse, const float* dlogp, const float* entropy,
+                                  const float* dentropy, void* dh, int64_t lddh, void* dweight,
+                                  int64_t lddw, void* workspace, size_t workspace_bytes, int sync,
+                                  void* stream);
+
 /* Static description of a status code. */
 const char* bakron_strerror(int status);
 

@@ -132,6 +132,15 @@ def lib() -> ctypes.CDLL:
     L.bakron_rmsnorm_backward.restype = i32
     L.bakron_token_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp]
     L.bakron_token_logprobs.restype = i32
+    L.bakron_head_logprobs_workspace_bytes.argtypes = [vp, i64, vp, i64, i32, i32, i32]
+    L.bakron_head_logprobs_workspace_bytes.restype = sz
+    L.bakron_head_logprobs.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, sz, i32, vp]
+    L.bakron_head_logprobs.restype = i32
+    L.bakron_head_logprobs_backward_workspace_bytes.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32]
+    L.bakron_head_logprobs_backward_workspace_bytes.restype = sz
+    L.bakron_head_logprobs_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64,
+                                                vp, sz, i32, vp]
+    L.bakron_head_logprobs_backward.restype = i32
     L.bakron_token_logprobs_backward.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     L.bakron_token_logprobs_backward.restype = i32
     L.bakron_strerror.argtypes = [i32]

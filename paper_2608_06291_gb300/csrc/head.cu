@@ -1,0 +1,515 @@
+// bakron_head_logprobs and bakron_head_logprobs_backward: log probabilities of given tokens
+// from hidden states h (t x d) and the head's weight W (v x d), and the gradients at both,
+// without the t x v logits.
+//
+//   l = h W^T,  lse = log sum_j exp l_j,  logp = l[target] - lse,  entropy = lse - sum_j p_j l_j
+//   G_tj = dlogp ([j = target] - p_tj) - dentropy p_tj (log p_tj + entropy)
+//   dh = G W,  dW = G^T h
+//
+// Forward: the tiles of h W^T end in the tensor cores' accumulators, and only each row's
+// maximum, its sum of exponentials and that sum weighted with the logits leave them, one
+// triple per row and half tile; a second kernel joins the triples in a fixed order.
+//
+// Backward: the vocabulary goes in pieces.  A piece's logits are formed again, G of the
+// piece is written in bf16 and multiplied by W's rows of the piece (a sum over pieces, in
+// fp32) and by h (the piece's rows of dW).  A token's own target is no part of that bf16 G: its
+// entry, often as large as all the others together and much the same from token to token, would bring its
+// rounding to dh and dW.  It is kept in fp32 and joins the fp32 sums as a multiple of W's
+// (h's) row.
+#include <algorithm>
+
+#include "pair_gemm.cuh"
+
+namespace bakron {
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LOWEST = -1e38f;      // stands for -inf, so that differences stay finite
+constexpr int NO_TOKEN = 0x7fffffff;
+
+__device__ __forceinline__ float exp2_fast(float v) {      // 2 ulp, results below 2^-126 are 0
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// ------------------------------------------------------------------ forward
+// Of 2^((l - m) log2 e) over a row's half tile: the maximum m, the sum s, and x, the sum weighted
+// with (l - m) log2 e.
+struct EpiLse {
+  static constexpr bool CHUNKED = true;
+  struct Params {
+    const int64_t* targets;
+    float *m, *s, *x;      // [half tile][row]
+    float* picked;         // the targets' logits
+    int rows, v;
+  };
+  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, float (&acc)[128]) {
+    const int cols = min(O.cols, E.v - O.col);      // may be none
+    float m = LOWEST;
+#pragma unroll
+    for (int u = 0; u < 128; ++u) {
+      if (u >= cols) acc[u] = LOWEST;
+      acc[u] = max_nan(acc[u], LOWEST);
+      m = max_nan(m, acc[u]);
+    }
+    if (O.row < E.rows && E.targets) {
+      const int64_t at = E.targets[O.row] - O.col;
+      if (at >= 0 && at < cols) {
+        float l = 0.f;      // (written in C++ it became an index, and the sums local memory)
+#pragma unroll
+        for (int u = 0; u < 128; ++u)
+          asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, %3;\n\t}"
+              : "+f"(l)
+              : "r"((int)at), "r"(u), "f"(acc[u]));
+        E.picked[O.row] = l;
+      }
+    }
+    float s[4] = {}, x[4] = {};
+#pragma unroll
+    for (int u = 0; u < 128; ++u) {
+      const float t = max_nan((acc[u] - m) * LOG2E, -126.f), e = exp2_fast(t);
+      if (u < cols) {
+        s[u & 3] += e;
+        x[u & 3] = fmaf(e, t, x[u & 3]);
+      }
+    }
+    if (O.row < E.rows) {
+      const int64_t at = (int64_t)(2 * O.nt + O.half) * E.rows + O.row;
+      E.m[at] = m;
+      E.s[at] = (s[0] + s[1]) + (s[2] + s[3]);
+      E.x[at] = (x[0] + x[1]) + (x[2] + x[3]);
+    }
+  }
+};
+
+struct JoinParams {
+  const int64_t* targets;
+  const float *m, *s, *x, *picked;
+  int parts, rows, v;
+  float *logp, *entropy, *lse;
+};
+
+// R rows and 256 / R threads for each: every thread joins each (256 / R)-th triple, then they join.
+template <int R>
+__global__ void __launch_bounds__(256) k_head_join(const JoinParams P) {
+  constexpr int N = 256 / R;
+  __shared__ float red[3][N][R];
+  const int r = threadIdx.x % R, n = threadIdx.x / R, row = blockIdx.x * R + r;
+  const bool in = row < P.rows;
+  float m = LOWEST;
+  if (in)
+    for (int p = n; p < P.parts; p += N) m = max_nan(m, P.m[(int64_t)p * P.rows + row]);
+  red[0][n][r] = m;
+  __syncthreads();
+  m = LOWEST;
+  for (int i = 0; i < N; ++i) m = max_nan(m, red[0][i][r]);
+  float s = 0.f, x = 0.f;
+  if (in)
+    for (int p = n; p < P.parts; p += N) {
+      const int64_t at = (int64_t)p * P.rows + row;
+      const float t = max_nan((P.m[at] - m) * LOG2E, -126.f), w = exp2_fast(t);
+      s = fmaf(w, P.s[at], s);
+      x = fmaf(w, fmaf(P.s[at], t, P.x[at]), x);
+    }
+  red[1][n][r] = s;
+  red[2][n][r] = x;
+  __syncthreads();
+  if (n > 0 || !in) return;
+  s = x = 0.f;
+  for (int i = 0; i < N; ++i) {
+    s += red[1][i][r];
+    x += red[2][i][r];
+  }
+  const float ls = logf(s), lse = m + ls;
+  P.lse[row] = lse;
+  P.entropy[row] = ls - LN2 * (x / s);
+  if (P.logp) {
+    const int64_t at = P.targets[row];
+    P.logp[row] = at >= 0 && at < P.v ? P.picked[row] - lse : 0.f;
+  }
+}
+
+// Rows that TMA cannot read as they lie, copied to rows of 16-byte multiples.
+__global__ void __launch_bounds__(256) k_head_copy(const __nv_bfloat16* from, int64_t ld, int64_t rows, int d,
+                                                   __nv_bfloat16* to, int64_t ldt) {
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
+    for (int c = threadIdx.x; c < d; c += blockDim.x) to[row * ldt + c] = from[row * ld + c];
+}
+
+// ------------------------------------------------------------------ backward
+struct EpiGrad {
+  static constexpr bool CHUNKED = false;
+  struct Params {
+    const int64_t* targets;
+    const float *lse, *dlogp, *entropy, *dentropy;
+    float* own;      // the target's entry, where the target lies in the piece
+    int rows, v, v0, count;
+  };
+  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, const CUtensorMap* map) {
+    float lse = 0.f, g = 0.f, u = 0.f, ent = 0.f;
+    int at = -1;      // the target's column in the piece
+    if (O.row < E.rows) {
+      lse = E.lse[O.row];
+      if (E.targets) {
+        const int64_t target = E.targets[O.row];
+        if (target >= 0 && target < E.v) {
+          if (E.dlogp) g = E.dlogp[O.row];
+          if (target >= E.v0 && target < (int64_t)E.v0 + E.count) at = (int)(target - E.v0);
+        }
+      }
+      if (E.dentropy) {
+        u = E.dentropy[O.row];
+        ent = E.entropy[O.row];
+      }
+    }
+    for (int c = 0; c < O.cols; c += 64) {
+      stage_free(O.lane);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t r[32];
+        tmem_ld32(O.tmem + c + 32 * h, r);
+        tmem_wait_ld();
+        const int own = at - (O.col + c + 32 * h);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float lp = max_nan(__uint_as_float(r[j]) - lse, -87.f), p = exp2_fast(lp * LOG2E);
+          float z = -p * fmaf(u, lp + ent, g);
+          if (j == own) {
+            E.own[O.row] = g + z;
+            z = 0.f;
+          }
+          r[j] = __float_as_uint(z);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            w[j] = bf16_pack(__uint_as_float(r[8 * k + 2 * j]), __uint_as_float(r[8 * k + 2 * j + 1]));
+          *staged(O.stage, O.lane, 4 * h + k) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+      stage_ready();
+      if (O.lane == 0) {
+        tma_store_2d(map, O.stage, O.col + c, O.row0);
+        bulk_commit();
+      }
+    }
+  }
+};
+
+__global__ void __launch_bounds__(256) k_head_no_token(int* first, int v) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < v) first[i] = NO_TOKEN;
+}
+// first[j]: the first token whose target is j.
+__global__ void __launch_bounds__(256) k_head_first(const int64_t* targets, int rows, int v, int* first) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows) return;
+  const int64_t at = targets[i];
+  if (at >= 0 && at < v) atomicMin(first + at, i);
+}
+// Row t of `more`, where t is the first token with its target and the target lies in the
+// piece: the sum of own h over the tokens of that target, in their order.
+constexpr int MORE_COLS = 512;
+__global__ void __launch_bounds__(128) k_head_more(const int64_t* targets, const int* first, const float* own,
+                                                   const __nv_bfloat16* h, int64_t ldh, int rows, int d, int v, int v0,
+                                                   int count, float* more, int64_t ldmore) {
+  const int t = blockIdx.x, c0 = blockIdx.y * MORE_COLS + threadIdx.x;
+  const int64_t target = targets[t];
+  if (target < v0 || target >= (int64_t)v0 + count || target >= v || first[target] != t) return;
+  __shared__ int found[128];
+  float acc[4] = {};
+  for (int i0 = t; i0 < rows; i0 += 128) {
+    const int i = i0 + threadIdx.x;
+    found[threadIdx.x] = i < rows && targets[i] == target;
+    const int any = __syncthreads_or(found[threadIdx.x]);
+    if (any)
+      for (int j = 0; j < 128; ++j) {
+        if (!found[j]) continue;
+        const float w = own[i0 + j];
+        const __nv_bfloat16* row = h + (i0 + j) * ldh;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c0 + 128 * k < d) acc[k] = fmaf(w, __bfloat162float(row[c0 + 128 * k]), acc[k]);
+      }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (c0 + 128 * k < d) more[(int64_t)t * ldmore + c0 + 128 * k] = acc[k];
+}
+
+// dh = the parts' sum + own W[target], rounded once.
+__global__ void __launch_bounds__(256) k_head_dh(const float* part, int splits, int64_t ldp, const int64_t* targets,
+                                                 const float* own, const __nv_bfloat16* w, int64_t ldw, int rows,
+                                                 int d, int v, __nv_bfloat16* dh, int64_t lddh) {
+  const int row = blockIdx.x;
+  const int64_t target = targets ? targets[row] : -1;
+  const bool scored = target >= 0 && target < v;
+  const float a = scored ? own[row] : 0.f;
+  for (int c = blockIdx.y * 256 + threadIdx.x; c < d; c += 256 * gridDim.y) {
+    float sum = 0.f;
+    for (int s = 0; s < splits; ++s) sum += part[((int64_t)s * rows + row) * ldp + c];
+    if (scored) sum = fmaf(a, __bfloat162float(w[target * ldw + c]), sum);
+    dh[row * lddh + c] = __float2bfloat16_rn(sum);
+  }
+}
+
+// ------------------------------------------------------------------ host side
+constexpr int HEAD_MAX_ROWS = 1 << 24, HEAD_MAX_V = 1 << 24, HEAD_MAX_D = 1 << 16;
+constexpr int LSE_ROWS = 16384;        // tokens of one forward pass over the weight: bounds the triples
+constexpr int LSE_GROUP = 8;           // K blocks (512 values) summed in place
+constexpr int64_t G_BYTES = 256 << 20; // of G kept at a time
+
+bool head_ok(int rows, int v, int d) {
+  return rows >= 0 && rows <= HEAD_MAX_ROWS && v >= 1 && v <= HEAD_MAX_V && d >= 1 && d <= HEAD_MAX_D;
+}
+bool in_place(const void* p, int64_t rows, int64_t ld) { return aligned16(p, rows > 1 ? ld * 2 : 0); }
+// The row stride a tensor map gets (any, for a single row).
+int64_t map_ld(int64_t rows, int64_t ld, int d) { return rows > 1 ? ld : round_up(d, 8); }
+
+// Columns of a tile for few tokens: as few as the busiest pair can get.
+int lse_bn(int rows, int v) {
+  if (rows > PG_M) return 256;
+  int best = 256;
+  int64_t cost = INT64_MAX;
+  for (int bn = 256; bn >= 128; bn -= 32) {
+    const int64_t c = (int64_t)ceil_div(ceil_div(v, bn), PG_PAIRS) * bn;
+    if (c < cost) {
+      cost = c;
+      best = bn;
+    }
+  }
+  return best;
+}
+
+int box_rows(int rows) { return rows >= 128 ? 128 : (int)round_up(rows, 8); }
+
+// Offsets into the workspaces.
+struct Carve {
+  size_t at = 256;
+  size_t take(size_t bytes) {
+    const size_t r = at;
+    at += align256(bytes);
+    return r;
+  }
+};
+struct HeadLayout {
+  size_t h = 0, w = 0, m, s, x, picked, bytes;
+  bool copy_h, copy_w;
+  HeadLayout(const void* ph, int64_t ldh, const void* pw, int64_t ldw, int rows, int v, int d) {
+    Carve c;
+    copy_h = !in_place(ph, rows, ldh);
+    copy_w = !in_place(pw, v, ldw);
+    if (copy_h) h = c.take((size_t)rows * round_up(d, 8) * 2);
+    if (copy_w) w = c.take((size_t)v * round_up(d, 8) * 2);
+    const int slice = std::min(rows, LSE_ROWS);
+    const size_t triples = (size_t)2 * ceil_div(v, lse_bn(slice, v)) * slice * 4;
+    m = c.take(triples);
+    s = c.take(triples);
+    x = c.take(triples);
+    picked = c.take((size_t)slice * 4);
+    bytes = c.at;
+  }
+};
+struct HeadBackLayout {
+  size_t h = 0, w = 0, own, first = 0, more = 0, g, part, bytes;
+  bool copy_h, copy_w;
+  int piece, splits;
+  int64_t ldg, ldp;      // of G, and of the fp32 sums
+  HeadBackLayout(const void* ph, int64_t ldh, const void* pw, int64_t ldw, int rows, int v, int d, bool dw) {
+    Carve c;
+    copy_h = !in_place(ph, rows, ldh);
+    copy_w = !in_place(pw, v, ldw);
+    if (copy_h) h = c.take((size_t)rows * round_up(d, 8) * 2);
+    if (copy_w) w = c.take((size_t)v * round_up(d, 8) * 2);
+    const int64_t most = std::max<int64_t>(256, G_BYTES / 2 / std::max(rows, 1) / 256 * 256);
+    const int pieces = (int)((v + most - 1) / most);
+    piece = (int)std::min<int64_t>(v, round_up(ceil_div(v, pieces), 256));
+    ldg = round_up(piece, 8);
+    ldp = round_up(d, 4);
+    const int64_t tiles = (int64_t)ceil_div(rows, PG_M) * ceil_div(d, 256);
+    splits = (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(2 * PG_PAIRS, (int)std::min<int64_t>(tiles, 1 << 20)), ceil_div(piece, 8 * PG_K), 32}));
+    own = c.take((size_t)rows * 4);
+    if (dw) {
+      first = c.take((size_t)v * 4);
+      more = c.take((size_t)rows * ldp * 4);
+    }
+    g = c.take((size_t)rows * ldg * 2);
+    part = c.take((size_t)splits * rows * ldp * 4);
+    bytes = c.at;
+  }
+};
+
+cudaError_t copy_rows(const void* from, int64_t ld, int64_t rows, int d, void* to, cudaStream_t s) {
+  k_head_copy<<<(unsigned)std::min<int64_t>(rows, 8 * ROW_SMS), 256, 0, s>>>((const __nv_bfloat16*)from, ld, rows, d,
+                                                                             (__nv_bfloat16*)to, round_up(d, 8));
+  return cudaGetLastError();
+}
+
+PairShape head_shape(int rows, int bn, int tn, int nk, int* status) {
+  PairShape S{};
+  S.tm = ceil_div(rows, PG_M);
+  S.tn = tn;
+  S.bn = bn;
+  S.nk = S.per = nk;
+  S.splits = 1;
+  S.group = nk;
+  S.band = 16;
+  S.rows = rows;
+  S.a_rows = box_rows(rows);
+  S.status = status;
+  S.spin_cycles = spin_cycles_from_env();
+  return S;
+}
+
+}  // namespace
+}  // namespace bakron
+
+using namespace bakron;
+
+extern "C" size_t bakron_head_logprobs_workspace_bytes(const void* h, int64_t ldh, const void* weight, int64_t ldw,
+                                                       int rows, int v, int d) {
+  return head_ok(rows, v, d) && rows > 0 ? HeadLayout(h, ldh, weight, ldw, rows, v, d).bytes : 0;
+}
+
+extern "C" int bakron_head_logprobs(const void* h, int64_t ldh, const void* weight, int64_t ldw, int rows, int v, int d,
+                                    const int64_t* targets, float* logp, float* entropy, float* lse, void* workspace,
+                                    size_t workspace_bytes, int sync, void* stream) {
+  if (!head_ok(rows, v, d)) return BAKRON_ERR_INVALID_ARG;
+  if (rows == 0) return BAKRON_OK;
+  if (!h || !weight || ldh < d || ldw < d || !entropy || !lse || (targets && !logp) || (!targets && logp) || !workspace ||
+      (uintptr_t)workspace % 16 != 0 || (uintptr_t)h % 2 != 0 || (uintptr_t)weight % 2 != 0)
+    return BAKRON_ERR_INVALID_ARG;
+  const HeadLayout L(h, ldh, weight, ldw, rows, v, d);
+  if (workspace_bytes < L.bytes) return BAKRON_ERR_WORKSPACE;
+  cudaStream_t s = (cudaStream_t)stream;
+  char* ws = (char*)workspace;
+  BK_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(int), s));
+  if (L.copy_h) {
+    BK_CUDA_OK(copy_rows(h, ldh, rows, d, ws + L.h, s));
+    h = ws + L.h;
+    ldh = round_up(d, 8);
+  }
+  if (L.copy_w) {
+    BK_CUDA_OK(copy_rows(weight, ldw, v, d, ws + L.w, s));
+    weight = ws + L.w;
+    ldw = round_up(d, 8);
+  }
+  for (int r0 = 0; r0 < rows; r0 += LSE_ROWS) {
+    const int n = std::min(rows - r0, LSE_ROWS), bn = lse_bn(std::min(rows, LSE_ROWS), v);
+    PairShape S = head_shape(n, bn, ceil_div(v, bn), ceil_div(d, PG_K), (int*)ws);
+    S.group = LSE_GROUP;
+    CUtensorMap a, b;
+    if (!pair_map(&a, false, (const __nv_bfloat16*)h + r0 * ldh, n, d, map_ld(n, ldh, d), PG_K, S.a_rows) ||
+        !pair_map(&b, false, weight, v, d, map_ld(v, ldw, d), PG_K, bn / 2))
+      return BAKRON_ERR_CUDA;
+    EpiLse::Params E{targets ? targets + r0 : nullptr, (float*)(ws + L.m), (float*)(ws + L.s), (float*)(ws + L.x),
+                     (float*)(ws + L.picked), n, v};
+    BK_CUDA_OK((pair_launch<EpiLse, false, false>(a, b, b, S, E, s)));
+    JoinParams J{E.targets, E.m, E.s, E.x, E.picked, 2 * S.tn, n, v, logp ? logp + r0 : nullptr, entropy + r0, lse + r0};
+    if (n < 64)
+      k_head_join<1><<<n, 256, 0, s>>>(J);
+    else
+      k_head_join<16><<<ceil_div(n, 16), 256, 0, s>>>(J);
+    BK_CUDA_OK(cudaGetLastError());
+  }
+  return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
+}
+
+extern "C" size_t bakron_head_logprobs_backward_workspace_bytes(const void* h, int64_t ldh, const void* weight,
+                                                                int64_t ldw, int rows, int v, int d, int weight_grad) {
+  return head_ok(rows, v, d) && rows > 0 ? HeadBackLayout(h, ldh, weight, ldw, rows, v, d, weight_grad != 0).bytes : 0;
+}
+
+extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const void* weight, int64_t ldw, int rows,
+                                             int v, int d, const int64_t* targets, const float* lse,
+                                             const float* dlogp, const float* entropy, const float* dentropy, void* dh,
+                                             int64_t lddh, void* dweight, int64_t lddw, void* workspace,
+                                             size_t workspace_bytes, int sync, void* stream) {
+  if (!head_ok(rows, v, d)) return BAKRON_ERR_INVALID_ARG;
+  if ((dweight && lddw < d) || (rows > 0 && (!h || !weight || ldh < d || ldw < d || !lse || (dlogp && !targets) ||
+                                             (dentropy && !entropy) || !dh || lddh < d || !workspace ||
+                                             (uintptr_t)workspace % 16 != 0 || (uintptr_t)h % 2 != 0 ||
+                                             (uintptr_t)weight % 2 != 0)))
+    return BAKRON_ERR_INVALID_ARG;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (rows == 0) {      // no token: no gradient at the weight
+    if (dweight) BK_CUDA_OK(cudaMemset2DAsync(dweight, (size_t)lddw * 2, 0, (size_t)d * 2, (size_t)v, s));
+    if (sync) BK_CUDA_OK(cudaStreamSynchronize(s));
+    return BAKRON_OK;
+  }
+  const HeadBackLayout L(h, ldh, weight, ldw, rows, v, d, dweight != nullptr);
+  if (workspace_bytes < L.bytes) return BAKRON_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
+  BK_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(int), s));
+  if (L.copy_h) {
+    BK_CUDA_OK(copy_rows(h, ldh, rows, d, ws + L.h, s));
+    h = ws + L.h;
+    ldh = round_up(d, 8);
+  }
+  if (L.copy_w) {
+    BK_CUDA_OK(copy_rows(weight, ldw, v, d, ws + L.w, s));
+    weight = ws + L.w;
+    ldw = round_up(d, 8);
+  }
+  float *own = (float*)(ws + L.own), *more = (float*)(ws + L.more), *part = (float*)(ws + L.part);
+  int* first = (int*)(ws + L.first);
+  const bool near = dweight && targets && dlogp;      // dW gets the targets' rows
+  if (near) {
+    k_head_no_token<<<ceil_div(v, 256), 256, 0, s>>>(first, v);
+    k_head_first<<<ceil_div(rows, 256), 256, 0, s>>>(targets, rows, v, first);
+    BK_CUDA_OK(cudaGetLastError());
+  }
+  const bool dw_tma = dweight && in_place(dweight, v, lddw);
+  for (int v0 = 0; v0 < v; v0 += L.piece) {
+    const int count = std::min(v - v0, L.piece);
+    const __nv_bfloat16* w = (const __nv_bfloat16*)weight + v0 * ldw;
+    void* G = ws + L.g;
+    CUtensorMap a, b, o;
+    // G of the piece
+    PairShape S = head_shape(rows, 256, ceil_div(count, 256), ceil_div(d, PG_K), (int*)ws);
+    if (!pair_map(&a, false, h, rows, d, map_ld(rows, ldh, d), PG_K, S.a_rows) ||
+        !pair_map(&b, false, w, count, d, map_ld(count, ldw, d), PG_K, 128) ||
+        !pair_map(&o, false, G, rows, count, L.ldg, 64, 32))
+      return BAKRON_ERR_CUDA;
+    EpiGrad::Params E{dlogp ? targets : nullptr, lse, dlogp, entropy, dentropy, own, rows, v, v0, count};
+    BK_CUDA_OK((pair_launch<EpiGrad, false, false>(a, b, o, S, E, s)));
+    // dh's part
+    S = head_shape(rows, 256, ceil_div(d, 256), ceil_div(count, PG_K), (int*)ws);
+    S.splits = L.splits;
+    S.per = ceil_div(S.nk, S.splits);
+    S.splits = ceil_div(S.nk, S.per);
+    if (!pair_map(&a, false, G, rows, count, L.ldg, PG_K, S.a_rows) ||
+        !pair_map(&b, false, w, count, d, map_ld(count, ldw, d), 64, PG_K) ||
+        !pair_map(&o, true, part, rows, d, L.ldp, 32, 32, L.splits))
+      return BAKRON_ERR_CUDA;
+    if (S.splits < L.splits && v0 == 0)      // no part of the rest: zeros
+      BK_CUDA_OK(cudaMemsetAsync(part + (int64_t)S.splits * rows * L.ldp, 0,
+                                 (size_t)(L.splits - S.splits) * rows * L.ldp * 4, s));
+    BK_CUDA_OK((pair_launch<EpiF32, false, true>(a, b, o, S, EpiF32::Params{v0 > 0}, s)));
+    if (!dweight) continue;
+    // the piece's rows of dW
+    if (near) {
+      k_head_more<<<dim3((unsigned)rows, (unsigned)ceil_div(d, MORE_COLS)), 128, 0, s>>>(
+          targets, first, own, (const __nv_bfloat16*)h, ldh, rows, d, v, v0, count, more, L.ldp);
+      BK_CUDA_OK(cudaGetLastError());
+    }
+    __nv_bfloat16* c = (__nv_bfloat16*)dweight + v0 * lddw;
+    S = head_shape(count, 256, ceil_div(d, 256), ceil_div(rows, PG_K), (int*)ws);
+    S.band = 8;
+    if (!pair_map(&a, false, G, rows, count, L.ldg, 64, PG_K) ||
+        !pair_map(&b, false, h, rows, d, map_ld(rows, ldh, d), 64, PG_K) ||
+        (dw_tma && !pair_map(&o, false, c, count, d, map_ld(count, lddw, d), 64, 32)))
+      return BAKRON_ERR_CUDA;
+    EpiBf16::Params B{dw_tma ? nullptr : c, lddw, count, d, near ? first + v0 : nullptr, more, L.ldp};
+    BK_CUDA_OK((pair_launch<EpiBf16, true, true>(a, b, dw_tma ? o : a, S, B, s)));
+  }
+  k_head_dh<<<dim3((unsigned)rows, (unsigned)std::min(ceil_div(d, 256), 8)), 256, 0, s>>>(
+      part, L.splits, L.ldp, dlogp ? targets : nullptr, own, (const __nv_bfloat16*)weight, ldw, rows, d, v,
+      (__nv_bfloat16*)dh, lddh);
+  BK_CUDA_OK(cudaGetLastError());
+  return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
+}

@@ -122,103 +122,6 @@ struct Ring {
 // the 4096^2 free-running objective from 8e-5 to 3e-4 of the fp64 solve's (an
 // earlier tie, then its cascade).
 
-// ---- CTA-pair forms (cluster of two along y; rank 0 issues the MMAs)
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-
-// Address, in the cluster's shared window, of the same variable in rank 0.
-__device__ __forceinline__ uint32_t at_rank0(const void* p) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
-  return r;
-}
-
-__device__ __forceinline__ void cmbar_arrive_expect_tx(uint32_t cbar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(
-                   cbar),
-               "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void cmbar_expect_tx_only(uint32_t cbar, uint32_t bytes) {
-  asm volatile("mbarrier.expect_tx.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(cbar),
-               "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void cmbar_arrive(uint32_t cbar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cbar)
-               : "memory");
-}
-
-// Bounded wait with cluster-scope acquire (arrivals from the other CTA).
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, long long limit) {
-  const long long t0 = clock64();
-  while (true) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    if (ok) return true;
-    if (clock64() - t0 > limit) return false;
-  }
-}
-
-// TMA loads into this CTA's shared memory whose completion is counted on an
-// mbarrier of rank 0 (cta_group::2: the barrier may sit in the peer CTA).
-__device__ __forceinline__ void tma_load_pair_c2(void* dst, const CUtensorMap* map, uint32_t cbar,
-                                                 int x, int y) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(cbar), "r"(x), "r"(y), "r"(0)
-      : "memory");
-}
-__device__ __forceinline__ void tma_load_2d_c2(void* dst, const CUtensorMap* map, uint32_t cbar,
-                                               int x, int y) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(cbar), "r"(x), "r"(y)
-      : "memory");
-}
-
-__device__ __forceinline__ void mma_tf32_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc,
-                                              uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::tf32 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
-// Arrives on the barrier at this offset in both CTAs of the pair once every
-// MMA issued so far has completed.
-__device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
-  asm volatile(
-      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
-      " [%0], %1;" ::"r"(smem_u32(bar)),
-      "h"((unsigned short)3)
-      : "memory");
-}
-
-// Sets the int at this offset in the other CTA of the pair.
-__device__ __forceinline__ void st_peer_flag(const void* local, int rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(local)), "r"(rank ^ 1));
-  asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(r), "r"(1u) : "memory");
-}
-
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-
 // Output block and K range of this CTA.
 struct Block {
   int rb, cb;         // output block (128-row block, 128-col block)

@@ -313,3 +313,94 @@ def bakron_token_logprobs_backward(logits, targets, lse, dlogp, entropy=None, de
     if rc != OK:
         raise BakronError(rc, "bakron_token_logprobs_backward")
     return out
+
+
+def _matrix(t, n, name, dev):
+    """A bf16 matrix of n columns: (tensor, rows, row stride)."""
+    if t.dim() != 2 or t.shape[1] != n:
+        raise ValueError(f"{name} must be a matrix of {n} columns")
+    return _rows(t, name, (_BF16,), dev)
+
+
+def bakron_head_logprobs(h, weight, targets=None, sync: bool = False, workspace=None, stream=None):
+    """``bakron_token_logprobs`` of the logits h weight^T, which are not kept: h (... x d) and
+    weight (v x d) bfloat16, ``targets`` int64 (outside 0..v-1: not scored, 0).  Returns
+    (logp, entropy, lse), fp32; logp None without targets.  ``sync``: wait, and raise what
+    the device reports (``bakron_read_status(workspace)`` tells it later)."""
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(h, stream)
+        if there is not None:
+            with there:
+                return bakron_head_logprobs(h, weight, targets, sync, workspace)
+    shape, dev = h.shape, h.get_device()
+    h, rows, ldh = _rows(h, "h", (_BF16,), dev)
+    lead, d = shape[:-1], shape[-1]
+    weight, v, ldw = _matrix(weight, d, "weight", dev)
+    t = pl = logp = None
+    if targets is not None:
+        targets = _vector(targets, rows, "targets", (torch.int64,), dev)
+        logp = _empty(lead, dtype=_F32, device=dev)
+        t, pl = targets.data_ptr(), logp.data_ptr()
+    entropy, lse = _empty(lead, dtype=_F32, device=dev), _empty(lead, dtype=_F32, device=dev)
+    L = lib()
+    ph, pw = h.data_ptr(), weight.data_ptr()
+    size = L.bakron_head_logprobs_workspace_bytes(ph, ldh, pw, ldw, rows, v, d)
+    ws, size = _workspace(workspace, size, dev)
+    rc = L.bakron_head_logprobs(ph, ldh, pw, ldw, rows, v, d, t, pl, entropy.data_ptr(), lse.data_ptr(),
+                                ws.data_ptr(), size, 1 if sync else 0, _raw_stream(dev))
+    if rc != OK:
+        raise BakronError(rc, "bakron_head_logprobs")
+    return logp, entropy, lse
+
+
+def _workspace(given, size, dev):
+    """The caller's workspace, or one of `size` bytes: (tensor, bytes)."""
+    if given is None:
+        return _empty(size, dtype=torch.uint8, device=dev), size
+    if given.get_device() != dev or not given.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{dev}")
+    return given, given.nbytes
+
+
+def bakron_head_logprobs_backward(h, weight, targets, lse, dlogp, entropy=None, dentropy=None,
+                                  weight_grad: bool = True, sync: bool = False, workspace=None, stream=None):
+    """The gradients of sum(dlogp logp + dentropy entropy) at h and at the weight, bfloat16;
+    ``lse`` and ``entropy`` from ``bakron_head_logprobs``.  Either gradient may be None.
+    Returns (dh, dweight), dweight None without ``weight_grad``."""
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(h, stream)
+        if there is not None:
+            with there:
+                return bakron_head_logprobs_backward(h, weight, targets, lse, dlogp, entropy, dentropy, weight_grad,
+                                                     sync, workspace)
+    shape, dev, f32 = h.shape, h.get_device(), (_F32,)
+    h, rows, ldh = _rows(h, "h", (_BF16,), dev)
+    d = shape[-1]
+    weight, v, ldw = _matrix(weight, d, "weight", dev)
+    t = g = e = u = pdw = None
+    if targets is not None:
+        targets = _vector(targets, rows, "targets", (torch.int64,), dev)
+        t = targets.data_ptr()
+    lse = _vector(lse, rows, "lse", f32, dev)
+    if dlogp is not None:
+        dlogp = _vector(dlogp, rows, "dlogp", f32, dev)
+        g = dlogp.data_ptr()
+    if entropy is not None:
+        entropy = _vector(entropy, rows, "entropy", f32, dev)
+        e = entropy.data_ptr()
+    if dentropy is not None:
+        dentropy = _vector(dentropy, rows, "dentropy", f32, dev)
+        u = dentropy.data_ptr()
+    dh, dweight = _empty(shape, dtype=_BF16, device=dev), None
+    if weight_grad:
+        dweight = _empty((v, d), dtype=_BF16, device=dev)
+        pdw = dweight.data_ptr()
+    L = lib()
+    ph, pw = h.data_ptr(), weight.data_ptr()
+    size = L.bakron_head_logprobs_backward_workspace_bytes(ph, ldh, pw, ldw, rows, v, d, 1 if weight_grad else 0)
+    ws, size = _workspace(workspace, size, dev)
+    rc = L.bakron_head_logprobs_backward(ph, ldh, pw, ldw, rows, v, d, t, lse.data_ptr(), g, e, u, dh.data_ptr(), d,
+                                         pdw, d, ws.data_ptr(), size, 1 if sync else 0, _raw_stream(dev))
+    if rc != OK:
+        raise BakronError(rc, "bakron_head_logprobs_backward")
+    return dh, dweight
