@@ -110,6 +110,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
   unsigned char* out = smem + PG_STAGES * PG_STAGE;
   uint64_t* bars = (uint64_t*)(out + PG_EPI_WARPS * PG_OUT);
   uint64_t* full = bars;                     // [STAGES] of the first CTA: both CTAs' halves are loaded
+                                           // (its producer expects the bytes of both: an arrival from the
+                                           // other CTA, a release at the cluster, cost 1000 cycles a block)
   uint64_t* empty = bars + PG_STAGES;        // [STAGES] read by its MMAs
   uint64_t* accF = bars + 2 * PG_STAGES;     // [2] sums finished
   uint64_t* accE = accF + 2;                 // [2] of the first CTA: sums read out by both
@@ -121,7 +123,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < PG_STAGES; ++s) {
-      mbar_init(&full[s], 2);      // the two CTAs' producers
+      mbar_init(&full[s], 1);      // the first CTA's producer, for both
       mbar_init(&empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
@@ -150,18 +152,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
     *abort_flag = 1;
     st_peer_flag((const void*)abort_flag, rank);
   };
+  auto wait_warp = [&](uint64_t* bar, uint32_t parity) -> bool {      // every lane tests: the vote keeps a warp together
+    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+    const long long t0 = clock64();
+    while (!__all_sync(0xffffffffu, mbar_test(bar, parity))) {
+      if (__any_sync(0xffffffffu, *abort_flag)) return false;
+      if (__any_sync(0xffffffffu, clock64() - t0 > S.spin_cycles)) {
+        if (lane == 0) timed_out();
+        return false;
+      }
+    }
+    return true;
+  };
   auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {      // false: give up, here or elsewhere
+    if (mbar_test(bar, parity)) return true;
     const long long t0 = clock64();
     while (true) {
-      uint32_t ok;
-      asm volatile(
-          "{\n\t.reg .pred p;\n\t"
-          "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-          "selp.u32 %0, 1, 0, p;\n\t}"
-          : "=r"(ok)
-          : "r"(smem_u32(bar)), "r"(parity)
-          : "memory");
-      if (ok) return true;
+      if (mbar_test(bar, parity)) return true;
       if (*abort_flag) return false;
       if (clock64() - t0 > S.spin_cycles) {
         timed_out();
@@ -172,26 +179,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
 
   if (warp == 0) {
     // ------------------------------------------------------------ loads
-    if (lane == 0) {
-      const uint32_t full0 = at_rank0(full);
-      const uint32_t bbytes = (uint32_t)S.bn * 64u;      // bn / 2 columns of 64 bf16
-      uint32_t it = 0;
-      bool ok = true;
-      for (int64_t item = first; item < items && ok; item += step) {
-        const PairItem I(S, item);
-        const int arow = I.mt * PG_M + rank * 128, bcol = I.nt * S.bn + rank * (S.bn >> 1);
-        const bool load_a = AMN || arow < S.rows;
-        const uint32_t abytes = AMN ? PG_OPERAND : load_a ? (uint32_t)S.a_rows * 128u : 0u;
-        for (int i = 0; i < I.n; ++i, ++it) {
-          const uint32_t s = it % PG_STAGES, use = it / PG_STAGES;
-          if (use > 0 && !wait(&empty[s], (use - 1) & 1u)) {
-            ok = false;
-            break;
-          }
+    const uint32_t full0 = at_rank0(full);
+    const uint32_t bbytes = (uint32_t)S.bn * 64u;      // bn / 2 columns of 64 bf16
+    uint32_t s = 0, parity = 1;      // a fresh barrier's phase before the first counts as complete
+    bool ok = true;
+    for (int64_t item = first; item < items && ok; item += step) {
+      const PairItem I(S, item);
+      const int arow = I.mt * PG_M + rank * 128, bcol = I.nt * S.bn + rank * (S.bn >> 1);
+      const bool load_a = AMN || arow < S.rows;
+      // of both CTAs; the second one's first row is 128 on
+      const uint32_t bytes = 2u * bbytes + (AMN ? 2u * PG_OPERAND
+                                                : (uint32_t)S.a_rows * (arow + 128 < S.rows ? 256u : 128u));
+      int k = I.k0 * PG_K;
+      for (int i = 0; i < I.n; ++i, k += PG_K) {
+        if (!wait_warp(&empty[s], parity)) {
+          ok = false;
+          break;
+        }
+        if (elected()) {
           unsigned char *a = smem + s * PG_STAGE, *b = a + PG_OPERAND;
-          const int k = (I.k0 + i) * PG_K;
           const uint32_t bar = full0 + s * 8u;
-          cmbar_arrive_expect_tx(bar, abytes + bbytes);
+          if (rank == 0) mbar_expect_tx(&full[s], bytes);
           if constexpr (AMN) {
             tma_load_2d_c2(a, &mapA, bar, arow, k);
             tma_load_2d_c2(a + 8192, &mapA, bar, arow + 64, k);
@@ -205,49 +213,59 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
             tma_load_2d_c2(b, &mapB, bar, k, bcol);
           }
         }
-      }
-      if (*abort_flag) {      // copies in flight land within microseconds; wait about a millisecond
-        const long long t0 = clock64();
-        while (clock64() - t0 < 2000000LL) __nanosleep(1000);
+        __syncwarp();
+        if (++s == PG_STAGES) s = 0, parity ^= 1u;
       }
     }
+    if (*abort_flag) {      // copies in flight land within microseconds; wait about a millisecond
+      const long long t0 = clock64();
+      while (clock64() - t0 < 2000000LL) __nanosleep(1000);
+    }
+    __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMAs
-    if (lane == 0) {
-      if (rank == 0) {
-        const uint32_t idesc = idesc_bf16(PG_M, S.bn) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u);
-        const uint64_t da0 = pair_desc(smem_u32(smem), AMN), db0 = pair_desc(smem_u32(smem) + PG_OPERAND, BMN);
-        constexpr uint64_t ka = AMN ? 2048 >> 4 : 2, kb = BMN ? 2048 >> 4 : 2;      // 16 K values on
-        uint32_t it = 0, g = 0;
-        bool ok = true;
-        for (int64_t item = first; item < items && ok; item += step) {
-          const PairItem I(S, item);
-          int in = 0;
-          for (int i = 0; i < I.n; ++i, ++it) {
-            const uint32_t s = it % PG_STAGES, a = g & 1u;
-            if (!wait(&full[s], (it / PG_STAGES) & 1u) || (in == 0 && g >= 2 && !wait(&accE[a], ((g >> 1) - 1) & 1u))) {
+    // The warp goes through the loop together and an elected lane issues: operands stay in uniform registers.
+    if (rank == 0) {
+      const uint32_t idesc = idesc_bf16(PG_M, S.bn) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u);
+      const uint64_t da0 = pair_desc(smem_u32(smem), AMN), db0 = pair_desc(smem_u32(smem) + PG_OPERAND, BMN);
+      constexpr uint64_t ka = AMN ? 2048 >> 4 : 2, kb = BMN ? 2048 >> 4 : 2;      // 16 K values on
+      uint32_t s = 0, parity = 0, g = 0;
+      bool ok = true;
+      for (int64_t item = first; item < items && ok; item += step) {
+        const PairItem I(S, item);
+        int left = I.n;
+        while (left > 0 && ok) {
+          const int n = Epi::CHUNKED ? min(left, S.group) : left;
+          const uint32_t a = g & 1u, d = tmem + a * 256u;
+          if (!wait_warp(&accE[a], ((g >> 1) & 1u) ^ 1u)) {
+            ok = false;
+            break;
+          }
+          for (int i = 0; i < n; ++i) {
+            if (!wait_warp(&full[s], parity)) {
               ok = false;
               break;
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint64_t da = da0 + (uint64_t)((s * PG_STAGE) >> 4), db = db0 + (uint64_t)((s * PG_STAGE) >> 4);
-            const uint32_t d = tmem + a * 256u;
+            const uint64_t da = da0 + (uint64_t)(s * (PG_STAGE >> 4)), db = db0 + (uint64_t)(s * (PG_STAGE >> 4));
+            if (elected()) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              mma_bf16_pair(d, da + kk * ka, db + kk * kb, idesc, (kk > 0 || in > 0) ? 1u : 0u);
-            mma_commit_pair(&empty[s]);
-            ++in;
-            if (i == I.n - 1 || (Epi::CHUNKED && in == S.group)) {
-              mma_commit_pair(&accF[a]);
-              ++g;
-              in = 0;
+              for (int kk = 0; kk < 4; ++kk)
+                mma_bf16_pair(d, da + kk * ka, db + kk * kb, idesc, (kk > 0 || i > 0) ? 1u : 0u);
+              mma_commit_pair(&empty[s]);
+              if (i == n - 1) mma_commit_pair(&accF[a]);
             }
+            __syncwarp();
+            if (++s == PG_STAGES) s = 0, parity ^= 1u;
           }
+          left -= n;
+          ++g;
         }
-        mma_commit_pair(done);
       }
-      if (!mbar_wait_cluster(done, 0, drain)) raise_status(S.status, BAKRON_ERR_TIMEOUT);
+      if (elected()) mma_commit_pair(done);
+      __syncwarp();
     }
+    if (lane == 0 && !mbar_wait_cluster(done, 0, drain)) raise_status(S.status, BAKRON_ERR_TIMEOUT);
     __syncwarp();
   } else {
     // ------------------------------------------------------------ epilogue
@@ -270,7 +288,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
     auto release = [&](uint32_t a) {
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) cmbar_arrive(accE0 + a * 8u);
+      if (lane == 0) cmbar_arrive_tmem(accE0 + a * 8u);
     };
     for (int64_t item = first; item < items && ok; item += step) {
       const PairItem I(S, item);

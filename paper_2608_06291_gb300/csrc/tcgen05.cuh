@@ -174,6 +174,14 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
       : "memory");
 }
 
+// One lane of a whole warp, the way the compiler knows it: what it does keeps its operands
+// in uniform registers.
+__device__ __forceinline__ bool elected() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
+
 // ---- CTA-pair forms (a cluster of two; rank 0 issues the MMAs)
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -202,6 +210,11 @@ __device__ __forceinline__ void cmbar_expect_tx_only(uint32_t cbar, uint32_t byt
 __device__ __forceinline__ void cmbar_arrive(uint32_t cbar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cbar)
                : "memory");
+}
+
+// The same after reads of TMEM alone (tcgen05.wait::ld and a fence order those): no memory to release.
+__device__ __forceinline__ void cmbar_arrive_tmem(uint32_t cbar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cbar) : "memory");
 }
 
 // Bounded wait with cluster-scope acquire (arrivals from the other CTA).
@@ -296,6 +309,7 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
       : "r"(taddr));
 }
 
+// 16 columns of this thread's TMEM lane; valid after tmem_wait_ld().
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
