@@ -530,6 +530,24 @@ int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float*
                   int sync, void* stream);
 
 /*
+ * bakron_linear_backward -- the gradient of bakron_linear's product at its tokens:
+ *   dx = dy What     (dy: the gradient at x What^T, before bias, activation and residual)
+ *   dy       device, rows (at most 2^24) x m BAKRON_BF16 values, row stride lddy (>= m)
+ *   packed   the weight from bakron_pack_weight, with its m, n, qmax, group_size
+ *   dx       device, rows x n BAKRON_BF16, row stride lddx (>= n); must not overlap dy
+ *   workspace device, >= bakron_linear_backward_workspace_bytes(...) bytes, 16-byte aligned; its
+ *            first word is the status of this call
+ *   sync     as for bakron_linear
+ * The sum runs over rows of different scales, so s (c - z) is formed in fp32 and rounded to bf16
+ * before it is multiplied; sums are fp32, in a fixed order, and the result is rounded once.
+ */
+size_t bakron_linear_backward_workspace_bytes(const void* dy, int rows, int64_t lddy, int m,
+                                              int n, int qmax, int group_size);
+int bakron_linear_backward(const void* dy, int rows, int64_t lddy, const void* packed, int m,
+                           int n, int qmax, int group_size, void* dx, int64_t lddx,
+                           void* workspace, size_t workspace_bytes, int sync, void* stream);
+
+/*
  * bakron_rmsnorm -- h = x + residual, y = weight * h / sqrt(mean(h^2) + eps), row by row.
  *   x, residual  device, rows x d, `dtype` BAKRON_F32 or BAKRON_BF16; residual may be NULL
  *   weight   device, d values, wdtype BAKRON_F32 or BAKRON_BF16
@@ -564,6 +582,33 @@ int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t
                             int dtype, int rows, int d, const void* weight, int wdtype,
                             float eps, const void* dsum, int64_t ldds, void* dx, int64_t lddx,
                             float* dw, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * bakron_layernorm -- h = x + residual, y = weight * (h - mean(h)) / sqrt(var(h) + eps) + bias, row by
+ * row, var(h) the mean of (h - mean(h))^2.  Arguments as for bakron_rmsnorm, and
+ *   bias     device, d values, bdtype BAKRON_F32 or BAKRON_BF16, or NULL: none
+ * All in fp32, the mean before the squares; y comes from the unrounded h.  A row that holds a NaN
+ * or an infinity gives NaNs; in 8 bits a NaN scale too.  eps 0 and a constant row: NaNs.
+ */
+int bakron_layernorm(const void* x, int dtype, int rows, int d, int64_t ldx,
+                     const void* residual, int64_t ldr, const void* weight, int wdtype,
+                     const void* bias, int bdtype, float eps, void* sum, int64_t lds, void* y,
+                     int ydtype, int64_t ldy, float* scales, void* stream);
+
+/*
+ * bakron_layernorm_backward -- its gradients, with g = weight * dy, c = h - mean(h), rho =
+ * 1 / sqrt(var(h) + eps):
+ *   dx = rho (g - mean(g) - c rho^2 mean(g c)) + dsum,   dw = sum over rows of dy c rho,
+ *   db = sum over rows of dy
+ * Arguments as for bakron_rmsnorm_backward, and
+ *   db       device, d fp32, written (zeros for no rows); summed in a fixed order
+ */
+size_t bakron_layernorm_backward_workspace_bytes(int rows, int d);
+int bakron_layernorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh,
+                              int dtype, int rows, int d, const void* weight, int wdtype,
+                              float eps, const void* dsum, int64_t ldds, void* dx, int64_t lddx,
+                              float* dw, float* db, void* workspace, size_t workspace_bytes,
+                              void* stream);
 
 /*
  * bakron_token_logprobs -- of each row of logits l (rows x v, BAKRON_F32 or BAKRON_BF16, v at

@@ -20,5 +20,6 @@ from .bakron import (BakronError, Factors, alloc_workspace, bakron_diag_gemm_tf3
                      strerror, workspace_bytes)
 from .buildlib import build  # noqa: F401
 from .operators import (PackedWeight, bakron_head_logprobs, bakron_head_logprobs_backward,  # noqa: F401
-                        bakron_linear, bakron_pack_weight, bakron_rmsnorm, bakron_rmsnorm_backward,
-                        bakron_token_logprobs, bakron_token_logprobs_backward)
+                        bakron_layernorm, bakron_layernorm_backward, bakron_linear, bakron_linear_backward,
+                        bakron_pack_weight, bakron_rmsnorm, bakron_rmsnorm_backward, bakron_token_logprobs,
+                        bakron_token_logprobs_backward)

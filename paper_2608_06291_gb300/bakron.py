@@ -130,6 +130,17 @@ def lib() -> ctypes.CDLL:
     L.bakron_rmsnorm_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, i32, f32, vp, i64, vp, i64, vp,
                                           vp, sz, vp]
     L.bakron_rmsnorm_backward.restype = i32
+    L.bakron_layernorm.argtypes = [vp, i32, i32, i32, i64, vp, i64, vp, i32, vp, i32, f32, vp, i64, vp, i32, i64, vp, vp]
+    L.bakron_layernorm.restype = i32
+    L.bakron_layernorm_backward_workspace_bytes.argtypes = [i32, i32]
+    L.bakron_layernorm_backward_workspace_bytes.restype = sz
+    L.bakron_layernorm_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, i32, f32, vp, i64, vp, i64, vp, vp,
+                                            vp, sz, vp]
+    L.bakron_layernorm_backward.restype = i32
+    L.bakron_linear_backward_workspace_bytes.argtypes = [vp, i32, i64, i32, i32, i32, i32]
+    L.bakron_linear_backward_workspace_bytes.restype = sz
+    L.bakron_linear_backward.argtypes = [vp, i32, i64, vp, i32, i32, i32, i32, vp, i64, vp, sz, i32, vp]
+    L.bakron_linear_backward.restype = i32
     L.bakron_token_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp]
     L.bakron_token_logprobs.restype = i32
     L.bakron_head_logprobs_workspace_bytes.argtypes = [vp, i64, vp, i64, i32, i32, i32]

@@ -1,0 +1,504 @@
+// bakron_layernorm and bakron_layernorm_backward.
+//
+//   h = x + r,  mu = mean(h),  rho = 1 / sqrt(mean((h - mu)^2) + eps),  y = w (h - mu) rho + b
+//   g = w dy,  c = h - mu
+//   dx = rho (g - mean(g) - c rho^2 mean(g c)) + dsum
+//   dw = sum over rows of dy c rho,  db = sum over rows of dy
+//
+// The mean first, then the sums of what is left of each element (not mean(h^2) - mu^2, which
+// loses the variance of rows far from zero): a row stays where the second pass finds it, in
+// registers or shared memory.  h is formed and kept in fp32 and rounded once where it is
+// stored; y comes from the unrounded one.
+#include <algorithm>
+
+#include "norm.cuh"
+
+namespace bakron {
+namespace {
+
+struct LayerParams {
+  const void *x, *res, *w, *b;
+  int64_t ldx, ldr, ldh, ldy;
+  void *h, *y;
+  float* scales;
+  int rows, d;
+  int wbf16, bbf16;
+  int vec;       // d % 8 is 0, and every row of x, res, h, y, w and b starts on 16 bytes (y: 8 for e4m3)
+  float eps;
+};
+
+// Of a group's 8 elements, those inside the row.
+template <bool VEC>
+__device__ __forceinline__ bool inside(int i, int j, int t, int nt, int d) {
+  return VEC ? elem<true>(i, 0, t, nt) < d : elem<false>(i, j, t, nt) < d;
+}
+
+// VPT groups of 8 elements of a row per thread in registers, bound by memory; AHEAD as in the
+// root-mean-square norm: long rows, a CTA takes several with the next one on its way.
+template <typename T, bool E4M3, int VPT, bool AHEAD, bool VEC>
+__global__ void __launch_bounds__(AHEAD || VPT > 1 ? 512 : 1024, AHEAD && VPT * sizeof(T) <= 4 ? 2 : 1)
+    k_layernorm(const LayerParams P) {
+  __shared__ float slots[2][3][32];
+  const int t = threadIdx.x, nt = blockDim.x;
+  struct Row {
+    Raw8<T> x[VPT], r[VPT];
+  };
+  auto load_row = [&](int64_t row, Row& o) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      raw_load<VEC>((const T*)P.x + row * P.ldx, i, t, nt, P.d, o.x[i]);
+      if (P.res) raw_load<VEC>((const T*)P.res + row * P.ldr, i, t, nt, P.d, o.r[i]);
+    }
+  };
+  Row next;
+  if (blockIdx.x < P.rows) load_row(blockIdx.x, next);
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x, turn ^= 1) {
+    float h[VPT][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      next.x[i].get(h[i]);
+      if (P.res) {
+        float r[8];
+        next.r[i].get(r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[i][j] += r[j];
+      }
+    }
+    if (AHEAD && row + gridDim.x < P.rows) load_row(row + gridDim.x, next);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += h[i][j];
+      if (P.h) row_store<VEC>((T*)P.h + row * P.ldh, i, t, nt, P.d, h[i]);
+    }
+    const float mu = cta_all(sum, AddOp(), slots[turn][0]) / (float)P.d;
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[i][j] -= mu;
+        if (inside<VEC>(i, j, t, nt, P.d)) ss = fmaf(h[i][j], h[i][j], ss);
+      }
+    ss = cta_all(ss, AddOp(), slots[turn][1]);
+    const float rho = 1.f / sqrtf(ss / (float)P.d + P.eps);
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float w[8], b[8] = {};
+      load_w<VEC>(P.w, P.wbf16, i, t, nt, P.d, w);
+      if (P.b) load_w<VEC>(P.b, P.bbf16, i, t, nt, P.d, b);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[i][j] = fmaf(h[i][j] * rho, w[j], b[j]);      // (w and b are 0 past the row)
+        if (E4M3) amax = max_nan(amax, fabsf(h[i][j]));
+      }
+      if (!E4M3) row_store<VEC>((T*)P.y + row * P.ldy, i, t, nt, P.d, h[i]);
+    }
+    if constexpr (E4M3) {
+      const RowScale sc(cta_all(amax, MaxNanOp(), slots[turn][2]));
+      if (t == 0) P.scales[row] = sc.s;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[i][j] = sc(h[i][j]);
+        row_store_e4m3<VEC>((uint8_t*)P.y + row * P.ldy, i, t, nt, P.d, h[i]);
+      }
+    }
+    if (!AHEAD) break;
+  }
+}
+
+// Rows too long for registers: x and r are read again in each pass.  h may be x or r, so it is
+// written last, in the pass that forms y.
+template <typename T, bool E4M3>
+__global__ void __launch_bounds__(1024) k_layernorm_long(const LayerParams P) {
+  __shared__ float slots[3][32];
+  const int64_t row = blockIdx.x;
+  const T* x = (const T*)P.x + row * P.ldx;
+  const T* res = P.res ? (const T*)P.res + row * P.ldr : nullptr;
+  auto at = [&](int e) { return res ? to_f32(x[e]) + to_f32(res[e]) : to_f32(x[e]); };
+  auto param = [](const void* p, int bf16, int e) { return bf16 ? to_f32(((const __nv_bfloat16*)p)[e]) : ((const float*)p)[e]; };
+  float sum = 0.f, ss = 0.f;
+  for (int e = threadIdx.x; e < P.d; e += blockDim.x) sum += at(e);
+  const float mu = cta_all(sum, AddOp(), slots[0]) / (float)P.d;
+  for (int e = threadIdx.x; e < P.d; e += blockDim.x) {
+    const float c = at(e) - mu;
+    ss = fmaf(c, c, ss);
+  }
+  ss = cta_all(ss, AddOp(), slots[1]);
+  const float rho = 1.f / sqrtf(ss / (float)P.d + P.eps);
+  auto norm = [&](float v, int e) { return fmaf((v - mu) * rho, param(P.w, P.wbf16, e), P.b ? param(P.b, P.bbf16, e) : 0.f); };
+  float amax = 0.f;
+  if (E4M3) {
+    for (int e = threadIdx.x; e < P.d; e += blockDim.x) amax = max_nan(amax, fabsf(norm(at(e), e)));
+    amax = cta_all(amax, MaxNanOp(), slots[2]);
+  }
+  const RowScale sc(amax);
+  if (E4M3 && threadIdx.x == 0) P.scales[row] = sc.s;
+  for (int e = threadIdx.x; e < P.d; e += blockDim.x) {
+    const float v = at(e), y = norm(v, e);
+    if (P.h) ((T*)P.h + row * P.ldh)[e] = from_f32<T>(v);
+    if constexpr (E4M3)
+      ((uint8_t*)P.y + row * P.ldy)[e] = e4m3(sc(y));
+    else
+      ((T*)P.y + row * P.ldy)[e] = from_f32<T>(y);
+  }
+}
+
+struct LayerBackParams {
+  const void *dy, *h, *w, *dsum;
+  int64_t lddy, ldh, ldds, lddx;
+  void* dx;
+  float *stats, *part;   // [rows][mu, rho]; [parts][dw, db][d]
+  int rows, d, wbf16, parts;
+  int vec;               // as for the norm
+  float eps;
+};
+
+// Two sums over the CTA in one butterfly: the lower half warp goes on with a, the upper with b.
+__device__ __forceinline__ void two_all(float& a, float& b, float2* slots) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const bool up = lane & 16;
+  float v = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 16);
+#pragma unroll
+  for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if ((lane & 15) == 0) (up ? slots[warp].y : slots[warp].x) = v;
+  if (warps > 1)
+    __syncthreads();
+  else
+    __syncwarp();
+  a = b = 0.f;
+  for (int w = 0; w < warps; ++w) {
+    const float2 s = slots[w];
+    a += s.x;
+    b += s.y;
+  }
+}
+
+// A CTA takes the rows blockIdx.x, + gridDim.x, ...; both parameters' gradients stay in registers
+// from row to row and leave as one part per CTA.  A row is read three times (mean, sums of what
+// is left, dx), from a ring of RING rows in shared memory that vector copies fill ahead; a
+// thread reads back only what it copied.  Rows that vectors cannot be used for (RING 1) are
+// copied when their turn comes.
+constexpr int LB_VPT = 4;
+
+template <typename T, typename W, bool VEC, int RING, int MAXT>
+__global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const LayerBackParams P) {
+  constexpr int VPT = LB_VPT;
+  static_assert(VEC || RING == 1, "whole vectors");
+  __shared__ float2 slots[2][16];
+  extern __shared__ __align__(16) unsigned char lb_ring[];   // [RING][h, dy, dsum][d]
+  const int t = threadIdx.x, nt = blockDim.x;
+  pdl_trigger();      // the parts' sum may get ready; it waits for this grid's end
+  float dw[VPT][8] = {}, db[VPT][8] = {};
+  int slot = 0;
+  T* ring = reinterpret_cast<T*>(lb_ring);
+  auto fetch = [&](int64_t row, int to) {      // each thread its own groups
+    T* at = ring + (int64_t)to * 3 * P.d;
+    if (row < P.rows) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        if constexpr (VEC) {
+          const int e0 = elem<true>(i, 0, t, nt);
+          if (e0 >= P.d) continue;
+#pragma unroll
+          for (int k = 0; k < 8; k += 16 / (int)sizeof(T)) {
+            copy16(at + e0 + k, (const T*)P.h + row * P.ldh + e0 + k);
+            copy16(at + P.d + e0 + k, (const T*)P.dy + row * P.lddy + e0 + k);
+            if (P.dsum) copy16(at + 2 * P.d + e0 + k, (const T*)P.dsum + row * P.ldds + e0 + k);
+          }
+        } else {
+          Raw8<T> a, b;
+          raw_load<false>((const T*)P.h + row * P.ldh, i, t, nt, P.d, a);
+          raw_load<false>((const T*)P.dy + row * P.lddy, i, t, nt, P.d, b);
+          float u[8], v[8];
+          a.get(u);
+          b.get(v);
+          row_store<false>(at, i, t, nt, P.d, u);
+          row_store<false>(at + P.d, i, t, nt, P.d, v);
+        }
+      }
+    }
+    if (VEC) copies_group();
+  };
+  if constexpr (VEC) {
+#pragma unroll
+    for (int s = 0; s < RING - 1; ++s) fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+  }
+  const float inv = 1.f / (float)P.d;
+  for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x) {
+    const T* here = ring + (int64_t)slot * 3 * P.d;
+    if constexpr (VEC && RING == 1) {
+      fetch(row, 0);
+      copies_left<0>();
+    } else if constexpr (VEC) {
+      copies_left<RING - 2>();
+      fetch(row + (int64_t)(RING - 1) * gridDim.x, slot == 0 ? RING - 1 : slot - 1);
+      slot = slot == RING - 1 ? 0 : slot + 1;
+    } else {
+      fetch(row, 0);
+    }
+    float mu = 0.f, mg = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float a[8], b[8], w[8];
+      row_load<VEC>(here, i, t, nt, P.d, a);
+      row_load<VEC>(here + P.d, i, t, nt, P.d, b);
+      row_load<VEC>((const W*)P.w, i, t, nt, P.d, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        mu += a[j];
+        mg = fmaf(w[j], b[j], mg);
+      }
+    }
+    two_all(mu, mg, slots[0]);
+    mu *= inv;
+    mg *= inv;
+    float ss = 0.f, gc = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float a[8], b[8], w[8];
+      row_load<VEC>(here, i, t, nt, P.d, a);
+      row_load<VEC>(here + P.d, i, t, nt, P.d, b);
+      row_load<VEC>((const W*)P.w, i, t, nt, P.d, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float c = inside<VEC>(i, j, t, nt, P.d) ? a[j] - mu : 0.f;
+        ss = fmaf(c, c, ss);
+        gc = fmaf(w[j] * b[j], c, gc);
+      }
+    }
+    two_all(ss, gc, slots[1]);
+    const float rho = 1.f / sqrtf(ss * inv + P.eps), k = rho * rho * (gc * inv);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float a[8], b[8], w[8], o[8];
+      row_load<VEC>(here, i, t, nt, P.d, a);
+      row_load<VEC>(here + P.d, i, t, nt, P.d, b);
+      row_load<VEC>((const W*)P.w, i, t, nt, P.d, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float c = a[j] - mu;
+        dw[i][j] = fmaf(b[j] * c, rho, dw[i][j]);      // (dy is 0 past the row)
+        db[i][j] += b[j];
+        o[j] = rho * fmaf(-k, c, fmaf(w[j], b[j], -mg));
+      }
+      if (P.dsum) {
+        row_load<VEC>(VEC ? here + 2 * P.d : (const T*)P.dsum + row * P.ldds, i, t, nt, P.d, a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] += a[j];
+      }
+      row_store<VEC>((T*)P.dx + row * P.lddx, i, t, nt, P.d, o);
+    }
+  }
+  float* part = P.part + (int64_t)blockIdx.x * 2 * P.d;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int e = elem<VEC>(i, j, t, nt);
+      if (e < P.d) {
+        part[e] = dw[i][j];
+        part[P.d + e] = db[i][j];
+      }
+    }
+}
+
+// Rows too long for that: dx of a row, and its mean and rho for the parameters' gradients.
+template <typename T>
+__global__ void __launch_bounds__(256) k_layernorm_dx(const LayerBackParams P) {
+  __shared__ float2 slots[2][16];
+  const int64_t row = blockIdx.x;
+  const T* h = (const T*)P.h + row * P.ldh;
+  const T* dy = (const T*)P.dy + row * P.lddy;
+  auto grad = [&](int e) {
+    return (P.wbf16 ? to_f32(((const __nv_bfloat16*)P.w)[e]) : ((const float*)P.w)[e]) * to_f32(dy[e]);
+  };
+  const float inv = 1.f / (float)P.d;
+  float mu = 0.f, mg = 0.f, ss = 0.f, gc = 0.f;
+  for (int e = threadIdx.x; e < P.d; e += blockDim.x) {
+    mu += to_f32(h[e]);
+    mg += grad(e);
+  }
+  two_all(mu, mg, slots[0]);
+  mu *= inv;
+  mg *= inv;
+  for (int e = threadIdx.x; e < P.d; e += blockDim.x) {
+    const float c = to_f32(h[e]) - mu;
+    ss = fmaf(c, c, ss);
+    gc = fmaf(grad(e), c, gc);
+  }
+  two_all(ss, gc, slots[1]);
+  const float rho = 1.f / sqrtf(ss * inv + P.eps), k = rho * rho * (gc * inv);
+  if (threadIdx.x == 0) {
+    P.stats[2 * row] = mu;
+    P.stats[2 * row + 1] = rho;
+  }
+  for (int e = threadIdx.x; e < P.d; e += blockDim.x) {
+    float v = rho * fmaf(-k, to_f32(h[e]) - mu, grad(e) - mg);
+    if (P.dsum) v += to_f32(((const T*)P.dsum + row * P.ldds)[e]);
+    ((T*)P.dx + row * P.lddx)[e] = from_f32<T>(v);
+  }
+}
+
+// Columns of part p: dy c rho and dy over the rows p, p + parts, ...
+template <typename T>
+__global__ void __launch_bounds__(256) k_layernorm_dwb(const LayerBackParams P) {
+  const int e = blockIdx.x * blockDim.x + threadIdx.x;
+  if (e >= P.d) return;
+  float s = 0.f, b = 0.f;
+  for (int64_t row = blockIdx.y; row < P.rows; row += P.parts) {
+    const float dy = to_f32(((const T*)P.dy + row * P.lddy)[e]);
+    s = fmaf(dy * (to_f32(((const T*)P.h + row * P.ldh)[e]) - P.stats[2 * row]), P.stats[2 * row + 1], s);
+    b += dy;
+  }
+  P.part[(int64_t)blockIdx.y * 2 * P.d + e] = s;
+  P.part[((int64_t)blockIdx.y * 2 + 1) * P.d + e] = b;
+}
+
+// Threads of a CTA (0: rows too long), and CTAs, each with its part: what an SM holds.
+constexpr int LB_SMEM = 220 * 1024;      // of an SM's, beside each CTA's kilobyte
+int layer_threads(int d) {
+  const int nt = (int)round_up(ceil_div(ceil_div(d, 8), LB_VPT), 32);
+  return nt <= 512 ? nt : 0;
+}
+struct LayerPlan {
+  int ring, ctas;      // rows of the ring, CTAs of an SM
+  LayerPlan(int d, int es, bool vec) {
+    const int nt = layer_threads(d), row = 3 * d * es;
+    ring = !vec || 2 * row > LB_SMEM ? 1 : nt > 256 || 2 * 3 * row > LB_SMEM ? 2 : 3;
+    ctas = nt ? std::max(1, std::min(512 / nt, LB_SMEM / (ring * row + 1024))) : 4;
+  }
+};
+int layer_parts(int rows, int d, int es, bool vec) {
+  return std::min(rows, ROW_SMS * LayerPlan(d, es, vec).ctas);
+}
+
+template <typename T, typename W>
+cudaError_t layer_back_launch(const LayerBackParams& P, cudaStream_t s) {
+  const int nt = layer_threads(P.d), ring = LayerPlan(P.d, sizeof(T), P.vec).ring;
+  if (!nt) {
+    k_layernorm_dx<T><<<P.rows, 256, 0, s>>>(P);
+    k_layernorm_dwb<T><<<dim3((unsigned)ceil_div(P.d, 256), (unsigned)P.parts), 256, 0, s>>>(P);
+    return cudaGetLastError();
+  }
+  auto kernel = k_layernorm_back<T, W, false, 1, 512>;
+  if (P.vec)
+    kernel = nt > 256 ? (ring == 1 ? k_layernorm_back<T, W, true, 1, 512> : k_layernorm_back<T, W, true, 2, 512>)
+             : ring == 1 ? k_layernorm_back<T, W, true, 1, 256>
+             : ring == 2 ? k_layernorm_back<T, W, true, 2, 256> : k_layernorm_back<T, W, true, 3, 256>;
+  else if (nt <= 256)
+    kernel = k_layernorm_back<T, W, false, 1, 256>;
+  static OncePerDevice once;
+  const cudaError_t e = once([] {
+    cudaError_t a = cudaSuccess;
+    for (auto k : {k_layernorm_back<T, W, false, 1, 256>, k_layernorm_back<T, W, false, 1, 512>,
+                   k_layernorm_back<T, W, true, 1, 256>, k_layernorm_back<T, W, true, 1, 512>,
+                   k_layernorm_back<T, W, true, 2, 256>, k_layernorm_back<T, W, true, 2, 512>,
+                   k_layernorm_back<T, W, true, 3, 256>})
+      if (a == cudaSuccess) a = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, LB_SMEM);
+    return a;
+  });
+  if (e != cudaSuccess) return e;
+  kernel<<<P.parts, nt, (size_t)ring * 3 * P.d * sizeof(T), s>>>(P);
+  return cudaGetLastError();
+}
+
+template <typename T, bool E4M3, bool VEC>
+int layer_launch(const LayerParams& P, cudaStream_t s) {
+  const int groups = ceil_div(P.d, 8);
+  const bool many = P.rows > 2 * ROW_SMS;
+  if (groups > 2048) {
+    k_layernorm_long<T, E4M3><<<P.rows, 1024, 0, s>>>(P);
+  } else if (groups > 1024 || (many && groups > 512)) {
+    const int vpt = groups > 1024 ? 4 : 2, nt = (int)round_up(ceil_div(groups, vpt), 32);
+    const int ctas = std::min(P.rows, ROW_SMS * ((vpt * (int)sizeof(T) <= 4 ? 1024 : 512) / nt));
+    if (vpt == 4)
+      k_layernorm<T, E4M3, 4, true, VEC><<<ctas, nt, 0, s>>>(P);
+    else
+      k_layernorm<T, E4M3, 2, true, VEC><<<ctas, nt, 0, s>>>(P);
+  } else if (many && groups > 256) {
+    k_layernorm<T, E4M3, 2, false, VEC><<<P.rows, (unsigned)round_up(ceil_div(groups, 2), 32), 0, s>>>(P);
+  } else {
+    k_layernorm<T, E4M3, 1, false, VEC><<<P.rows, (unsigned)round_up(groups, 32), 0, s>>>(P);
+  }
+  BK_CUDA_OK(cudaGetLastError());
+  return BAKRON_OK;
+}
+
+template <typename T>
+int layer_kinds(const LayerParams& P, bool q, cudaStream_t s) {
+  if (q) return P.vec ? layer_launch<T, true, true>(P, s) : layer_launch<T, true, false>(P, s);
+  return P.vec ? layer_launch<T, false, true>(P, s) : layer_launch<T, false, false>(P, s);
+}
+
+}  // namespace
+}  // namespace bakron
+
+using namespace bakron;
+
+extern "C" int bakron_layernorm(const void* x, int dtype, int rows, int d, int64_t ldx, const void* residual,
+                                int64_t ldr, const void* weight, int wdtype, const void* bias, int bdtype, float eps,
+                                void* sum, int64_t lds, void* y, int ydtype, int64_t ldy, float* scales, void* stream) {
+  if (rows < 0 || d < 1 || d > NORM_MAX_D || !float_dtype(dtype) || !float_dtype(wdtype) ||
+      (bias && !float_dtype(bdtype)) || (ydtype != dtype && ydtype != BAKRON_E4M3) || !(eps >= 0.f))
+    return BAKRON_ERR_INVALID_ARG;
+  if (rows == 0) return BAKRON_OK;
+  if (!x || !weight || !y || ldx < d || ldy < d || (residual && ldr < d) || (sum && lds < d) ||
+      (ydtype == BAKRON_E4M3 && !scales))
+    return BAKRON_ERR_INVALID_ARG;
+  const int es = dtype == BAKRON_F32 ? 4 : 2;
+  const bool q = ydtype == BAKRON_E4M3;
+  LayerParams P{};
+  P.x = x; P.res = residual; P.w = weight; P.b = bias; P.h = sum; P.y = y; P.scales = scales;
+  P.ldx = ldx; P.ldr = ldr; P.ldh = lds; P.ldy = ldy;
+  P.rows = rows; P.d = d; P.wbf16 = wdtype == BAKRON_BF16; P.bbf16 = bdtype == BAKRON_BF16; P.eps = eps;
+  P.vec = d % 8 == 0 && aligned16(x, ldx * es) && (!residual || aligned16(residual, ldr * es)) &&
+          (!sum || aligned16(sum, lds * es)) && aligned16(weight, 0) && aligned16(bias, 0) &&
+          (q ? ((uintptr_t)y | (uintptr_t)ldy) % 8 == 0 : aligned16(y, ldy * es));
+  cudaStream_t s = (cudaStream_t)stream;
+  return dtype == BAKRON_F32 ? layer_kinds<float>(P, q, s) : layer_kinds<__nv_bfloat16>(P, q, s);
+}
+
+extern "C" size_t bakron_layernorm_backward_workspace_bytes(int rows, int d) {
+  if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
+  int parts = 0;      // whichever way the call goes
+  for (int es : {2, 4})
+    for (bool vec : {false, true}) parts = std::max(parts, layer_parts(rows, d, es, vec));
+  return align256((size_t)rows * 8) + (size_t)parts * d * 8 + 256;
+}
+
+extern "C" int bakron_layernorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, int dtype, int rows,
+                                         int d, const void* weight, int wdtype, float eps, const void* dsum,
+                                         int64_t ldds, void* dx, int64_t lddx, float* dw, float* db, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
+  if (rows < 0 || d < 1 || d > NORM_MAX_D || !float_dtype(dtype) || !float_dtype(wdtype) || !(eps >= 0.f) || !dw ||
+      !db || !workspace)
+    return BAKRON_ERR_INVALID_ARG;
+  if (rows > 0 && (!dy || !h || !weight || !dx || lddy < d || ldh < d || lddx < d || (dsum && ldds < d)))
+    return BAKRON_ERR_INVALID_ARG;
+  if (workspace_bytes < bakron_layernorm_backward_workspace_bytes(rows, d)) return BAKRON_ERR_WORKSPACE;
+  cudaStream_t s = (cudaStream_t)stream;
+  LayerBackParams P{};
+  P.dy = dy; P.h = h; P.w = weight; P.dsum = dsum; P.dx = dx;
+  P.lddy = lddy; P.ldh = ldh; P.ldds = ldds; P.lddx = lddx;
+  P.rows = rows; P.d = d; P.wbf16 = wdtype == BAKRON_BF16; P.eps = eps;
+  P.stats = (float*)workspace;
+  P.part = (float*)((char*)workspace + align256((size_t)rows * 8));
+  if (rows > 0) {
+    const int es = dtype == BAKRON_F32 ? 4 : 2;
+    P.vec = d % 8 == 0 && aligned16(dy, lddy * es) && aligned16(h, ldh * es) && (!dsum || aligned16(dsum, ldds * es)) &&
+            aligned16(dx, lddx * es) && aligned16(weight, 0);
+    P.parts = layer_parts(rows, d, es, P.vec);
+    const auto launch = dtype == BAKRON_F32
+                            ? (P.wbf16 ? layer_back_launch<float, __nv_bfloat16> : layer_back_launch<float, float>)
+                            : (P.wbf16 ? layer_back_launch<__nv_bfloat16, __nv_bfloat16>
+                                       : layer_back_launch<__nv_bfloat16, float>);
+    BK_CUDA_OK(launch(P, s));
+  }
+  BK_CUDA_OK(launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(d, 32), 2), dim3(32, 32), 0, s, P.part, P.parts, d, dw, db));
+  return BAKRON_OK;
+}

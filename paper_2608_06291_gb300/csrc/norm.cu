@@ -5,17 +5,12 @@
 //
 // The sum h is formed and kept in fp32; it is rounded once where it is stored, and y
 // comes from the unrounded one.
-#include <float.h>
-
 #include <algorithm>
 
-#include "rowops.cuh"
+#include "norm.cuh"
 
 namespace bakron {
 namespace {
-
-constexpr int NORM_MAX_D = 1 << 16;
-constexpr float E4M3_MAX = 448.f;
 
 struct NormParams {
   const void *x, *res, *w;
@@ -26,141 +21,6 @@ struct NormParams {
   int wbf16;
   int vec;       // d % 8 is 0, and every row of x, res, h, y and w starts on 16 bytes (y: 8 for e4m3)
   float eps;
-};
-
-// Element (i, j) of a thread's VPT groups of 8: 8 neighbours where vectors can be used (VEC:
-// d is a multiple of 8 and every row starts on 16 bytes), else one every `nt` elements, so
-// that a warp's loads stay together.
-template <bool VEC>
-__device__ __forceinline__ int elem(int i, int j, int t, int nt) {
-  return VEC ? (t + i * nt) * 8 + j : (i * 8 + j) * nt + t;
-}
-
-template <bool VEC, typename T>
-__device__ __forceinline__ void row_load(const T* p, int i, int t, int nt, int d, float (&v)[8]) {
-  if constexpr (VEC) {
-    const int e0 = elem<true>(i, 0, t, nt);
-    if (e0 < d) {
-      load8(p + e0, v);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = elem<false>(i, j, t, nt);
-      v[j] = e < d ? to_f32(p[e]) : 0.f;
-    }
-  }
-}
-
-template <bool VEC, typename T>
-__device__ __forceinline__ void row_store(T* p, int i, int t, int nt, int d, const float (&v)[8]) {
-  if constexpr (VEC) {
-    const int e0 = elem<true>(i, 0, t, nt);
-    if (e0 < d) store8(p + e0, v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = elem<false>(i, j, t, nt);
-      if (e < d) p[e] = from_f32<T>(v[j]);
-    }
-  }
-}
-
-__device__ __forceinline__ uint8_t e4m3(float v) {
-  return (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3);
-}
-
-template <bool VEC>
-__device__ __forceinline__ void row_store_e4m3(uint8_t* p, int i, int t, int nt, int d, const float (&v)[8]) {
-  if constexpr (VEC) {
-    const int e0 = elem<true>(i, 0, t, nt);
-    if (e0 >= d) return;
-    uint32_t q[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      q[j] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * j], v[2 * j + 1]), __NV_SATFINITE, __NV_E4M3);
-    *reinterpret_cast<uint2*>(p + e0) = make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = elem<false>(i, j, t, nt);
-      if (e < d) p[e] = e4m3(v[j]);
-    }
-  }
-}
-
-// 8 elements as they are stored.
-template <typename T>
-struct Raw8;
-template <>
-struct Raw8<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
-  }
-  __device__ __forceinline__ void set(const float (&v)[8]) {
-    a = make_float4(v[0], v[1], v[2], v[3]);
-    b = make_float4(v[4], v[5], v[6], v[7]);
-  }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  }
-};
-template <>
-struct Raw8<__nv_bfloat16> {
-  uint4 a;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void set(const float (&v)[8]) {
-    a = make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7]));
-  }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    v[0] = bf16_lo(a.x); v[1] = bf16_hi(a.x); v[2] = bf16_lo(a.y); v[3] = bf16_hi(a.y);
-    v[4] = bf16_lo(a.z); v[5] = bf16_hi(a.z); v[6] = bf16_lo(a.w); v[7] = bf16_hi(a.w);
-  }
-};
-
-template <bool VEC, typename T>
-__device__ __forceinline__ void raw_load(const T* p, int i, int t, int nt, int d, Raw8<T>& r) {
-  if (VEC && elem<true>(i, 0, t, nt) < d) {
-    r.load(p + elem<true>(i, 0, t, nt));
-  } else {
-    float v[8];
-    if constexpr (VEC) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    } else {
-      row_load<false>(p, i, t, nt, d, v);
-    }
-    r.set(v);
-  }
-}
-
-// The weight, fp32 or bf16.
-template <bool VEC>
-__device__ __forceinline__ void load_w(const void* w, int bf16, int i, int t, int nt, int d, float (&v)[8]) {
-  if (bf16)
-    row_load<VEC>((const __nv_bfloat16*)w, i, t, nt, d, v);
-  else
-    row_load<VEC>((const float*)w, i, t, nt, d, v);
-}
-
-// A row's scale, and its values over it: a product with the reciprocal, or a quotient
-// where the scale is so small that the reciprocal would overflow.
-struct RowScale {
-  float s, inv;
-  bool small;
-  __device__ explicit RowScale(float amax) {
-    s = amax / E4M3_MAX;
-    if (s == 0.f) s = 1.f;
-    small = s < FLT_MIN;
-    inv = 1.f / s;
-  }
-  __device__ __forceinline__ float operator()(float y) const { return small ? y / s : y * inv; }
 };
 
 // VPT groups of 8 elements of a row per thread in registers.  Bound by memory: what counts is
@@ -461,22 +321,6 @@ __global__ void __launch_bounds__(256) k_rmsnorm_dw(const NormBackParams P) {
   P.part[(int64_t)blockIdx.y * P.d + e] = s;
 }
 
-// dw = the parts' sum, always in the same order: 32 columns a CTA, 32 ranges of parts, whose
-// sums a warp joins pairwise (one after another they were the largest part of dw's error).
-__global__ void __launch_bounds__(1024) k_sum_parts(const float* part, int parts, int d, float* dw) {
-  __shared__ float s[32][33];
-  const int c = blockIdx.x * 32 + threadIdx.x;
-  pdl_wait();
-  float v = 0.f;
-  if (c < d)
-    for (int p = threadIdx.y; p < parts; p += 32) v += part[(int64_t)p * d + c];
-  s[threadIdx.y][threadIdx.x] = v;
-  __syncthreads();
-  v = warp_all(s[threadIdx.x][threadIdx.y], AddOp());
-  const int at = blockIdx.x * 32 + threadIdx.y;
-  if (threadIdx.x == 0 && at < d) dw[at] = v;
-}
-
 // Threads of a CTA (0: rows too long), and CTAs, each with its part of dw: what an SM holds.
 constexpr int NB_SMEM = 220 * 1024;      // of an SM's, beside each CTA's kilobyte
 int back_threads(int d) {
@@ -553,8 +397,6 @@ int norm_kinds(const NormParams& P, bool q, cudaStream_t s) {
   return P.vec ? norm_launch<T, false, true>(P, s) : norm_launch<T, false, false>(P, s);
 }
 
-bool float_dtype(int t) { return t == BAKRON_F32 || t == BAKRON_BF16; }
-
 }  // namespace
 }  // namespace bakron
 
@@ -620,6 +462,7 @@ extern "C" int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void*
                                                        : back_launch<__nv_bfloat16, float>);
     BK_CUDA_OK(launch(P, s));
   }
-  BK_CUDA_OK(launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(d, 32)), dim3(32, 32), 0, s, P.part, P.parts, d, dw));
+  BK_CUDA_OK(launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(d, 32)), dim3(32, 32), 0, s, P.part, P.parts, d, dw,
+                       (float*)nullptr));
   return BAKRON_OK;
 }

@@ -1,9 +1,10 @@
 """The operators that run and score a quantised model, same names as the C ABI:
-the product with a quantised weight, the root-mean-square norm, the log
-probabilities of given tokens, and the gradients of the last two.
+the product with a quantised weight, the root-mean-square norm and the layer norm, the log
+probabilities of given tokens from logits or straight from the hidden states, and the
+gradients of each (the product's at its tokens).
 
 Results carry no autograd graph, whatever their inputs ask for: a training step calls the
-``*_backward`` operators itself, and the product has none.
+``*_backward`` operators itself.
 
 Tensors may have any number of leading dimensions where their rows are evenly
 spaced (or else are copied); the last dimension is contiguous.  Work is enqueued on
@@ -69,6 +70,15 @@ def _vector(t, n, name, dtypes, device):
     if t.dtype not in dtypes or t.numel() != n or t.get_device() != device:
         raise ValueError(f"{name} must be {n} values of {_names(dtypes)} on cuda:{device}")
     return t if t.is_contiguous() else t.contiguous()
+
+
+def _workspace(given, size, dev):
+    """The caller's workspace, or one of `size` bytes: (tensor, bytes)."""
+    if given is None:
+        return _empty(size, dtype=torch.uint8, device=dev), size
+    if given.get_device() != dev or not given.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{dev}")
+    return given, given.nbytes
 
 
 _gpus = 0
@@ -183,6 +193,37 @@ def bakron_linear(x, weight: PackedWeight, x_scales=None, bias=None, activation=
     return out
 
 
+def bakron_linear_backward(dy, weight: PackedWeight, out=None, workspace=None, sync: bool = False, stream=None):
+    """dx = dy What, the gradient of ``bakron_linear``'s product at its tokens: dy (... x m,
+    bfloat16) is the gradient at x What^T, before bias, activation and residual.  Returns
+    dx (... x n, bfloat16).  ``sync``: wait, and raise what the device reports
+    (``bakron_read_status(workspace)`` tells it later)."""
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(dy, stream)
+        if there is not None:
+            with there:
+                return bakron_linear_backward(dy, weight, out, workspace, sync)
+    m, n, dev = weight.m, weight.n, weight.buf.get_device()
+    shape = dy.shape
+    dy, rows, lddy = _rows(dy, "dy", (_BF16,), dev)
+    if shape[-1] != m:
+        raise ValueError(f"dy must have {m} columns")
+    xshape = shape[:-1] + (n,)
+    if out is None:
+        out, ldx = _empty(xshape, dtype=_BF16, device=dev), n
+    else:
+        ldx = _result(out, xshape, "out", _BF16, dev)
+    L = lib()
+    py = dy.data_ptr()
+    size = L.bakron_linear_backward_workspace_bytes(py, rows, lddy, m, n, weight.qmax, weight.group_size)
+    ws, size = _workspace(workspace, size, dev)
+    rc = L.bakron_linear_backward(py, rows, lddy, weight.buf.data_ptr(), m, n, weight.qmax, weight.group_size,
+                                  out.data_ptr(), ldx, ws.data_ptr(), size, 1 if sync else 0, _raw_stream(dev))
+    if rc != OK:
+        raise BakronError(rc, "bakron_linear_backward")
+    return out
+
+
 def bakron_rmsnorm(x, weight, eps: float = 1e-6, residual=None, out_dtype=None, stream=None):
     """h = x + residual, y = weight h / sqrt(mean(h^2) + eps) over the last dimension.
     Returns (y, scales, h): y of ``out_dtype`` (default x's; or float8_e4m3fn with
@@ -246,6 +287,74 @@ def bakron_rmsnorm_backward(dy, h, weight, eps: float = 1e-6, dsum=None, stream=
     if rc != OK:
         raise BakronError(rc, "bakron_rmsnorm_backward")
     return dx, dw
+
+
+def bakron_layernorm(x, weight, bias=None, eps: float = 1e-5, residual=None, out_dtype=None, stream=None):
+    """h = x + residual, y = weight (h - mean(h)) / sqrt(var(h) + eps) + bias over the last
+    dimension.  Returns (y, scales, h) as ``bakron_rmsnorm`` does."""
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(x, stream)
+        if there is not None:
+            with there:
+                return bakron_layernorm(x, weight, bias, eps, residual, out_dtype)
+    shape, dev, dtype = x.shape, x.get_device(), x.dtype
+    x, rows, ldx = _rows(x, "x", (_F32, _BF16), dev)
+    d = shape[-1]
+    weight = _vector(weight, d, "weight", (_F32, _BF16), dev)
+    if out_dtype is None:
+        out_dtype = dtype
+    elif out_dtype is not dtype and out_dtype is not _E4M3:
+        raise ValueError("out_dtype must be x's or float8_e4m3fn")
+    y = _empty(shape, dtype=out_dtype, device=dev)
+    scales = h = s = ph = r = b = None
+    ldr = bt = 0
+    if bias is not None:
+        bias = _vector(bias, d, "bias", (_F32, _BF16), dev)
+        b, bt = bias.data_ptr(), _DTYPES[bias.dtype]
+    if residual is not None:
+        residual, _, ldr = _like(residual, shape, "residual", dtype, dev)
+        h = _empty(shape, dtype=dtype, device=dev)
+        ph, r = h.data_ptr(), residual.data_ptr()
+    if out_dtype is _E4M3:
+        scales = _empty(shape[:-1], dtype=_F32, device=dev)
+        s = scales.data_ptr()
+    rc = lib().bakron_layernorm(x.data_ptr(), _DTYPES[dtype], rows, d, ldx, r, ldr, weight.data_ptr(),
+                                _DTYPES[weight.dtype], b, bt, eps, ph, d, y.data_ptr(), _DTYPES[out_dtype], d, s,
+                                _raw_stream(dev))
+    if rc != OK:
+        raise BakronError(rc, "bakron_layernorm")
+    return y, scales, h
+
+
+def bakron_layernorm_backward(dy, h, weight, eps: float = 1e-5, dsum=None, stream=None):
+    """Gradients of y = weight (h - mean(h)) / sqrt(var(h) + eps) + bias, given dy and the
+    gradient ``dsum`` that reaches h past the norm.  Returns (dx of h's type, dweight fp32,
+    dbias fp32)."""
+    if stream is not None or _gpus != 1:
+        there = _elsewhere(dy, stream)
+        if there is not None:
+            with there:
+                return bakron_layernorm_backward(dy, h, weight, eps, dsum)
+    shape, dev, dtype = h.shape, h.get_device(), h.dtype
+    h, rows, ldh = _rows(h, "h", (_F32, _BF16), dev)
+    d = shape[-1]
+    dy, _, lddy = _like(dy, shape, "dy", dtype, dev)
+    weight = _vector(weight, d, "weight", (_F32, _BF16), dev)
+    ps, ldds = None, 0
+    if dsum is not None:
+        dsum, _, ldds = _like(dsum, shape, "dsum", dtype, dev)
+        ps = dsum.data_ptr()
+    L = lib()
+    dx = _empty(shape, dtype=dtype, device=dev)
+    dw, db = _empty(d, dtype=_F32, device=dev), _empty(d, dtype=_F32, device=dev)
+    size = L.bakron_layernorm_backward_workspace_bytes(rows, d)
+    ws = _empty(size, dtype=torch.uint8, device=dev)
+    rc = L.bakron_layernorm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, _DTYPES[dtype], rows, d,
+                                     weight.data_ptr(), _DTYPES[weight.dtype], eps, ps, ldds, dx.data_ptr(), d,
+                                     dw.data_ptr(), db.data_ptr(), ws.data_ptr(), size, _raw_stream(dev))
+    if rc != OK:
+        raise BakronError(rc, "bakron_layernorm_backward")
+    return dx, dw, db
 
 
 def bakron_token_logprobs(logits, targets=None, top: int = 0, stream=None):
@@ -351,15 +460,6 @@ def bakron_head_logprobs(h, weight, targets=None, sync: bool = False, workspace=
     if rc != OK:
         raise BakronError(rc, "bakron_head_logprobs")
     return logp, entropy, lse
-
-
-def _workspace(given, size, dev):
-    """The caller's workspace, or one of `size` bytes: (tensor, bytes)."""
-    if given is None:
-        return _empty(size, dtype=torch.uint8, device=dev), size
-    if given.get_device() != dev or not given.is_contiguous():
-        raise ValueError(f"workspace must be a contiguous tensor on cuda:{dev}")
-    return given, given.nbytes
 
 
 def bakron_head_logprobs_backward(h, weight, targets, lse, dlogp, entropy=None, dentropy=None,
