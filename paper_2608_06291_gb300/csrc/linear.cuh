@@ -131,6 +131,12 @@ __device__ __forceinline__ uint32_t pair8(uint32_t w0, uint32_t w1, int p, __nv_
   return *reinterpret_cast<uint32_t*>(&r);
 }
 
+// The kernel behind it may start at once, and waits for it before it raises the status.
+static __global__ void k_clear_status(int* status) {
+  pdl_trigger();
+  *status = 0;
+}
+
 // Many tokens (linear_tc.cu): the bytes of workspace its call needs (the status, the tokens'
 // copy where they cannot be read as they are), and the call.
 size_t linear_tc_workspace(const void* x, bool x8, int rows, int64_t ldx, int n, bool bytes8);

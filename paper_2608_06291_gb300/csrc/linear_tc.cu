@@ -89,19 +89,6 @@ struct TcParams {
   long long spin_cycles;
 };
 
-// Whether a phase is over, without waiting (mbar_test's try_wait may hold the thread a while).
-__device__ __forceinline__ bool mbar_look(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
 // A warp's wait for two barriers, every lane testing (the vote keeps the control flow
 // uniform); gives up after `limit` cycles, or once another role has.
 __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, uint64_t* bar2, uint32_t parity2, long long limit,
@@ -698,11 +685,6 @@ __global__ void __launch_bounds__(256)
         ((uint8_t*)out)[row * ldo + k] = v;
     }
   }
-}
-
-__global__ void k_clear_status(int* status) {
-  pdl_trigger();
-  *status = 0;
 }
 
 template <class S, bool EXACT>

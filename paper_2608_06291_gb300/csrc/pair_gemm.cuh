@@ -152,29 +152,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
     *abort_flag = 1;
     st_peer_flag((const void*)abort_flag, rank);
   };
-  auto wait_warp = [&](uint64_t* bar, uint32_t parity) -> bool {      // every lane tests: the vote keeps a warp together
-    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-    const long long t0 = clock64();
-    while (!__all_sync(0xffffffffu, mbar_test(bar, parity))) {
-      if (__any_sync(0xffffffffu, *abort_flag)) return false;
-      if (__any_sync(0xffffffffu, clock64() - t0 > S.spin_cycles)) {
-        if (lane == 0) timed_out();
-        return false;
-      }
-    }
-    return true;
-  };
-  auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {      // false: give up, here or elsewhere
-    if (mbar_test(bar, parity)) return true;
-    const long long t0 = clock64();
-    while (true) {
-      if (mbar_test(bar, parity)) return true;
-      if (*abort_flag) return false;
-      if (clock64() - t0 > S.spin_cycles) {
-        timed_out();
-        return false;
-      }
-    }
+  auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {      // a warp; false: give up, here or elsewhere
+    if (mbar_wait_warp(bar, parity, S.spin_cycles, abort_flag)) return true;
+    if (lane == 0 && !*abort_flag) timed_out();
+    __syncwarp();
+    return false;
   };
 
   if (warp == 0) {
@@ -192,7 +174,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
                                                 : (uint32_t)S.a_rows * (arow + 128 < S.rows ? 256u : 128u));
       int k = I.k0 * PG_K;
       for (int i = 0; i < I.n; ++i, k += PG_K) {
-        if (!wait_warp(&empty[s], parity)) {
+        if (!wait(&empty[s], parity)) {
           ok = false;
           break;
         }
@@ -237,12 +219,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
         while (left > 0 && ok) {
           const int n = Epi::CHUNKED ? min(left, S.group) : left;
           const uint32_t a = g & 1u, d = tmem + a * 256u;
-          if (!wait_warp(&accE[a], ((g >> 1) & 1u) ^ 1u)) {
+          if (!wait(&accE[a], ((g >> 1) & 1u) ^ 1u)) {
             ok = false;
             break;
           }
           for (int i = 0; i < n; ++i) {
-            if (!wait_warp(&full[s], parity)) {
+            if (!wait(&full[s], parity)) {
               ok = false;
               break;
             }
@@ -278,12 +260,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
     O.cols = S.bn >> 1;
     uint32_t g = 0;
     bool ok = true;
-    auto sums = [&](uint32_t a) -> bool {      // warp-uniform: tcgen05.ld is warp-collective
-      int r = 1;
-      if (lane == 0) r = wait(&accF[a], (g >> 1) & 1u) ? 1 : 0;
-      r = __shfl_sync(0xffffffffu, r, 0);
+    auto sums = [&](uint32_t a) -> bool {
+      const bool r = wait(&accF[a], (g >> 1) & 1u);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      return r != 0;
+      return r;
     };
     auto release = [&](uint32_t a) {
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

@@ -46,6 +46,30 @@ __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 
+// Whether a phase is over, without waiting (mbar_test's try_wait may hold the thread a while).
+__device__ __forceinline__ bool mbar_look(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+// A warp's wait, every lane testing (the vote keeps the warp together); false once `limit` cycles
+// are over, or another role has set the flag (null: nobody's).
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, long long limit, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_look(bar, parity))) return true;
+  const long long t0 = clock64();
+  while (true) {
+    if (__any_sync(0xffffffffu, (abort_flag && *abort_flag) || clock64() - t0 > limit)) return false;
+    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+  }
+}
+
 // Wait for the phase of `bar` with the given parity to complete, for at most
 // `limit` cycles.  Returns false on time-out.
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, long long limit) {
@@ -307,6 +331,12 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
         "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
         "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr));
+}
+
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
 }
 
 // 16 columns of this thread's TMEM lane; valid after tmem_wait_ld().
