@@ -5,29 +5,24 @@
 // sum as it does in the forward product: an operand is s (c - z), formed in fp32 and rounded
 // once to bf16.
 //
-// Up to FUSED_TOKENS tokens: one kernel. D (128 columns of What x BN tokens) = A B with A the
-// operands of a 128-column block, formed from the codes in shared memory as the MMAs take them
-// (MN-major), and B the tokens' gradients, K-major by TMA.  What's rows are shared by the CTAs of a
-// cluster, which add their parts through each other's shared memory, always in the same order.
+// Up to FUSED_TOKENS tokens: one kernel. D (128 columns of What x bn tokens) += A B with A the
+// operands of a 128 x 128 block, formed from its codes in shared memory as the MMAs take them
+// (MN-major), and B the tokens' gradients, K-major by TMA.
 // More tokens: the weight is written out in bf16 once, and read by the pair product.
-#include <cooperative_groups.h>
-
 #include <algorithm>
 
 #include "linear.cuh"
 #include "pair_gemm.cuh"
 
-namespace cg = cooperative_groups;
-
 namespace bakron {
 namespace {
 
 // ------------------------------------------------------------------ few tokens
-constexpr int FB_WARPS = 8;                      // expand, then write out
-constexpr int FB_THREADS = 32 * (2 + FB_WARPS);  // warp 0 loads gradients, warp 1 issues MMAs
-constexpr int FB_K = 64;                         // rows of What of a stage
-constexpr uint32_t FB_A = FB_K * 128 * 2;        // its operands: 2 x 64 columns, [row][64]
-constexpr int FB_STAGES = 4;
+constexpr int FB_WARPS = 16;                     // form operands
+constexpr int FB_THREADS = 32 * (8 + FB_WARPS);  // warps 0 and 2 load, warp 1 issues MMAs, warps 4-7 write out
+constexpr uint32_t FB_A = LIN_BLOCK * LIN_BLOCK * 2;   // operands: [64 rows][64 columns], two by two
+constexpr int FB_RING = 8;                       // most stages of a ring
+constexpr int FB_MAX_BN = 192;
 
 struct FusedParams {
   const unsigned char* codes;
@@ -36,12 +31,29 @@ struct FusedParams {
   int64_t mp;
   int kblocks, chunks, G;
   int rows, n, bn;         // tokens, columns, tokens of a tile (a multiple of 16)
-  int nk, per;             // stages in all, of a CTA of the cluster
+  int nk, token_tiles, tiles;      // 128-row blocks; tiles in all
+  int na, nb, nc;          // stages of the operands' ring, the gradients', the codes'
   __nv_bfloat16* dx;
   int64_t ldx;
-  int vec;                 // dx can be written 16 bytes at a time
+  float* part;             // [CTA][its first tile, its last][token][128 columns]
+  int vec;                 // dx can be written 8 bytes at a time
   int* status;
   long long spin_cycles;
+};
+
+// The CTAs' equal shares of all tiles' blocks.
+struct Shares {
+  int64_t units;
+  int nk, ctas;
+  __host__ __device__ Shares(const FusedParams& P, int ctas_) : units((int64_t)P.tiles * P.nk), nk(P.nk), ctas(ctas_) {}
+  __host__ __device__ __forceinline__ int64_t begin(int cta) const { return units * cta / ctas; }
+  __host__ __device__ int owner(int64_t unit) const {
+    int i = (int)(unit * ctas / units);
+    while (begin(i + 1) <= unit) ++i;
+    return i;
+  }
+  // of a CTA's sums of a tile: its first tile, or another (then its last)
+  __host__ __device__ __forceinline__ int64_t slot(int cta, int tile) const { return 2 * (int64_t)cta + (begin(cta) / nk != tile); }
 };
 
 // Two values c - z times s, rounded once: s = hi + lo, and what the small product loses is
@@ -58,42 +70,54 @@ __device__ __forceinline__ uint32_t scaled8(uint32_t w, int odd, __half2 z1024, 
   return bf16_pack(c.x * s, c.y * s);
 }
 
-// What a thread needs of a stage: a row's unit (two with 8 bits a code), its grids.
-template <bool W8, bool ONE>
-struct Piece {
-  uint4 u[W8 ? 2 : 1];
-  float s[ONE ? 1 : 4];
-  uint8_t z[ONE ? 1 : 4];
-};
-
-// ONE: the 128 columns of a block have one grid a row.
-template <bool W8, bool ONE>
-__global__ void __launch_bounds__(FB_THREADS, 2) k_back_fused(const __grid_constant__ CUtensorMap map, const FusedParams P) {
+// A CTA takes an equal share of all tiles' blocks, one after another; a tile that several share is
+// summed from their parts, in their order, by a second kernel.  (As clusters that add
+// through each other's shared memory, no more than 15 of 8 CTAs ran at a time.)
+// ONE: the 128 columns of a block have one grid a row.  TEAMS: see below; na and nc are multiples of
+// it, so that a ring's slot always belongs to one team, which knows the phase it is in.
+template <bool W8, bool ONE, int TEAMS>
+__global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_constant__ CUtensorMap map, const FusedParams P) {
+  constexpr int TEAM = FB_WARPS / TEAMS;      // warps
+  constexpr uint32_t CODES = W8 ? 16384 : 8192, GRID = LIN_BLOCK * 5, GRIDS = ONE ? 1 : 4;
   extern __shared__ __align__(1024) unsigned char fb_smem[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)fb_smem + 1023) & ~(uintptr_t)1023);
-  const uint32_t stage_bytes = FB_A + (uint32_t)P.bn * 128u;
-  __shared__ uint64_t full[FB_STAGES], formed[FB_STAGES], empty[FB_STAGES], done;
+  const uint32_t half_b = (uint32_t)P.bn * 128u;
+  unsigned char* tokens = smem + P.na * FB_A;     // [nb][two 64-row halves][bn][64]
+  unsigned char* codes = tokens + P.nb * 2 * half_b;     // [nc][codes], then [nc][GRIDS][scales, zeros]
+  unsigned char* grids = codes + P.nc * CODES;
+  // F: tokens and codes loaded, operands formed, sums finished; E: free again
+  __shared__ uint64_t bF[FB_RING], bE[FB_RING], cF[FB_RING], cE[FB_RING], aF[FB_RING], aE[FB_RING], accF[2], accE[2],
+      done;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  cg::cluster_group cluster = cg::this_cluster();
-  const int splits = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
-  const int cb = blockIdx.x / splits, tok0 = blockIdx.y * P.bn;
-  const int k0 = part * P.per, nk = max(0, min(P.per, P.nk - k0));
-  const uint32_t cols = P.bn <= 32 ? 32u : P.bn <= 64 ? 64u : P.bn <= 128 ? 128u : 256u;
+  pdl_trigger();      // the sum of the parts may get ready; it waits for this grid's end
+  const Shares share(P, gridDim.x);
+  const int64_t u0 = share.begin(blockIdx.x), u1 = share.begin(blockIdx.x + 1);
+  const int tile0 = (int)(u0 / P.nk), first_k = (int)(u0 % P.nk), count = (int)(u1 - u0);
+  uint32_t cols = 32;      // of TMEM, for one tile's sums
+  while (cols < (uint32_t)P.bn) cols *= 2;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < FB_STAGES; ++i) {
-      mbar_init(&full[i], 1);
-      mbar_init(&formed[i], FB_WARPS);
-      mbar_init(&empty[i], 1);
+    for (int i = 0; i < FB_RING; ++i) {
+      mbar_init(&bF[i], 1);
+      mbar_init(&bE[i], 1);
+      mbar_init(&cF[i], 1);
+      mbar_init(&cE[i], TEAM);
+      mbar_init(&aF[i], TEAM);
+      mbar_init(&aE[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&accF[i], 1);
+      mbar_init(&accE[i], 4);
     }
     mbar_init(&done, 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(cols)
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)),
+                 "r"(2 * cols)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -117,151 +141,196 @@ __global__ void __launch_bounds__(FB_THREADS, 2) k_back_fused(const __grid_const
 
   if (warp == 0) {
     // ------------------------------------------------------------ gradients
-    int it = 0;
-    for (; it < nk; ++it) {
-      const int s = it % FB_STAGES;
-      if (it >= FB_STAGES && !wait(&empty[s], (uint32_t)(it / FB_STAGES - 1) & 1u)) break;
+    int it = 0, s = 0, k = first_k, tile = tile0;
+    uint32_t parity = 1;      // a fresh barrier's phase before the first counts as complete
+    for (; it < count; ++it) {
+      if (!wait(&bE[s], parity)) break;
       if (elected()) {
-        mbar_expect_tx(&full[s], (uint32_t)P.bn * 128u);
-        tma_load_2d(smem + s * stage_bytes + FB_A, &map, &full[s], (k0 + it) * FB_K, tok0);
+        unsigned char* to = tokens + s * 2 * half_b;
+        const int tok = tile % P.token_tiles * P.bn;
+        mbar_expect_tx(&bF[s], 2 * half_b);
+        tma_load_2d(to, &map, &bF[s], k * LIN_BLOCK, tok);
+        tma_load_2d(to + half_b, &map, &bF[s], k * LIN_BLOCK + 64, tok);
       }
       __syncwarp();
+      if (++k == P.nk) k = 0, ++tile;
+      if (++s == P.nb) s = 0, parity ^= 1u;
     }
     // every copy has landed before the CTA (and its shared memory) goes
-    for (int j = max(0, it - FB_STAGES); j < it; ++j) wait(&full[j % FB_STAGES], (uint32_t)(j / FB_STAGES) & 1u, true);
+    for (int j = max(0, it - P.nb); j < it; ++j) wait(&bF[j % P.nb], (uint32_t)(j / P.nb) & 1u, true);
+  } else if (warp == 2) {
+    // ------------------------------------------------------------ codes and grids
+    int it = 0, s = 0, k = first_k, tile = tile0;
+    uint32_t parity = 1;
+    for (; it < count; ++it) {
+      if (!wait(&cE[s], parity)) break;
+      if (elected()) {
+        const int cb = tile / P.token_tiles;
+        mbar_expect_tx(&cF[s], CODES + GRIDS * GRID);
+        bulk_load(codes + s * CODES, P.codes + ((int64_t)k * P.kblocks + cb) * CODES, CODES, &cF[s]);
+#pragma unroll
+        for (int j = 0; j < (int)GRIDS; ++j) {
+          const int g = P.G == 1 ? 0 : min((cb * 4 + j) / P.chunks, P.G - 1);
+          const int64_t at = g * P.mp + (int64_t)k * LIN_BLOCK;
+          unsigned char* to = grids + (s * GRIDS + j) * GRID;
+          bulk_load(to, P.scales + at, LIN_BLOCK * 4, &cF[s]);
+          bulk_load(to + LIN_BLOCK * 4, P.zeros + at, LIN_BLOCK, &cF[s]);
+        }
+      }
+      __syncwarp();
+      if (++k == P.nk) k = 0, ++tile;
+      if (++s == P.nc) s = 0, parity ^= 1u;
+    }
+    for (int j = max(0, it - P.nc); j < it; ++j) wait(&cF[j % P.nc], (uint32_t)(j / P.nc) & 1u, true);
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMAs
     const uint32_t idesc = idesc_bf16(128, P.bn) | 1u << 15;
-    for (int it = 0; it < nk; ++it) {
-      const int s = it % FB_STAGES;
-      const uint32_t parity = (uint32_t)(it / FB_STAGES) & 1u;
-      if (!wait(&full[s], parity) || !wait(&formed[s], parity)) break;
+    int sa = 0, sb = 0, k = first_k, more = 0;      // more: the tile has begun
+    uint32_t pa = 0, pb = 0, g = 0;
+    for (int it = 0; it < count; ++it) {
+      if ((!more && !wait(&accE[g & 1u], ((g >> 1) & 1u) ^ 1u)) || !wait(&bF[sb], pb) || !wait(&aF[sa], pa)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t at = smem_u32(smem) + s * stage_bytes;
-      const uint64_t a = pair_desc(at, true), b = smem_desc(at + FB_A);
+      const uint32_t d = tmem + (g & 1u) * cols;
+      const uint64_t a = pair_desc(smem_u32(smem) + sa * FB_A, true), b = smem_desc(smem_u32(tokens) + sb * 2 * half_b);
+      const bool last = it == count - 1 || k == P.nk - 1;
       if (elected()) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma_bf16(tmem, a + k * (2048 >> 4), b + k * 2, idesc, it > 0 || k > 0 ? 1u : 0u);
-        mma_commit(&empty[s]);
+        for (int kk = 0; kk < 8; ++kk)
+          mma_bf16(d, a + (kk >> 2) * (FB_A / 2 >> 4) + (kk & 3) * (2048 >> 4), b + (kk >> 2) * (half_b >> 4) + (kk & 3) * 2,
+                   idesc, more || kk > 0 ? 1u : 0u);
+        mma_commit(&aE[sa]);
+        mma_commit(&bE[sb]);
+        if (last) mma_commit(&accF[g & 1u]);
       }
       __syncwarp();
+      more = !last;
+      if (last) ++g;
+      if (++k == P.nk) k = 0;
+      if (++sa == P.na) sa = 0, pa ^= 1u;
+      if (++sb == P.nb) sb = 0, pb ^= 1u;
     }
     if (elected()) mma_commit(&done);
     __syncwarp();
     wait(&done, 0, true);
-  } else {
+  } else if (warp >= 8) {
     // ------------------------------------------------------------ operands
-    // A thread takes a row's 32 codes of a stage: lanes 0-7 eight rows of unit 0, the next eight
-    // the same rows of unit 1, ..., so that loads are whole lines and the 16-byte stores of
-    // eight lanes cover the banks.
-    constexpr int UNITS = W8 ? 8 : 4, D = W8 || !ONE ? 2 : 4;      // stages ahead: as registers allow
-    const int t = lane >> 3, r0 = (warp - 2) * 8 + (lane & 7);
-    int grid[ONE ? 1 : 4];
+    // Teams take blocks in turn: what a block costs beside its codes, mostly waits, is hidden by the
+    // other teams (16 warps on one block: 70 us for 16 tokens x 28672 x 8192).  A thread takes 32 codes
+    // of each of 4 rows: lanes 0-7 eight rows of a unit, the next eight the same rows of the next
+    // unit, ..., so that eight lanes' 16-byte loads and stores cover the banks.
+    const int t = lane >> 3, r0 = (warp % TEAM) * 8 + (lane & 7);
+    for (int it = (warp - 8) / TEAM; it < count; it += TEAMS) {
+      const int c = it % P.nc, s = it % P.na;
+      if (!wait(&cF[c], (uint32_t)(it / P.nc) & 1u)) break;
+      if (!wait(&aE[s], ((uint32_t)(it / P.na) & 1u) ^ 1u)) break;
+      const unsigned char *here = codes + c * CODES, *grid = grids + c * GRIDS * GRID;
+      unsigned char* to = smem + s * FB_A + (r0 & 63) * 128;
 #pragma unroll
-    for (int j = 0; j < (ONE ? 1 : 4); ++j) grid[j] = P.G == 1 ? 0 : min((cb * 4 + j) / P.chunks, P.G - 1);
-    auto load = [&](int it, Piece<W8, ONE>& to) {
-      const int64_t row = (int64_t)(k0 + it) * FB_K + r0;
-      const uint4* at = reinterpret_cast<const uint4*>(P.codes) +
-                        (((row >> 7) * P.kblocks + cb) * UNITS + t) * LIN_BLOCK + (row & 127);
+      for (int i = 0; i < LIN_BLOCK / 8 / TEAM; ++i) {
+        const int r = r0 + i * 8 * TEAM;
+        uint4 u[W8 ? 2 : 1];
 #pragma unroll
-      for (int h = 0; h < (W8 ? 2 : 1); ++h) to.u[h] = __ldg(at + h * 4 * LIN_BLOCK);
+        for (int h = 0; h < (W8 ? 2 : 1); ++h) u[h] = *reinterpret_cast<const uint4*>(here + ((4 * h + t) * LIN_BLOCK + r) * 16);
+        float sf[GRIDS], zf[GRIDS];
 #pragma unroll
-      for (int j = 0; j < (ONE ? 1 : 4); ++j) {
-        to.s[j] = __ldg(P.scales + grid[j] * P.mp + row);
-        to.z[j] = __ldg(P.zeros + grid[j] * P.mp + row);
-      }
-    };
-    Piece<W8, ONE> next[D];
-#pragma unroll
-    for (int q = 0; q < D; ++q)
-      if (q < nk) load(q, next[q]);
-    bool ok = true;
-    for (int base = 0; base < nk && ok; base += FB_STAGES) {
-#pragma unroll
-      for (int q = 0; q < FB_STAGES; ++q) {
-        const int it = base + q;
-        if (it >= nk || !ok) break;
-        const Piece<W8, ONE> here = next[q % D];
-        if (it + D < nk) load(it + D, next[q % D]);
-        if (base > 0 && !wait(&empty[q], (uint32_t)(base / FB_STAGES - 1) & 1u)) {
-          ok = false;
-          break;
+        for (int j = 0; j < (int)GRIDS; ++j) {
+          sf[j] = reinterpret_cast<const float*>(grid + j * GRID)[r];
+          zf[j] = (float)grid[j * GRID + LIN_BLOCK * 4 + r];
         }
-        unsigned char* a = smem + q * stage_bytes + r0 * 128;
+        unsigned char* a = to + (i * 8 * TEAM / 64) * (FB_A / 2) + (i * 8 * TEAM % 64) * 128;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float sf = here.s[ONE ? 0 : j], zf = (float)here.z[ONE ? 0 : j];
           uint32_t o[4];
           if constexpr (W8) {
-            const __half2 z = __float2half2_rn(1024.f + zf);
-            const uint32_t* w = reinterpret_cast<const uint32_t*>(&here.u[j >> 1]);
+            const __half2 z = __float2half2_rn(1024.f + zf[ONE ? 0 : j]);
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(&u[j >> 1]);
 #pragma unroll
-            for (int p = 0; p < 4; ++p) o[p] = scaled8(w[2 * (j & 1) + (p >> 1)], p & 1, z, sf);
+            for (int p = 0; p < 4; ++p) o[p] = scaled8(w[2 * (j & 1) + (p >> 1)], p & 1, z, sf[ONE ? 0 : j]);
           } else {
-            const __nv_bfloat162 z = __float2bfloat162_rn(128.f + zf), hi = __float2bfloat162_rn(sf);
-            const __nv_bfloat162 lo = __float2bfloat162_rn(sf - __low2float(hi));
-            const uint32_t w = reinterpret_cast<const uint32_t*>(&here.u[0])[j];
+            const __nv_bfloat162 z = __float2bfloat162_rn(128.f + zf[ONE ? 0 : j]), hi = __float2bfloat162_rn(sf[ONE ? 0 : j]);
+            const __nv_bfloat162 lo = __float2bfloat162_rn(sf[ONE ? 0 : j] - __low2float(hi));
+            const uint32_t w = reinterpret_cast<const uint32_t*>(&u[0])[j];
 #pragma unroll
             for (int p = 0; p < 4; ++p) o[p] = scaled(pair4(w, p, z), hi, lo);
           }
-          *reinterpret_cast<uint4*>(a + (j >> 1) * 8192 + (((4 * (j & 1) + t) ^ (r0 & 7)) << 4)) =
+          *reinterpret_cast<uint4*>(a + (j >> 1) * 8192 + (((4 * (j & 1) + t) ^ (r & 7)) << 4)) =
               make_uint4(o[0], o[1], o[2], o[3]);
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&formed[q]);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&cE[c]);
+        mbar_arrive(&aF[s]);
       }
     }
-    if (ok) wait(&done, 0);
-  }
-  // ------------------------------------------------------------ sums
-  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  __syncthreads();      // the stages are free: the CTA's sums take their place, [token][128 columns]
-  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  float* mine = reinterpret_cast<float*>(smem);
-  if (warp >= 2) {
-    const int q = warp & 3, half = (warp - 2) >> 2, each = P.bn >> 1;
-    if (nk > 0) {
-      for (int c = half * each; c < (half + 1) * each; c += 8) {
-        uint32_t r[8];
-        tmem_ld8(tmem + ((uint32_t)(q * 32) << 16) + c, r);
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------ sums
+    const int q = warp & 3;
+    int64_t u = u0;
+    for (uint32_t g = 0; u < u1; ++g) {
+      const int tile = (int)(u / P.nk);
+      const int64_t begin = (int64_t)tile * P.nk, end = begin + P.nk;
+      const bool whole = u == begin && u1 >= end;
+      const int tok0 = tile % P.token_tiles * P.bn, tokens = min(P.bn, P.rows - tok0);
+      const int col = tile / P.token_tiles * LIN_BLOCK + q * 32 + lane;
+      __nv_bfloat16* out = P.dx + (int64_t)tok0 * P.ldx + col;
+      if (!wait(&accF[g & 1u], (g >> 1) & 1u)) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      float* mine = P.part + share.slot(blockIdx.x, tile) * P.bn * LIN_BLOCK + q * 32 + lane;
+      for (int c = 0; c < tokens; c += 16) {
+        uint32_t v[16];
+        tmem_ld16(tmem + (g & 1u) * cols + ((uint32_t)(q * 32) << 16) + c, v);
         tmem_wait_ld();
 #pragma unroll
-        for (int u = 0; u < 8; ++u) mine[(c + u) * 128 + q * 32 + lane] = __uint_as_float(r[u]);
+        for (int i = 0; i < 16; ++i) {
+          if (c + i >= tokens) continue;
+          if (!whole)
+            mine[(c + i) * LIN_BLOCK] = __uint_as_float(v[i]);
+          else if (col < P.n)
+            out[(c + i) * P.ldx] = __float2bfloat16_rn(__uint_as_float(v[i]));
+        }
       }
-    } else {
-      for (int c = half * each; c < (half + 1) * each; ++c) mine[c * 128 + q * 32 + lane] = 0.f;
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&accE[g & 1u]);
+      u = min(end, u1);
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  if (splits > 1)
-    cluster.sync();
-  else
-    __syncthreads();
+  __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 1)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
-  const int tokens = min(P.bn, P.rows - tok0);
-  for (int i = part * FB_THREADS + (int)threadIdx.x; i < tokens * 16; i += splits * FB_THREADS) {
-    const int tok = i >> 4, c = (i & 15) * 8;
-    float v[8] = {};
-    for (int p = 0; p < splits; ++p) {
-      float u[8];
-      load8((splits > 1 ? cluster.map_shared_rank(mine, p) : mine) + tok * 128 + c, u);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += u[k];
-    }
-    const int col = cb * 128 + c;
-    __nv_bfloat16* out = P.dx + (int64_t)(tok0 + tok) * P.ldx + col;
-    if (P.vec && col + 8 <= P.n) {
-      store8(out, v);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (col + k < P.n) out[k] = __float2bfloat16_rn(v[k]);
-    }
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * cols) : "memory");
+}
+
+// Tiles that several CTAs share: their parts' sum.  A thread has 4 columns of a token.
+__global__ void __launch_bounds__(256) k_back_join(const FusedParams P, int ctas) {
+  pdl_wait();
+  const Shares share(P, ctas);
+  const int tile = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
+  const int tok = i >> 5, token = tile % P.token_tiles * P.bn + tok;
+  const int col = tile / P.token_tiles * LIN_BLOCK + (i & 31) * 4;
+  const int c0 = share.owner((int64_t)tile * P.nk), c1 = share.owner((int64_t)(tile + 1) * P.nk - 1);
+  if (c0 == c1 || tok >= P.bn || token >= P.rows || col >= P.n) return;
+  const float* from = P.part + (int64_t)tok * LIN_BLOCK + (i & 31) * 4;
+  const int64_t size = (int64_t)P.bn * LIN_BLOCK;
+  float4 v = *reinterpret_cast<const float4*>(from + share.slot(c0, tile) * size);
+#pragma unroll 4
+  for (int c = c0 + 1; c <= c1; ++c) {      // (a CTA between the first and the last has nothing else)
+    const float4 w = *reinterpret_cast<const float4*>(from + (int64_t)c * 2 * size);
+    v.x += w.x;
+    v.y += w.y;
+    v.z += w.z;
+    v.w += w.w;
   }
-  if (splits > 1) cluster.sync();      // nobody's shared memory goes before it is read
+  __nv_bfloat16* out = P.dx + token * P.ldx + col;
+  if (P.vec && col + 4 <= P.n) {
+    *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pack(v.x, v.y), bf16_pack(v.z, v.w));
+  } else {
+    const float o[4] = {v.x, v.y, v.z, v.w};
+    for (int k = 0; k < 4 && col + k < P.n; ++k) out[k] = __float2bfloat16_rn(o[k]);
+  }
 }
 
 // ------------------------------------------------------------------ many tokens
@@ -311,57 +380,63 @@ __global__ void __launch_bounds__(256) k_back_copy(const __nv_bfloat16* from, in
 }
 
 constexpr int FUSED_TOKENS = 512;
+constexpr uint32_t FB_SMEM = 227 * 1024 - 1024;      // beside the barriers
 
-struct BackLayout {
-  size_t dy = 0, w, bytes;
-  bool copy;
-  int64_t ldw;
-  BackLayout(const void* p, int rows, int64_t ld, int m, int n) {
-    size_t at = 256;
-    copy = !aligned16(p, rows > 1 ? ld * 2 : 0);
-    if (copy) {
-      dy = at;
-      at += align256((size_t)rows * round_up(m, 8) * 2);
-    }
-    w = at;
-    ldw = round_up(n, LIN_BLOCK);
-    bytes = rows > FUSED_TOKENS ? w + align256((size_t)m * ldw * 2) : at;
+// How few tokens are shared out.
+struct FusedPlan {
+  int bn, token_tiles, tiles, nk, ctas, teams, na, nb, nc;
+  bool shared;      // tiles by CTAs
+  size_t smem;
+  FusedPlan(int rows, int m, int n, bool bytes8, bool one) {
+    bn = (int)round_up(ceil_div(rows, ceil_div(rows, FB_MAX_BN)), 16);      // as even as tiles allow
+    token_tiles = ceil_div(rows, bn);
+    tiles = ceil_div(n, LIN_BLOCK) * token_tiles;
+    nk = ceil_div(m, LIN_BLOCK);
+    // every SM, but no fewer than 4 blocks each: a part costs its sums' way through memory
+    ctas = (int)std::max<int64_t>(1, std::min<int64_t>(ROW_SMS, (int64_t)tiles * nk / 4));
+    shared = nk > 1 && tiles % ctas != 0;      // else shares are whole tiles
+    const uint32_t tok = (uint32_t)bn * 256, code = (bytes8 ? 16384 : 8192) + LIN_BLOCK * 5 * (one ? 1 : 4);
+    auto fits = [&](int a, int b, int c) { return 1024 + a * FB_A + b * tok + c * code <= FB_SMEM; };
+    na = teams = fits(4, 2, 4) ? 4 : 2;      // (two blocks of operands always fit)
+    nb = 2;
+    nc = fits(na, nb, 4) ? 4 : 2;
+    while (nb < FB_RING && fits(na, nb + 1, nc)) ++nb;
+    smem = 1024 + na * FB_A + nb * tok + nc * code;
   }
 };
 
-constexpr uint32_t FB_SMEM_MAX = FB_STAGES * (FB_A + 256 * 128) + 1024;
+struct BackLayout {
+  size_t dy = 0, part = 0, w = 0, bytes;
+  bool copy;
+  int64_t ldw;
+  BackLayout(const void* p, int rows, int64_t ld, int m, int n, const FusedPlan& F) {
+    size_t at = 256;
+    auto take = [&](size_t b) {
+      const size_t r = at;
+      at += align256(b);
+      return r;
+    };
+    copy = !aligned16(p, rows > 1 ? ld * 2 : 0);
+    if (copy) dy = take((size_t)rows * round_up(m, 8) * 2);
+    ldw = round_up(n, LIN_BLOCK);
+    if (rows <= FUSED_TOKENS) {
+      part = take((size_t)F.ctas * 2 * F.bn * LIN_BLOCK * 4);
+    } else {
+      w = take((size_t)m * ldw * 2);
+    }
+    bytes = at;
+  }
+};
+bool one_grid(int n, int group_size) { return group_size == 0 || group_size == n || group_size % LIN_BLOCK == 0; }
 
-// Tokens of a tile: as even as tiles of at most 256 allow.
-int fused_bn(int rows) { return (int)round_up(ceil_div(rows, ceil_div(rows, 256)), 16); }
-// CTAs of a cluster: What's rows are split until two CTAs an SM are busy (one, where tiles are tall).
-int fused_splits(int rows, int m, int n) {
-  const int bn = fused_bn(rows), tiles = ceil_div(n, 128) * ceil_div(rows, bn);
-  const int slots = ROW_SMS * (2 * (FB_STAGES * (FB_A + bn * 128) + 2048) <= 227 * 1024 ? 2 : 1);
-  return std::max(1, std::min({slots / tiles, ceil_div(m, 2 * FB_K), 8}));
-}
-
-template <bool W8, bool ONE>
-cudaError_t fused_launch(const CUtensorMap& map, const FusedParams& P, int splits, cudaStream_t s) {
+template <bool W8, bool ONE, int TEAMS>
+cudaError_t fused_launch(const CUtensorMap& map, const FusedParams& P, const FusedPlan& F, cudaStream_t s) {
   static OncePerDevice once;
   const cudaError_t e = once([] {
-    return cudaFuncSetAttribute(k_back_fused<W8, ONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FB_SMEM_MAX);
+    return cudaFuncSetAttribute(k_back_fused<W8, ONE, TEAMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FB_SMEM);
   });
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(ceil_div(P.n, 128) * splits), (unsigned)ceil_div(P.rows, P.bn));
-  cfg.blockDim = dim3(FB_THREADS);
-  // the stages, or the sums that take their place
-  cfg.dynamicSmemBytes = std::max<size_t>(FB_STAGES * (FB_A + (size_t)P.bn * 128), (size_t)P.bn * 512) + 1024;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = splits;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, k_back_fused<W8, ONE>, map, P);
+  return launch_pdl(k_back_fused<W8, ONE, TEAMS>, dim3(F.ctas), dim3(FB_THREADS), F.smem, s, map, P);
 }
 
 constexpr int LB_MAX_DIM = 1 << 17, LB_MAX_ROWS = 1 << 24;
@@ -378,7 +453,9 @@ using namespace bakron;
 
 extern "C" size_t bakron_linear_backward_workspace_bytes(const void* dy, int rows, int64_t lddy, int m, int n, int qmax,
                                                          int group_size) {
-  return back_ok(rows, m, n, qmax, group_size) && rows > 0 ? BackLayout(dy, rows, lddy, m, n).bytes : 0;
+  return back_ok(rows, m, n, qmax, group_size) && rows > 0 
+             ? BackLayout(dy, rows, lddy, m, n, FusedPlan(rows, m, n, qmax > 15, one_grid(n, group_size))).bytes
+             : 0;
 }
 
 extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, const void* packed, int m, int n, int qmax,
@@ -389,7 +466,9 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
   if (!dy || !packed || !dx || lddy < m || lddx < n || (uintptr_t)packed % 16 != 0 || (uintptr_t)dy % 2 != 0 ||
       (uintptr_t)dx % 2 != 0 || !workspace || (uintptr_t)workspace % 16 != 0)
     return BAKRON_ERR_INVALID_ARG;
-  const BackLayout B(dy, rows, lddy, m, n);
+  const bool one = one_grid(n, group_size);
+  const FusedPlan plan(rows, m, n, qmax > 15, one);
+  const BackLayout B(dy, rows, lddy, m, n, plan);
   if (workspace_bytes < B.bytes) return BAKRON_ERR_WORKSPACE;
   const WeightLayout L(m, n, qmax, group_size);
   const unsigned char* p = (const unsigned char*)packed;
@@ -402,20 +481,26 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
     dy = ws + B.dy;
     lddy = round_up(m, 8);
   }
-  k_clear_status<<<1, 1, 0, s>>>((int*)ws);
-  BK_CUDA_OK(cudaGetLastError());
   const int64_t ldmap = rows > 1 ? lddy : round_up(m, 8);
   CUtensorMap a, b, o;
+  k_clear_status<<<1, 1, 0, s>>>((int*)ws);
+  BK_CUDA_OK(cudaGetLastError());
   if (rows <= FUSED_TOKENS) {
+    if (!pair_map(&a, false, dy, rows, m, ldmap, 64, plan.bn)) return BAKRON_ERR_CUDA;
     FusedParams F{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, L.mp, (int)(L.np / LIN_BLOCK),
-                  L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, rows, n, fused_bn(rows), ceil_div(m, FB_K), 0,
-                  (__nv_bfloat16*)dx, lddx, aligned16(dx, rows > 1 ? lddx * 2 : 0), (int*)ws, spin_cycles_from_env()};
-    const int splits = fused_splits(rows, m, n);
-    F.per = ceil_div(F.nk, splits);
-    if (!pair_map(&a, false, dy, rows, m, ldmap, FB_K, F.bn)) return BAKRON_ERR_CUDA;
-    const bool one = L.G == 1 || L.group % LIN_BLOCK == 0;
-    BK_CUDA_OK(L.bytes8 ? (one ? fused_launch<true, true>(a, F, splits, s) : fused_launch<true, false>(a, F, splits, s))
-                        : (one ? fused_launch<false, true>(a, F, splits, s) : fused_launch<false, false>(a, F, splits, s)));
+                  L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, rows, n, plan.bn, plan.nk, plan.token_tiles,
+                  plan.tiles, plan.na, plan.nb, plan.nc, (__nv_bfloat16*)dx, lddx, (float*)(ws + B.part),
+                  aligned16(dx, rows > 1 ? lddx * 2 : 0), (int*)ws,
+                  spin_cycles_from_env()};
+    const auto launch =
+        plan.teams == 4 ? (L.bytes8 ? (one ? fused_launch<true, true, 4> : fused_launch<true, false, 4>)
+                                    : (one ? fused_launch<false, true, 4> : fused_launch<false, false, 4>))
+                        : (L.bytes8 ? (one ? fused_launch<true, true, 2> : fused_launch<true, false, 2>)
+                                    : (one ? fused_launch<false, true, 2> : fused_launch<false, false, 2>));
+    BK_CUDA_OK(launch(a, F, plan, s));
+    if (plan.shared)
+      BK_CUDA_OK(launch_pdl(k_back_join, dim3((unsigned)ceil_div(plan.bn, 8), (unsigned)plan.tiles), dim3(256), 0, s, F,
+                            plan.ctas));
     return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
   }
   ExpandParams E{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, m, (int)(L.np / LIN_BLOCK),
