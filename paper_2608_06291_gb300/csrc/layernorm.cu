@@ -180,20 +180,32 @@ __device__ __forceinline__ void two_all(float& a, float& b, float2* slots) {
 
 // A CTA takes the rows blockIdx.x, + gridDim.x, ...; both parameters' gradients stay in registers
 // from row to row and leave as one part per CTA.  A row is read three times (mean, sums of what
-// is left, dx), from a ring of RING rows in shared memory that vector copies fill ahead; a
-// thread reads back only what it copied.  Rows that vectors cannot be used for (RING 1) are
-// copied when their turn comes.
+// is left, dx) from shared memory, and a thread reads back only what it put there.  Many rows
+// that vectors can be used for: four groups of 8 a thread, a ring of RING rows that vector copies
+// fill ahead, the weight in registers (the ring leaves little of the SM's memory to its cache).
+// Else (RING 1): no more than two groups a thread, more threads, a row when its turn comes.
 constexpr int LB_VPT = 4;
 
-template <typename T, typename W, bool VEC, int RING, int MAXT>
-__global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const LayerBackParams P) {
-  constexpr int VPT = LB_VPT;
+template <typename T, typename W, bool VEC, int RING, int VPT, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 2 : 1) k_layernorm_back(const LayerBackParams P) {
+  constexpr bool KEEP_W = VPT == LB_VPT;
   static_assert(VEC || RING == 1, "whole vectors");
-  __shared__ float2 slots[2][16];
+  __shared__ float2 slots[2][32];
   extern __shared__ __align__(16) unsigned char lb_ring[];   // [RING][h, dy, dsum][d]
   const int t = threadIdx.x, nt = blockDim.x;
   pdl_trigger();      // the parts' sum may get ready; it waits for this grid's end
   float dw[VPT][8] = {}, db[VPT][8] = {};
+  Raw8<W> weight[KEEP_W ? VPT : 1];
+  if constexpr (KEEP_W) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) raw_load<VEC>((const W*)P.w, i, t, nt, P.d, weight[i]);
+  }
+  auto get_w = [&](int i, float (&w)[8]) {
+    if constexpr (KEEP_W)
+      weight[i].get(w);
+    else
+      row_load<VEC>((const W*)P.w, i, t, nt, P.d, w);
+  };
   int slot = 0;
   T* ring = reinterpret_cast<T*>(lb_ring);
   auto fetch = [&](int64_t row, int to) {      // each thread its own groups
@@ -247,7 +259,7 @@ __global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const Layer
       float a[8], b[8], w[8];
       row_load<VEC>(here, i, t, nt, P.d, a);
       row_load<VEC>(here + P.d, i, t, nt, P.d, b);
-      row_load<VEC>((const W*)P.w, i, t, nt, P.d, w);
+      get_w(i, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         mu += a[j];
@@ -263,7 +275,7 @@ __global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const Layer
       float a[8], b[8], w[8];
       row_load<VEC>(here, i, t, nt, P.d, a);
       row_load<VEC>(here + P.d, i, t, nt, P.d, b);
-      row_load<VEC>((const W*)P.w, i, t, nt, P.d, w);
+      get_w(i, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float c = inside<VEC>(i, j, t, nt, P.d) ? a[j] - mu : 0.f;
@@ -278,7 +290,7 @@ __global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const Layer
       float a[8], b[8], w[8], o[8];
       row_load<VEC>(here, i, t, nt, P.d, a);
       row_load<VEC>(here + P.d, i, t, nt, P.d, b);
-      row_load<VEC>((const W*)P.w, i, t, nt, P.d, w);
+      get_w(i, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float c = a[j] - mu;
@@ -359,51 +371,48 @@ __global__ void __launch_bounds__(256) k_layernorm_dwb(const LayerBackParams P) 
   P.part[((int64_t)blockIdx.y * 2 + 1) * P.d + e] = b;
 }
 
-// Threads of a CTA (0: rows too long), and CTAs, each with its part: what an SM holds.
+// The launch: groups of 8 a thread (0: rows too long), threads, rows of the ring, CTAs an SM.
 constexpr int LB_SMEM = 220 * 1024;      // of an SM's, beside each CTA's kilobyte
-int layer_threads(int d) {
-  const int nt = (int)round_up(ceil_div(ceil_div(d, 8), LB_VPT), 32);
-  return nt <= 512 ? nt : 0;
-}
+constexpr int LB_MANY = 2 * ROW_SMS;     // rows; up to here a row's latency counts, not what an SM holds
 struct LayerPlan {
-  int ring, ctas;      // rows of the ring, CTAs of an SM
-  LayerPlan(int d, int es, bool vec) {
-    const int nt = layer_threads(d), row = 3 * d * es;
-    ring = !vec || 2 * row > LB_SMEM ? 1 : nt > 256 || 2 * 3 * row > LB_SMEM ? 2 : 3;
-    ctas = nt ? std::max(1, std::min(512 / nt, LB_SMEM / (ring * row + 1024))) : 4;
+  int vpt, nt, ring, ctas;
+  LayerPlan(int rows, int d, int es, bool vec) {
+    const int groups = ceil_div(d, 8), row = 3 * d * es;
+    ring = 1;
+    vpt = groups > 2048 ? 0 : groups > 1024 ? 2 : 1;
+    if (vpt && vec && rows > LB_MANY && 2 * row <= LB_SMEM) {
+      vpt = LB_VPT;
+      ring = groups > 1024 || 2 * 3 * row > LB_SMEM ? 2 : 3;
+    }
+    nt = vpt ? (int)round_up(ceil_div(groups, vpt), 32) : 256;
+    ctas = vpt ? std::max(1, std::min((vpt == LB_VPT ? 512 : 1024) / nt, LB_SMEM / (ring * row + 1024))) : 4;
   }
+  int parts(int rows) const { return std::min(rows, ROW_SMS * ctas); }
 };
-int layer_parts(int rows, int d, int es, bool vec) {
-  return std::min(rows, ROW_SMS * LayerPlan(d, es, vec).ctas);
-}
 
 template <typename T, typename W>
-cudaError_t layer_back_launch(const LayerBackParams& P, cudaStream_t s) {
-  const int nt = layer_threads(P.d), ring = LayerPlan(P.d, sizeof(T), P.vec).ring;
-  if (!nt) {
+cudaError_t layer_back_launch(const LayerBackParams& P, const LayerPlan& L, cudaStream_t s) {
+  if (!L.vpt) {
     k_layernorm_dx<T><<<P.rows, 256, 0, s>>>(P);
     k_layernorm_dwb<T><<<dim3((unsigned)ceil_div(P.d, 256), (unsigned)P.parts), 256, 0, s>>>(P);
     return cudaGetLastError();
   }
-  auto kernel = k_layernorm_back<T, W, false, 1, 512>;
-  if (P.vec)
-    kernel = nt > 256 ? (ring == 1 ? k_layernorm_back<T, W, true, 1, 512> : k_layernorm_back<T, W, true, 2, 512>)
-             : ring == 1 ? k_layernorm_back<T, W, true, 1, 256>
-             : ring == 2 ? k_layernorm_back<T, W, true, 2, 256> : k_layernorm_back<T, W, true, 3, 256>;
-  else if (nt <= 256)
-    kernel = k_layernorm_back<T, W, false, 1, 256>;
   static OncePerDevice once;
   const cudaError_t e = once([] {
     cudaError_t a = cudaSuccess;
-    for (auto k : {k_layernorm_back<T, W, false, 1, 256>, k_layernorm_back<T, W, false, 1, 512>,
-                   k_layernorm_back<T, W, true, 1, 256>, k_layernorm_back<T, W, true, 1, 512>,
-                   k_layernorm_back<T, W, true, 2, 256>, k_layernorm_back<T, W, true, 2, 512>,
-                   k_layernorm_back<T, W, true, 3, 256>})
+    for (auto k : {k_layernorm_back<T, W, false, 1, 1, 1024>, k_layernorm_back<T, W, false, 1, 2, 1024>,
+                   k_layernorm_back<T, W, true, 1, 1, 1024>, k_layernorm_back<T, W, true, 1, 2, 1024>,
+                   k_layernorm_back<T, W, true, 2, LB_VPT, 256>, k_layernorm_back<T, W, true, 2, LB_VPT, 512>,
+                   k_layernorm_back<T, W, true, 3, LB_VPT, 256>})
       if (a == cudaSuccess) a = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, LB_SMEM);
     return a;
   });
   if (e != cudaSuccess) return e;
-  kernel<<<P.parts, nt, (size_t)ring * 3 * P.d * sizeof(T), s>>>(P);
+  const auto kernel = L.vpt == 1   ? (P.vec ? k_layernorm_back<T, W, true, 1, 1, 1024> : k_layernorm_back<T, W, false, 1, 1, 1024>)
+                      : L.vpt == 2 ? (P.vec ? k_layernorm_back<T, W, true, 1, 2, 1024> : k_layernorm_back<T, W, false, 1, 2, 1024>)
+                      : L.nt > 256 ? k_layernorm_back<T, W, true, 2, LB_VPT, 512>
+                      : L.ring == 2 ? k_layernorm_back<T, W, true, 2, LB_VPT, 256> : k_layernorm_back<T, W, true, 3, LB_VPT, 256>;
+  kernel<<<P.parts, L.nt, (size_t)L.ring * 3 * P.d * sizeof(T), s>>>(P);
   return cudaGetLastError();
 }
 
@@ -467,7 +476,7 @@ extern "C" size_t bakron_layernorm_backward_workspace_bytes(int rows, int d) {
   if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
   int parts = 0;      // whichever way the call goes
   for (int es : {2, 4})
-    for (bool vec : {false, true}) parts = std::max(parts, layer_parts(rows, d, es, vec));
+    for (bool vec : {false, true}) parts = std::max(parts, LayerPlan(rows, d, es, vec).parts(rows));
   return align256((size_t)rows * 8) + (size_t)parts * d * 8 + 256;
 }
 
@@ -492,12 +501,13 @@ extern "C" int bakron_layernorm_backward(const void* dy, int64_t lddy, const voi
     const int es = dtype == BAKRON_F32 ? 4 : 2;
     P.vec = d % 8 == 0 && aligned16(dy, lddy * es) && aligned16(h, ldh * es) && (!dsum || aligned16(dsum, ldds * es)) &&
             aligned16(dx, lddx * es) && aligned16(weight, 0);
-    P.parts = layer_parts(rows, d, es, P.vec);
+    const LayerPlan L(rows, d, es, P.vec);
+    P.parts = L.parts(rows);
     const auto launch = dtype == BAKRON_F32
                             ? (P.wbf16 ? layer_back_launch<float, __nv_bfloat16> : layer_back_launch<float, float>)
                             : (P.wbf16 ? layer_back_launch<__nv_bfloat16, __nv_bfloat16>
                                        : layer_back_launch<__nv_bfloat16, float>);
-    BK_CUDA_OK(launch(P, s));
+    BK_CUDA_OK(launch(P, L, s));
   }
   BK_CUDA_OK(launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(d, 32), 2), dim3(32, 32), 0, s, P.part, P.parts, d, dw, db));
   return BAKRON_OK;
