@@ -179,16 +179,145 @@ __device__ __forceinline__ void two_all(float& a, float& b, float2* slots) {
 }
 
 // A CTA takes the rows blockIdx.x, + gridDim.x, ...; both parameters' gradients stay in registers
-// from row to row and leave as one part per CTA.  A row is read three times (mean, sums of what
-// is left, dx) from shared memory, and a thread reads back only what it put there.  Many rows
-// that vectors can be used for: four groups of 8 a thread, a ring of RING rows that vector copies
-// fill ahead, the weight in registers (the ring leaves little of the SM's memory to its cache).
-// Else (RING 1): no more than two groups a thread, more threads, a row when its turn comes.
-constexpr int LB_VPT = 4;
+// from row to row and leave as one part per CTA.
+//
+// Many rows of up to 8192 elements that vectors can be used for: 16 elements a thread, read once
+// from a ring of RING rows that vector copies fill ahead, and kept in fp32, as pairs, through the three
+// passes (mean, sums of what is left, dx).  What bounds it is instructions before it is memory: with the
+// row read back from shared memory and widened in each pass, one value an instruction, 8192 x 4096
+// in bf16 with dsum took 98 us.
+constexpr int LB_GROUPS = 1024;      // groups of 8: 512 threads
+template <typename T, typename W, int RING, int MAXT>
+__global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const LayerBackParams P) {
+  __shared__ float2 slots[2][32];
+  extern __shared__ __align__(16) unsigned char lb_ring[];   // [RING][h, dy, dsum][d]
+  const int t = threadIdx.x, nt = blockDim.x;
+  pdl_trigger();      // the parts' sum may get ready; it waits for this grid's end
+  auto pairs = [](const float (&v)[8], Two* p) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = Two(v[2 * j], v[2 * j + 1]);
+  };
+  const Two zero(0.f, 0.f);
+  Two w[8], dw[8], db[8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float v[8];
+    row_load<true>((const W*)P.w, i, t, nt, P.d, v);
+    pairs(v, w + 4 * i);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) dw[j] = db[j] = zero;
+  T* ring = reinterpret_cast<T*>(lb_ring);
+  auto fetch = [&](int64_t row, int to) {      // each thread its own groups
+    T* at = ring + (int64_t)to * 3 * P.d;
+    if (row < P.rows) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int e0 = elem<true>(i, 0, t, nt);
+        if (e0 >= P.d) continue;
+#pragma unroll
+        for (int k = 0; k < 8; k += 16 / (int)sizeof(T)) {
+          copy16(at + e0 + k, (const T*)P.h + row * P.ldh + e0 + k);
+          copy16(at + P.d + e0 + k, (const T*)P.dy + row * P.lddy + e0 + k);
+          if (P.dsum) copy16(at + 2 * P.d + e0 + k, (const T*)P.dsum + row * P.ldds + e0 + k);
+        }
+      }
+    }
+    copies_group();
+  };
+#pragma unroll
+  for (int s = 0; s < RING - 1; ++s) fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+  const float inv = 1.f / (float)P.d;
+  int slot = 0;
+  for (int64_t row = blockIdx.x; row < P.rows; row += gridDim.x) {
+    const T* here = ring + (int64_t)slot * 3 * P.d;
+    copies_left<RING - 2>();
+    fetch(row + (int64_t)(RING - 1) * gridDim.x, slot == 0 ? RING - 1 : slot - 1);
+    slot = slot == RING - 1 ? 0 : slot + 1;
+    Two c[8], b[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float v[8];
+      row_load<true>(here, i, t, nt, P.d, v);
+      pairs(v, c + 4 * i);
+      row_load<true>(here + P.d, i, t, nt, P.d, v);
+      pairs(v, b + 4 * i);
+    }
+    Two s0 = c[0], s1 = Two::mul(w[0], b[0]);
+#pragma unroll
+    for (int j = 1; j < 8; ++j) {
+      s0 = Two::add(s0, c[j]);
+      s1 = Two::fma(w[j], b[j], s1);
+    }
+    float mu, mg, ss, gc, hi;
+    s0.get(mu, hi);
+    mu += hi;
+    s1.get(mg, hi);
+    mg += hi;
+    two_all(mu, mg, slots[0]);
+    mu *= inv;
+    mg *= inv;
+    const Two minus_mu(-mu, -mu);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bool in = elem<true>(i, 0, t, nt) < P.d;
+#pragma unroll
+      for (int j = 4 * i; j < 4 * i + 4; ++j) c[j] = in ? Two::add(c[j], minus_mu) : zero;
+    }
+    s0 = Two::mul(c[0], c[0]);
+    s1 = Two::mul(Two::mul(w[0], b[0]), c[0]);
+#pragma unroll
+    for (int j = 1; j < 8; ++j) {
+      s0 = Two::fma(c[j], c[j], s0);
+      s1 = Two::fma(Two::mul(w[j], b[j]), c[j], s1);
+    }
+    s0.get(ss, hi);
+    ss += hi;
+    s1.get(gc, hi);
+    gc += hi;
+    two_all(ss, gc, slots[1]);
+    const float rho = 1.f / sqrtf(ss * inv + P.eps), k = rho * rho * (gc * inv);
+    const Two rr(rho, rho), minus_k(-k, -k), minus_mg(-mg, -mg);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float o[8];
+#pragma unroll
+      for (int j = 4 * i; j < 4 * i + 4; ++j) {
+        dw[j] = Two::fma(Two::mul(b[j], c[j]), rr, dw[j]);
+        db[j] = Two::add(db[j], b[j]);
+        const Two v = Two::mul(rr, Two::fma(minus_k, c[j], Two::fma(w[j], b[j], minus_mg)));
+        v.get(o[2 * (j & 3)], o[2 * (j & 3) + 1]);
+      }
+      if (P.dsum) {
+        float v[8];
+        row_load<true>(here + 2 * P.d, i, t, nt, P.d, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] += v[j];
+      }
+      row_store<true>((T*)P.dx + row * P.lddx, i, t, nt, P.d, o);
+    }
+  }
+  float* part = P.part + (int64_t)blockIdx.x * 2 * P.d;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float v[8], u[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      dw[4 * i + j].get(v[2 * j], v[2 * j + 1]);
+      db[4 * i + j].get(u[2 * j], u[2 * j + 1]);
+    }
+    row_store<true>(part, i, t, nt, P.d, v);
+    row_store<true>(part + P.d, i, t, nt, P.d, u);
+  }
+}
 
-template <typename T, typename W, bool VEC, int RING, int VPT, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 2 : 1) k_layernorm_back(const LayerBackParams P) {
-  constexpr bool KEEP_W = VPT == LB_VPT;
+// Longer rows, and rows that vectors cannot be used for: up to 1024 threads, so 64 registers.  A row is
+// read three times from shared memory, and a thread reads back only what it put there; a ring where
+// vectors can be used (with the weight in registers: it leaves little of the SM's memory to its cache),
+// else a row (RING 1) is copied when its turn comes.
+template <typename T, typename W, bool VEC, int RING, int VPT>
+__global__ void __launch_bounds__(1024) k_layernorm_back_wide(const LayerBackParams P) {
+  constexpr bool KEEP_W = RING > 1;
   static_assert(VEC || RING == 1, "whole vectors");
   __shared__ float2 slots[2][32];
   extern __shared__ __align__(16) unsigned char lb_ring[];   // [RING][h, dy, dsum][d]
@@ -319,29 +448,60 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 2 : 1) k_layernorm_back(co
     }
 }
 
-// Rows too long for that: dx of a row, and its mean and rho for the parameters' gradients.
 template <typename T>
-__global__ void __launch_bounds__(256) k_layernorm_dx(const LayerBackParams P) {
-  __shared__ float2 slots[2][16];
+__device__ __forceinline__ void load_n(const T* p, float (&v)[1]) { v[0] = to_f32(*p); }
+template <typename T>
+__device__ __forceinline__ void load_n(const T* p, float (&v)[8]) { load8(p, v); }
+
+// dx of a row, and its mean and rho for the parameters' gradients: rows too long for that, and few
+// rows, where what counts is to start early and to run short loops (the kernel above unrolls 16
+// elements three times; executed once, its instructions come from memory: 37 x 11003 in fp32 40 us).
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(1024) k_layernorm_dx(const LayerBackParams P) {
+  constexpr int N = VEC ? 8 : 1;
+  __shared__ float2 slots[2][32];
   const int64_t row = blockIdx.x;
   const T* h = (const T*)P.h + row * P.ldh;
   const T* dy = (const T*)P.dy + row * P.lddy;
-  auto grad = [&](int e) {
-    return (P.wbf16 ? to_f32(((const __nv_bfloat16*)P.w)[e]) : ((const float*)P.w)[e]) * to_f32(dy[e]);
+  auto grad = [&](int e, float (&g)[N]) {
+    float w[N];
+    load_n(dy + e, g);
+    if (P.wbf16)
+      load_n((const __nv_bfloat16*)P.w + e, w);
+    else
+      load_n((const float*)P.w + e, w);
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[j] *= w[j];
   };
+  pdl_trigger();
   const float inv = 1.f / (float)P.d;
+  const int step = blockDim.x * N;
   float mu = 0.f, mg = 0.f, ss = 0.f, gc = 0.f;
-  for (int e = threadIdx.x; e < P.d; e += blockDim.x) {
-    mu += to_f32(h[e]);
-    mg += grad(e);
+#pragma unroll 2
+  for (int e = threadIdx.x * N; e < P.d; e += step) {
+    float a[N], g[N];
+    load_n(h + e, a);
+    grad(e, g);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      mu += a[j];
+      mg += g[j];
+    }
   }
   two_all(mu, mg, slots[0]);
   mu *= inv;
   mg *= inv;
-  for (int e = threadIdx.x; e < P.d; e += blockDim.x) {
-    const float c = to_f32(h[e]) - mu;
-    ss = fmaf(c, c, ss);
-    gc = fmaf(grad(e), c, gc);
+#pragma unroll 2
+  for (int e = threadIdx.x * N; e < P.d; e += step) {
+    float a[N], g[N];
+    load_n(h + e, a);
+    grad(e, g);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float c = a[j] - mu;
+      ss = fmaf(c, c, ss);
+      gc = fmaf(g[j], c, gc);
+    }
   }
   two_all(ss, gc, slots[1]);
   const float rho = 1.f / sqrtf(ss * inv + P.eps), k = rho * rho * (gc * inv);
@@ -349,10 +509,47 @@ __global__ void __launch_bounds__(256) k_layernorm_dx(const LayerBackParams P) {
     P.stats[2 * row] = mu;
     P.stats[2 * row + 1] = rho;
   }
-  for (int e = threadIdx.x; e < P.d; e += blockDim.x) {
-    float v = rho * fmaf(-k, to_f32(h[e]) - mu, grad(e) - mg);
-    if (P.dsum) v += to_f32(((const T*)P.dsum + row * P.ldds)[e]);
-    ((T*)P.dx + row * P.lddx)[e] = from_f32<T>(v);
+#pragma unroll 2
+  for (int e = threadIdx.x * N; e < P.d; e += step) {
+    float a[N], g[N];
+    load_n(h + e, a);
+    grad(e, g);
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[j] = rho * fmaf(-k, a[j] - mu, g[j] - mg);
+    if (P.dsum) {
+      load_n((const T*)P.dsum + row * P.ldds + e, a);
+#pragma unroll
+      for (int j = 0; j < N; ++j) g[j] += a[j];
+    }
+    if constexpr (VEC)
+      store8((T*)P.dx + row * P.lddx + e, g);
+    else
+      ((T*)P.dx + row * P.lddx)[e] = from_f32<T>(g[0]);
+  }
+}
+
+// Few rows: dw and db from the rows themselves, joined as k_sum_parts joins parts.
+template <typename T>
+__global__ void __launch_bounds__(1024) k_layernorm_sums(const LayerBackParams P, float* dw, float* db) {
+  __shared__ float s[2][32][33];
+  const int c = blockIdx.x * 32 + threadIdx.x;
+  pdl_wait();
+  float v = 0.f, b = 0.f;
+  if (c < P.d)
+    for (int64_t row = threadIdx.y; row < P.rows; row += 32) {
+      const float dy = to_f32(((const T*)P.dy + row * P.lddy)[c]);
+      v = fmaf(dy * (to_f32(((const T*)P.h + row * P.ldh)[c]) - P.stats[2 * row]), P.stats[2 * row + 1], v);
+      b += dy;
+    }
+  s[0][threadIdx.y][threadIdx.x] = v;
+  s[1][threadIdx.y][threadIdx.x] = b;
+  __syncthreads();
+  v = warp_all(s[0][threadIdx.x][threadIdx.y], AddOp());
+  b = warp_all(s[1][threadIdx.x][threadIdx.y], AddOp());
+  const int at = blockIdx.x * 32 + threadIdx.y;
+  if (threadIdx.x == 0 && at < P.d) {
+    dw[at] = v;
+    db[at] = b;
   }
 }
 
@@ -371,47 +568,57 @@ __global__ void __launch_bounds__(256) k_layernorm_dwb(const LayerBackParams P) 
   P.part[((int64_t)blockIdx.y * 2 + 1) * P.d + e] = b;
 }
 
-// The launch: groups of 8 a thread (0: rows too long), threads, rows of the ring, CTAs an SM.
-constexpr int LB_SMEM = 220 * 1024;      // of an SM's, beside each CTA's kilobyte
-constexpr int LB_MANY = 2 * ROW_SMS;     // rows; up to here a row's latency counts, not what an SM holds
+// The launch: groups of 8 a thread (0: dx by itself), threads, rows of the ring, CTAs an SM.
+constexpr int LB_SMEM = 220 * 1024;      // of an SM, with a kilobyte and the slots beside each ring
+constexpr int LB_FEW = 2 * ROW_SMS;      // rows: up to here, no loop over rows
 struct LayerPlan {
+  bool few, paired;
   int vpt, nt, ring, ctas;
   LayerPlan(int rows, int d, int es, bool vec) {
     const int groups = ceil_div(d, 8), row = 3 * d * es;
+    few = rows <= LB_FEW;
     ring = 1;
-    vpt = groups > 2048 ? 0 : groups > 1024 ? 2 : 1;
-    if (vpt && vec && rows > LB_MANY && 2 * row <= LB_SMEM) {
-      vpt = LB_VPT;
-      ring = groups > 1024 || 2 * 3 * row > LB_SMEM ? 2 : 3;
-    }
-    nt = vpt ? (int)round_up(ceil_div(groups, vpt), 32) : 256;
-    ctas = vpt ? std::max(1, std::min((vpt == LB_VPT ? 512 : 1024) / nt, LB_SMEM / (ring * row + 1024))) : 4;
+    vpt = few || groups > 2048 ? 0 : groups > 1024 ? 2 : 1;
+    if (vpt && vec && 2 * row <= LB_SMEM) vpt = ring = 2;
+    paired = ring == 2 && groups <= LB_GROUPS;
+    nt = vpt ? (int)round_up(ceil_div(groups, vpt), 32) : few ? (int)std::min<int64_t>(1024, round_up(vec ? groups : ceil_div(d, 4), 32)) : 256;
+    ctas = vpt ? std::max(1, std::min((paired ? 512 : 1024) / nt, LB_SMEM / (ring * row + 1536))) : 4;
+    while (ring > 1 && ring < (paired ? 4 : 2) && ctas * ((ring + 1) * row + 1536) <= LB_SMEM) ++ring;
   }
-  int parts(int rows) const { return std::min(rows, ROW_SMS * ctas); }
+  int parts(int rows) const { return few ? 0 : std::min(rows, ROW_SMS * ctas); }
 };
 
 template <typename T, typename W>
 cudaError_t layer_back_launch(const LayerBackParams& P, const LayerPlan& L, cudaStream_t s) {
   if (!L.vpt) {
-    k_layernorm_dx<T><<<P.rows, 256, 0, s>>>(P);
-    k_layernorm_dwb<T><<<dim3((unsigned)ceil_div(P.d, 256), (unsigned)P.parts), 256, 0, s>>>(P);
+    if (P.vec)
+      k_layernorm_dx<T, true><<<P.rows, L.nt, 0, s>>>(P);
+    else
+      k_layernorm_dx<T, false><<<P.rows, L.nt, 0, s>>>(P);
+    if (!L.few) k_layernorm_dwb<T><<<dim3((unsigned)ceil_div(P.d, 256), (unsigned)P.parts), 256, 0, s>>>(P);
     return cudaGetLastError();
   }
   static OncePerDevice once;
   const cudaError_t e = once([] {
     cudaError_t a = cudaSuccess;
-    for (auto k : {k_layernorm_back<T, W, false, 1, 1, 1024>, k_layernorm_back<T, W, false, 1, 2, 1024>,
-                   k_layernorm_back<T, W, true, 1, 1, 1024>, k_layernorm_back<T, W, true, 1, 2, 1024>,
-                   k_layernorm_back<T, W, true, 2, LB_VPT, 256>, k_layernorm_back<T, W, true, 2, LB_VPT, 512>,
-                   k_layernorm_back<T, W, true, 3, LB_VPT, 256>})
+    for (auto k : {k_layernorm_back<T, W, 2, 256>, k_layernorm_back<T, W, 3, 256>, k_layernorm_back<T, W, 4, 256>,
+                   k_layernorm_back<T, W, 2, 512>, k_layernorm_back<T, W, 3, 512>, k_layernorm_back<T, W, 4, 512>,
+                   k_layernorm_back_wide<T, W, false, 1, 1>, k_layernorm_back_wide<T, W, false, 1, 2>,
+                   k_layernorm_back_wide<T, W, true, 1, 2>, k_layernorm_back_wide<T, W, true, 2, 2>})
       if (a == cudaSuccess) a = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, LB_SMEM);
     return a;
   });
   if (e != cudaSuccess) return e;
-  const auto kernel = L.vpt == 1   ? (P.vec ? k_layernorm_back<T, W, true, 1, 1, 1024> : k_layernorm_back<T, W, false, 1, 1, 1024>)
-                      : L.vpt == 2 ? (P.vec ? k_layernorm_back<T, W, true, 1, 2, 1024> : k_layernorm_back<T, W, false, 1, 2, 1024>)
-                      : L.nt > 256 ? k_layernorm_back<T, W, true, 2, LB_VPT, 512>
-                      : L.ring == 2 ? k_layernorm_back<T, W, true, 2, LB_VPT, 256> : k_layernorm_back<T, W, true, 3, LB_VPT, 256>;
+  auto kernel = L.ring == 2 ? k_layernorm_back_wide<T, W, true, 2, 2>
+                            : k_layernorm_back_wide<T, W, true, 1, 2>;      // fp32 rows so long that a ring holds one
+  if (!P.vec)
+    kernel = L.vpt == 1 ? k_layernorm_back_wide<T, W, false, 1, 1> : k_layernorm_back_wide<T, W, false, 1, 2>;
+  else if (L.paired && L.nt <= 256)
+    kernel = L.ring == 2   ? k_layernorm_back<T, W, 2, 256>
+             : L.ring == 3 ? k_layernorm_back<T, W, 3, 256> : k_layernorm_back<T, W, 4, 256>;
+  else if (L.paired)
+    kernel = L.ring == 2   ? k_layernorm_back<T, W, 2, 512>
+             : L.ring == 3 ? k_layernorm_back<T, W, 3, 512> : k_layernorm_back<T, W, 4, 512>;
   kernel<<<P.parts, L.nt, (size_t)L.ring * 3 * P.d * sizeof(T), s>>>(P);
   return cudaGetLastError();
 }
@@ -509,6 +716,10 @@ extern "C" int bakron_layernorm_backward(const void* dy, int64_t lddy, const voi
                                        : layer_back_launch<__nv_bfloat16, float>);
     BK_CUDA_OK(launch(P, L, s));
   }
-  BK_CUDA_OK(launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(d, 32), 2), dim3(32, 32), 0, s, P.part, P.parts, d, dw, db));
+  if (rows > 0 && rows <= LB_FEW)
+    BK_CUDA_OK(launch_pdl(dtype == BAKRON_F32 ? k_layernorm_sums<float> : k_layernorm_sums<__nv_bfloat16>,
+                          dim3((unsigned)ceil_div(d, 32)), dim3(32, 32), 0, s, P, dw, db));
+  else
+    BK_CUDA_OK(launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(d, 32), 2), dim3(32, 32), 0, s, P.part, P.parts, d, dw, db));
   return BAKRON_OK;
 }

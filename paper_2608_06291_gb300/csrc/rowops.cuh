@@ -75,6 +75,11 @@ struct Two {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
     return r;
   }
+  __device__ __forceinline__ static Two mul(const Two& a, const Two& b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+  }
 };
 
 struct AddOp {
