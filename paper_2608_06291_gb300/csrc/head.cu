@@ -18,6 +18,7 @@
 // (h's) row.
 #include <algorithm>
 
+#include "linear.cuh"
 #include "pair_gemm.cuh"
 
 namespace bakron {
@@ -97,6 +98,7 @@ __global__ void __launch_bounds__(256) k_head_join(const JoinParams P) {
   __shared__ float red[3][N][R];
   const int r = threadIdx.x % R, n = threadIdx.x / R, row = blockIdx.x * R + r;
   const bool in = row < P.rows;
+  pdl_wait();
   float m = LOWEST;
   if (in)
     for (int p = n; p < P.parts; p += N) m = max_nan(m, P.m[(int64_t)p * P.rows + row]);
@@ -245,6 +247,7 @@ __global__ void __launch_bounds__(128) k_head_more(const int64_t* targets, const
 __global__ void __launch_bounds__(256) k_head_dh(const float* part, int splits, int64_t ldp, const int64_t* targets,
                                                  const float* own, const __nv_bfloat16* w, int64_t ldw, int rows,
                                                  int d, int v, __nv_bfloat16* dh, int64_t lddh) {
+  pdl_wait();
   const int row = blockIdx.x;
   const int64_t target = targets ? targets[row] : -1;
   const bool scored = target >= 0 && target < v;
@@ -330,8 +333,14 @@ struct HeadBackLayout {
     piece = (int)std::min<int64_t>(v, round_up(ceil_div(v, pieces), 256));
     ldg = round_up(piece, 8);
     ldp = round_up(d, 4);
+    // dh's sum runs over the piece in `splits` ranges: what the busiest pair takes, a range costing
+    // some 4 blocks beside its own (2048 tokens x 128256 x 4096 by 2 ranges 4.00 ms forward and back, by 4 3.86)
     const int64_t tiles = (int64_t)ceil_div(rows, PG_M) * ceil_div(d, 256);
-    splits = (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(2 * PG_PAIRS, (int)std::min<int64_t>(tiles, 1 << 20)), ceil_div(piece, 8 * PG_K), 32}));
+    const int nk = ceil_div(piece, PG_K);
+    auto cost = [&](int s) { return (tiles * s + PG_PAIRS - 1) / PG_PAIRS * (ceil_div(nk, s) + 4); };
+    splits = 1;
+    for (int s = 2; s <= std::min(32, nk); ++s)
+      if (cost(s) * 50 < cost(splits) * 49) splits = s;
     own = c.take((size_t)rows * 4);
     if (dw) {
       first = c.take((size_t)v * 4);
@@ -387,7 +396,8 @@ extern "C" int bakron_head_logprobs(const void* h, int64_t ldh, const void* weig
   if (workspace_bytes < L.bytes) return BAKRON_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)stream;
   char* ws = (char*)workspace;
-  BK_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(int), s));
+  k_clear_status<<<1, 1, 0, s>>>((int*)ws);
+  BK_CUDA_OK(cudaGetLastError());
   if (L.copy_h) {
     BK_CUDA_OK(copy_rows(h, ldh, rows, d, ws + L.h, s));
     h = ws + L.h;
@@ -410,11 +420,8 @@ extern "C" int bakron_head_logprobs(const void* h, int64_t ldh, const void* weig
                      (float*)(ws + L.picked), n, v};
     BK_CUDA_OK((pair_launch<EpiLse, false, false>(a, b, b, S, E, s)));
     JoinParams J{E.targets, E.m, E.s, E.x, E.picked, 2 * S.tn, n, v, logp ? logp + r0 : nullptr, entropy + r0, lse + r0};
-    if (n < 64)
-      k_head_join<1><<<n, 256, 0, s>>>(J);
-    else
-      k_head_join<16><<<ceil_div(n, 16), 256, 0, s>>>(J);
-    BK_CUDA_OK(cudaGetLastError());
+    BK_CUDA_OK(n < 64 ? launch_pdl(k_head_join<1>, dim3(n), dim3(256), 0, s, J)
+                      : launch_pdl(k_head_join<16>, dim3(ceil_div(n, 16)), dim3(256), 0, s, J));
   }
   return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
 }
@@ -444,7 +451,8 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
   const HeadBackLayout L(h, ldh, weight, ldw, rows, v, d, dweight != nullptr);
   if (workspace_bytes < L.bytes) return BAKRON_ERR_WORKSPACE;
   char* ws = (char*)workspace;
-  BK_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(int), s));
+  k_clear_status<<<1, 1, 0, s>>>((int*)ws);
+  BK_CUDA_OK(cudaGetLastError());
   if (L.copy_h) {
     BK_CUDA_OK(copy_rows(h, ldh, rows, d, ws + L.h, s));
     h = ws + L.h;
@@ -507,9 +515,8 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
     EpiBf16::Params B{dw_tma ? nullptr : c, lddw, count, d, near ? first + v0 : nullptr, more, L.ldp};
     BK_CUDA_OK((pair_launch<EpiBf16, true, true>(a, b, dw_tma ? o : a, S, B, s)));
   }
-  k_head_dh<<<dim3((unsigned)rows, (unsigned)std::min(ceil_div(d, 256), 8)), 256, 0, s>>>(
-      part, L.splits, L.ldp, dlogp ? targets : nullptr, own, (const __nv_bfloat16*)weight, ldw, rows, d, v,
-      (__nv_bfloat16*)dh, lddh);
-  BK_CUDA_OK(cudaGetLastError());
+  BK_CUDA_OK(launch_pdl(k_head_dh, dim3((unsigned)rows, (unsigned)std::min(ceil_div(d, 256), 8)), dim3(256), 0, s, part,
+                        L.splits, L.ldp, dlogp ? targets : nullptr, own, (const __nv_bfloat16*)weight, ldw, rows, d, v,
+                        (__nv_bfloat16*)dh, lddh));
   return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
 }

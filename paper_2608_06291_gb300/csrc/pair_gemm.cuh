@@ -145,6 +145,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
   cluster_sync_all();      // both CTAs' barriers are there
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_slot;
+  pdl_wait();         // so far nothing of the kernels before was touched
   const int64_t items = S.items(), step = gridDim.x >> 1, first = blockIdx.x >> 1;
   constexpr long long drain = 4000000000LL;      // about 2 s: the bound of the way out
   auto timed_out = [&]() {
@@ -314,6 +315,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
     if (lane == 0) bulk_commit_and_wait();
     __syncwarp();
   }
+  pdl_trigger();      // (from the start, CTAs of the next kernel in the queue cost 77 tokens' forward pass 9 us of 46)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   cluster_sync_all();      // neither CTA's memory or barriers go while the other may use them
@@ -438,8 +440,7 @@ cudaError_t pair_launch(const CUtensorMap& a, const CUtensorMap& b, const CUtens
   if (e != cudaSuccess) return e;
   const int64_t items = S.items();
   const unsigned pairs = (unsigned)(items < PG_PAIRS ? items : PG_PAIRS);
-  k_pair_gemm<Epi, AMN, BMN><<<2 * pairs, PG_THREADS, PG_SMEM, s>>>(a, b, o, S, E);
-  return cudaGetLastError();
+  return launch_pdl(k_pair_gemm<Epi, AMN, BMN>, dim3(2 * pairs), dim3(PG_THREADS), PG_SMEM, s, a, b, o, S, E);
 }
 
 }  // namespace bakron
