@@ -84,11 +84,15 @@ struct EpiLse {
   }
 };
 
+static_assert(2 * PG_PAIRS <= 256, "a thread a flag");
 struct JoinParams {
   const int64_t* targets;
   const float *m, *s, *x, *picked;
   int parts, rows, v;
   float *logp, *entropy, *lse;
+  const int* flags;      // of the product's CTAs
+  int ctas, more;        // more: not the call's first
+  int* status;
 };
 
 // R rows and 256 / R threads for each: every thread joins each (256 / R)-th triple, then they join.
@@ -99,6 +103,10 @@ __global__ void __launch_bounds__(256) k_head_join(const JoinParams P) {
   const int r = threadIdx.x % R, n = threadIdx.x / R, row = blockIdx.x * R + r;
   const bool in = row < P.rows;
   pdl_wait();
+  if (blockIdx.x == 0) {
+    const int bad = __syncthreads_or((int)threadIdx.x < P.ctas && P.flags[threadIdx.x] != 0);
+    if (threadIdx.x == 0 && (bad || !P.more)) *P.status = bad ? BAKRON_ERR_TIMEOUT : 0;
+  }
   float m = LOWEST;
   if (in)
     for (int p = n; p < P.parts; p += N) m = max_nan(m, P.m[(int64_t)p * P.rows + row]);
@@ -201,32 +209,38 @@ struct EpiGrad {
   }
 };
 
-__global__ void __launch_bounds__(256) k_head_no_token(int* first, int v) {
+__global__ void __launch_bounds__(256) k_head_no_token(int* first, int* tokens, int v) {
   const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < v) first[i] = NO_TOKEN;
+  if (i >= v) return;
+  first[i] = NO_TOKEN;
+  tokens[i] = 0;
 }
-// first[j]: the first token whose target is j.
-__global__ void __launch_bounds__(256) k_head_first(const int64_t* targets, int rows, int v, int* first) {
+// first[j]: the first token whose target is j; tokens[j]: how many there are.
+__global__ void __launch_bounds__(256) k_head_first(const int64_t* targets, int rows, int v, int* first, int* tokens) {
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i >= rows) return;
   const int64_t at = targets[i];
-  if (at >= 0 && at < v) atomicMin(first + at, i);
+  if (at < 0 || at >= v) return;
+  atomicMin(first + at, i);
+  atomicAdd(tokens + at, 1);
 }
 // Row t of `more`, where t is the first token with its target and the target lies in the
 // piece: the sum of own h over the tokens of that target, in their order.
 constexpr int MORE_COLS = 512;
-__global__ void __launch_bounds__(128) k_head_more(const int64_t* targets, const int* first, const float* own,
-                                                   const __nv_bfloat16* h, int64_t ldh, int rows, int d, int v, int v0,
-                                                   int count, float* more, int64_t ldmore) {
+__global__ void __launch_bounds__(128) k_head_more(const int64_t* targets, const int* first, const int* tokens,
+                                                   const float* own, const __nv_bfloat16* h, int64_t ldh, int rows, int d,
+                                                   int v, int v0, int count, float* more, int64_t ldmore) {
   const int t = blockIdx.x, c0 = blockIdx.y * MORE_COLS + threadIdx.x;
   const int64_t target = targets[t];
   if (target < v0 || target >= (int64_t)v0 + count || target >= v || first[target] != t) return;
   __shared__ int found[128];
   float acc[4] = {};
-  for (int i0 = t; i0 < rows; i0 += 128) {
+  int left = tokens[target];      // (a target that is not repeated is found at once)
+  for (int i0 = t; i0 < rows && left > 0; i0 += 128) {
     const int i = i0 + threadIdx.x;
     found[threadIdx.x] = i < rows && targets[i] == target;
-    const int any = __syncthreads_or(found[threadIdx.x]);
+    const int any = __syncthreads_count(found[threadIdx.x]);
+    left -= any;
     if (any)
       for (int j = 0; j < 128; ++j) {
         if (!found[j]) continue;
@@ -300,10 +314,11 @@ struct Carve {
   }
 };
 struct HeadLayout {
-  size_t h = 0, w = 0, m, s, x, picked, bytes;
+  size_t flags, h = 0, w = 0, m, s, x, picked, bytes;
   bool copy_h, copy_w;
   HeadLayout(const void* ph, int64_t ldh, const void* pw, int64_t ldw, int rows, int v, int d) {
     Carve c;
+    flags = c.take(2 * PG_PAIRS * sizeof(int));
     copy_h = !in_place(ph, rows, ldh);
     copy_w = !in_place(pw, v, ldw);
     if (copy_h) h = c.take((size_t)rows * round_up(d, 8) * 2);
@@ -318,7 +333,7 @@ struct HeadLayout {
   }
 };
 struct HeadBackLayout {
-  size_t h = 0, w = 0, own, first = 0, more = 0, g, part, bytes;
+  size_t h = 0, w = 0, own, first = 0, tokens = 0, more = 0, g, part, bytes;
   bool copy_h, copy_w;
   int piece, splits;
   int64_t ldg, ldp;      // of G, and of the fp32 sums
@@ -344,6 +359,7 @@ struct HeadBackLayout {
     own = c.take((size_t)rows * 4);
     if (dw) {
       first = c.take((size_t)v * 4);
+      tokens = c.take((size_t)v * 4);
       more = c.take((size_t)rows * ldp * 4);
     }
     g = c.take((size_t)rows * ldg * 2);
@@ -396,8 +412,6 @@ extern "C" int bakron_head_logprobs(const void* h, int64_t ldh, const void* weig
   if (workspace_bytes < L.bytes) return BAKRON_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)stream;
   char* ws = (char*)workspace;
-  k_clear_status<<<1, 1, 0, s>>>((int*)ws);
-  BK_CUDA_OK(cudaGetLastError());
   if (L.copy_h) {
     BK_CUDA_OK(copy_rows(h, ldh, rows, d, ws + L.h, s));
     h = ws + L.h;
@@ -412,6 +426,7 @@ extern "C" int bakron_head_logprobs(const void* h, int64_t ldh, const void* weig
     const int n = std::min(rows - r0, LSE_ROWS), bn = lse_bn(std::min(rows, LSE_ROWS), v);
     PairShape S = head_shape(n, bn, ceil_div(v, bn), ceil_div(d, PG_K), (int*)ws);
     S.group = LSE_GROUP;
+    S.flags = (int*)(ws + L.flags);
     CUtensorMap a, b;
     if (!pair_map(&a, false, (const __nv_bfloat16*)h + r0 * ldh, n, d, map_ld(n, ldh, d), PG_K, S.a_rows) ||
         !pair_map(&b, false, weight, v, d, map_ld(v, ldw, d), PG_K, bn / 2))
@@ -419,7 +434,8 @@ extern "C" int bakron_head_logprobs(const void* h, int64_t ldh, const void* weig
     EpiLse::Params E{targets ? targets + r0 : nullptr, (float*)(ws + L.m), (float*)(ws + L.s), (float*)(ws + L.x),
                      (float*)(ws + L.picked), n, v};
     BK_CUDA_OK((pair_launch<EpiLse, false, false>(a, b, b, S, E, s)));
-    JoinParams J{E.targets, E.m, E.s, E.x, E.picked, 2 * S.tn, n, v, logp ? logp + r0 : nullptr, entropy + r0, lse + r0};
+    JoinParams J{E.targets, E.m, E.s, E.x, E.picked, 2 * S.tn, n, v, logp ? logp + r0 : nullptr, entropy + r0, lse + r0,
+                 S.flags, (int)pair_ctas(S), r0 > 0, (int*)ws};
     BK_CUDA_OK(n < 64 ? launch_pdl(k_head_join<1>, dim3(n), dim3(256), 0, s, J)
                       : launch_pdl(k_head_join<16>, dim3(ceil_div(n, 16)), dim3(256), 0, s, J));
   }
@@ -464,11 +480,11 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
     ldw = round_up(d, 8);
   }
   float *own = (float*)(ws + L.own), *more = (float*)(ws + L.more), *part = (float*)(ws + L.part);
-  int* first = (int*)(ws + L.first);
+  int *first = (int*)(ws + L.first), *tokens = (int*)(ws + L.tokens);
   const bool near = dweight && targets && dlogp;      // dW gets the targets' rows
   if (near) {
-    k_head_no_token<<<ceil_div(v, 256), 256, 0, s>>>(first, v);
-    k_head_first<<<ceil_div(rows, 256), 256, 0, s>>>(targets, rows, v, first);
+    k_head_no_token<<<ceil_div(v, 256), 256, 0, s>>>(first, tokens, v);
+    k_head_first<<<ceil_div(rows, 256), 256, 0, s>>>(targets, rows, v, first, tokens);
     BK_CUDA_OK(cudaGetLastError());
   }
   const bool dw_tma = dweight && in_place(dweight, v, lddw);
@@ -502,7 +518,7 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
     // the piece's rows of dW
     if (near) {
       k_head_more<<<dim3((unsigned)rows, (unsigned)ceil_div(d, MORE_COLS)), 128, 0, s>>>(
-          targets, first, own, (const __nv_bfloat16*)h, ldh, rows, d, v, v0, count, more, L.ldp);
+          targets, first, tokens, own, (const __nv_bfloat16*)h, ldh, rows, d, v, v0, count, more, L.ldp);
       BK_CUDA_OK(cudaGetLastError());
     }
     __nv_bfloat16* c = (__nv_bfloat16*)dweight + v0 * lddw;

@@ -192,7 +192,6 @@ __global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const Layer
   __shared__ float2 slots[2][32];
   extern __shared__ __align__(16) unsigned char lb_ring[];   // [RING][h, dy, dsum][d]
   const int t = threadIdx.x, nt = blockDim.x;
-  pdl_trigger();      // the parts' sum may get ready; it waits for this grid's end
   auto pairs = [](const float (&v)[8], Two* p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) p[j] = Two(v[2 * j], v[2 * j + 1]);
@@ -297,6 +296,7 @@ __global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const Layer
       row_store<true>((T*)P.dx + row * P.lddx, i, t, nt, P.d, o);
     }
   }
+  pdl_trigger();
   float* part = P.part + (int64_t)blockIdx.x * 2 * P.d;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -473,7 +473,6 @@ __global__ void __launch_bounds__(1024) k_layernorm_dx(const LayerBackParams P) 
 #pragma unroll
     for (int j = 0; j < N; ++j) g[j] *= w[j];
   };
-  pdl_trigger();
   const float inv = 1.f / (float)P.d;
   const int step = blockDim.x * N;
   float mu = 0.f, mg = 0.f, ss = 0.f, gc = 0.f;
@@ -504,6 +503,7 @@ __global__ void __launch_bounds__(1024) k_layernorm_dx(const LayerBackParams P) 
     }
   }
   two_all(ss, gc, slots[1]);
+  pdl_trigger();
   const float rho = 1.f / sqrtf(ss * inv + P.eps), k = rho * rho * (gc * inv);
   if (threadIdx.x == 0) {
     P.stats[2 * row] = mu;
@@ -692,7 +692,7 @@ extern "C" int bakron_layernorm_backward(const void* dy, int64_t lddy, const voi
                                          int64_t ldds, void* dx, int64_t lddx, float* dw, float* db, void* workspace,
                                          size_t workspace_bytes, void* stream) {
   if (rows < 0 || d < 1 || d > NORM_MAX_D || !float_dtype(dtype) || !float_dtype(wdtype) || !(eps >= 0.f) || !dw ||
-      !db || !workspace)
+      !db || !workspace || (uintptr_t)workspace % 16 != 0)
     return BAKRON_ERR_INVALID_ARG;
   if (rows > 0 && (!dy || !h || !weight || !dx || lddy < d || ldh < d || lddx < d || (dsum && ldds < d)))
     return BAKRON_ERR_INVALID_ARG;

@@ -37,7 +37,8 @@ struct FusedParams {
   int64_t ldx;
   float* part;             // [CTA][its first tile, its last][token][128 columns]
   int vec;                 // dx can be written 8 bytes at a time
-  int* status;
+  int* status;             // and each CTA's error or 0, which the last kernel joins
+  int* flags;
   long long spin_cycles;
 };
 
@@ -91,7 +92,6 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_trigger();      // the sum of the parts may get ready; it waits for this grid's end
   const Shares share(P, gridDim.x);
   const int64_t u0 = share.begin(blockIdx.x), u1 = share.begin(blockIdx.x + 1);
   const int tile0 = (int)(u0 / P.nk), first_k = (int)(u0 % P.nk), count = (int)(u1 - u0);
@@ -126,15 +126,10 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
   constexpr long long drain = 4000000000LL;      // about 2 s: the bound of the way out
-  auto timed_out = [&]() {
-    pdl_wait();      // the status is cleared by the kernel before
-    raise_status(P.status, BAKRON_ERR_TIMEOUT);
-    abort_flag = 1;
-  };
   // a warp's wait; `out`: on the way out, whatever happened elsewhere
   auto wait = [&](uint64_t* bar, uint32_t parity, bool out = false) -> bool {
     if (mbar_wait_warp(bar, parity, out ? drain : P.spin_cycles, out ? nullptr : &abort_flag)) return true;
-    if (lane == 0 && !abort_flag) timed_out();
+    if (lane == 0) abort_flag = 1;
     __syncwarp();
     return false;
   };
@@ -300,6 +295,8 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  pdl_trigger();      // the sum of the parts may get ready; it waits for this grid's end
+  if (threadIdx.x == 0) P.flags[blockIdx.x] = abort_flag ? BAKRON_ERR_TIMEOUT : 0;
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * cols) : "memory");
 }
@@ -307,6 +304,10 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
 // Tiles that several CTAs share: their parts' sum.  A thread has 4 columns of a token.
 __global__ void __launch_bounds__(256) k_back_join(const FusedParams P, int ctas) {
   pdl_wait();
+  if (blockIdx.x + blockIdx.y == 0) {
+    const int bad = __syncthreads_or((int)threadIdx.x < ctas && P.flags[threadIdx.x] != 0);
+    if (threadIdx.x == 0) *P.status = bad ? BAKRON_ERR_TIMEOUT : 0;
+  }
   const Shares share(P, ctas);
   const int tile = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
   const int tok = i >> 5, token = tile % P.token_tiles * P.bn + tok;
@@ -383,9 +384,9 @@ constexpr int FUSED_TOKENS = 512;
 constexpr uint32_t FB_SMEM = 227 * 1024 - 1024;      // beside the barriers
 
 // How few tokens are shared out.
+static_assert(ROW_SMS <= 256, "a thread a flag");
 struct FusedPlan {
   int bn, token_tiles, tiles, nk, ctas, teams, na, nb, nc;
-  bool shared;      // tiles by CTAs
   size_t smem;
   FusedPlan(int rows, int m, int n, bool bytes8, bool one) {
     bn = (int)round_up(ceil_div(rows, ceil_div(rows, FB_MAX_BN)), 16);      // as even as tiles allow
@@ -394,7 +395,6 @@ struct FusedPlan {
     nk = ceil_div(m, LIN_BLOCK);
     // every SM, but no fewer than 4 blocks each: a part costs its sums' way through memory
     ctas = (int)std::max<int64_t>(1, std::min<int64_t>(ROW_SMS, (int64_t)tiles * nk / 4));
-    shared = nk > 1 && tiles % ctas != 0;      // else shares are whole tiles
     const uint32_t tok = (uint32_t)bn * 256, code = (bytes8 ? 16384 : 8192) + LIN_BLOCK * 5 * (one ? 1 : 4);
     auto fits = [&](int a, int b, int c) { return 1024 + a * FB_A + b * tok + c * code <= FB_SMEM; };
     na = teams = fits(4, 2, 4) ? 4 : 2;      // (two blocks of operands always fit)
@@ -406,7 +406,7 @@ struct FusedPlan {
 };
 
 struct BackLayout {
-  size_t dy = 0, part = 0, w = 0, bytes;
+  size_t dy = 0, flags = 0, part = 0, w = 0, bytes;
   bool copy;
   int64_t ldw;
   BackLayout(const void* p, int rows, int64_t ld, int m, int n, const FusedPlan& F) {
@@ -420,6 +420,7 @@ struct BackLayout {
     if (copy) dy = take((size_t)rows * round_up(m, 8) * 2);
     ldw = round_up(n, LIN_BLOCK);
     if (rows <= FUSED_TOKENS) {
+      flags = take((size_t)F.ctas * sizeof(int));
       part = take((size_t)F.ctas * 2 * F.bn * LIN_BLOCK * 4);
     } else {
       w = take((size_t)m * ldw * 2);
@@ -436,7 +437,8 @@ cudaError_t fused_launch(const CUtensorMap& map, const FusedParams& P, const Fus
     return cudaFuncSetAttribute(k_back_fused<W8, ONE, TEAMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FB_SMEM);
   });
   if (e != cudaSuccess) return e;
-  return launch_pdl(k_back_fused<W8, ONE, TEAMS>, dim3(F.ctas), dim3(FB_THREADS), F.smem, s, map, P);
+  k_back_fused<W8, ONE, TEAMS><<<F.ctas, FB_THREADS, F.smem, s>>>(map, P);
+  return cudaGetLastError();
 }
 
 constexpr int LB_MAX_DIM = 1 << 17, LB_MAX_ROWS = 1 << 24;
@@ -483,14 +485,12 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
   }
   const int64_t ldmap = rows > 1 ? lddy : round_up(m, 8);
   CUtensorMap a, b, o;
-  k_clear_status<<<1, 1, 0, s>>>((int*)ws);
-  BK_CUDA_OK(cudaGetLastError());
   if (rows <= FUSED_TOKENS) {
     if (!pair_map(&a, false, dy, rows, m, ldmap, 64, plan.bn)) return BAKRON_ERR_CUDA;
     FusedParams F{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, L.mp, (int)(L.np / LIN_BLOCK),
                   L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, rows, n, plan.bn, plan.nk, plan.token_tiles,
                   plan.tiles, plan.na, plan.nb, plan.nc, (__nv_bfloat16*)dx, lddx, (float*)(ws + B.part),
-                  aligned16(dx, rows > 1 ? lddx * 2 : 0), (int*)ws,
+                  aligned16(dx, rows > 1 ? lddx * 2 : 0), (int*)ws, (int*)(ws + B.flags),
                   spin_cycles_from_env()};
     const auto launch =
         plan.teams == 4 ? (L.bytes8 ? (one ? fused_launch<true, true, 4> : fused_launch<true, false, 4>)
@@ -498,11 +498,12 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
                         : (L.bytes8 ? (one ? fused_launch<true, true, 2> : fused_launch<true, false, 2>)
                                     : (one ? fused_launch<false, true, 2> : fused_launch<false, false, 2>));
     BK_CUDA_OK(launch(a, F, plan, s));
-    if (plan.shared)
-      BK_CUDA_OK(launch_pdl(k_back_join, dim3((unsigned)ceil_div(plan.bn, 8), (unsigned)plan.tiles), dim3(256), 0, s, F,
+    BK_CUDA_OK(launch_pdl(k_back_join, dim3((unsigned)ceil_div(plan.bn, 8), (unsigned)plan.tiles), dim3(256), 0, s, F,
                             plan.ctas));
     return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
   }
+  k_clear_status<<<1, 1, 0, s>>>((int*)ws);
+  BK_CUDA_OK(cudaGetLastError());
   ExpandParams E{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, m, (int)(L.np / LIN_BLOCK),
                  L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, L.mp, (__nv_bfloat16*)(ws + B.w), B.ldw};
   const unsigned ctas = (unsigned)(L.mp * E.kblocks * (L.units / 4) / 64);

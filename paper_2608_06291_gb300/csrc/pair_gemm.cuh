@@ -46,7 +46,8 @@ struct PairShape {
   int band;            // row tiles walked side by side
   int rows;            // rows of A: CTAs behind the last load none (K-major A)
   int a_rows;          // rows of a K-major A box (a multiple of 8, at most 128)
-  int* status;
+  int* status;         // gets the error of a wait that ran out; or, where there are
+  int* flags;          // flags, each CTA's is written: the error or 0 (so nothing has to be cleared before)
   long long spin_cycles;
   __host__ __device__ int64_t items() const { return (int64_t)tm * tn * splits; }
 };
@@ -149,7 +150,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
   const int64_t items = S.items(), step = gridDim.x >> 1, first = blockIdx.x >> 1;
   constexpr long long drain = 4000000000LL;      // about 2 s: the bound of the way out
   auto timed_out = [&]() {
-    raise_status(S.status, BAKRON_ERR_TIMEOUT);
+    if (!S.flags) raise_status(S.status, BAKRON_ERR_TIMEOUT);
     *abort_flag = 1;
     st_peer_flag((const void*)abort_flag, rank);
   };
@@ -248,7 +249,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
       if (elected()) mma_commit_pair(done);
       __syncwarp();
     }
-    if (lane == 0 && !mbar_wait_cluster(done, 0, drain)) raise_status(S.status, BAKRON_ERR_TIMEOUT);
+    if (lane == 0 && !mbar_wait_cluster(done, 0, drain)) timed_out();
     __syncwarp();
   } else {
     // ------------------------------------------------------------ epilogue
@@ -320,6 +321,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
   __syncthreads();
   cluster_sync_all();      // neither CTA's memory or barriers go while the other may use them
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (threadIdx.x == 0 && S.flags) S.flags[blockIdx.x] = *abort_flag ? BAKRON_ERR_TIMEOUT : 0;
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
@@ -430,6 +432,11 @@ inline bool pair_map(CUtensorMap* map, bool f32, const void* base, int64_t rows,
 
 constexpr int PG_PAIRS = ROW_SMS / 2;
 
+inline unsigned pair_ctas(const PairShape& S) {
+  const int64_t items = S.items();
+  return 2 * (unsigned)(items < PG_PAIRS ? items : PG_PAIRS);
+}
+
 template <class Epi, bool AMN, bool BMN>
 cudaError_t pair_launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const PairShape& S,
                         const typename Epi::Params& E, cudaStream_t s) {
@@ -438,9 +445,7 @@ cudaError_t pair_launch(const CUtensorMap& a, const CUtensorMap& b, const CUtens
     return cudaFuncSetAttribute(k_pair_gemm<Epi, AMN, BMN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PG_SMEM);
   });
   if (e != cudaSuccess) return e;
-  const int64_t items = S.items();
-  const unsigned pairs = (unsigned)(items < PG_PAIRS ? items : PG_PAIRS);
-  return launch_pdl(k_pair_gemm<Epi, AMN, BMN>, dim3(2 * pairs), dim3(PG_THREADS), PG_SMEM, s, a, b, o, S, E);
+  return launch_pdl(k_pair_gemm<Epi, AMN, BMN>, dim3(pair_ctas(S)), dim3(PG_THREADS), PG_SMEM, s, a, b, o, S, E);
 }
 
 }  // namespace bakron

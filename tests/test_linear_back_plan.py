@@ -41,9 +41,6 @@ int main() {
               const int first = (int)(s.begin(c) / p.nk), last = (int)((s.begin(c + 1) - 1) / p.nk);
               ok = ok && s.slot(c, first) == 2 * c && (last == first || s.slot(c, last) == 2 * c + 1);
             }
-            bool shared = false;
-            for (int c = 0; c < p.ctas; ++c) shared = shared || s.begin(c) % p.nk != 0;
-            ok = ok && shared <= p.shared;
           }
           if (!ok && bad++ < 20) std::printf("rows %d m %d n %d w8 %d one %d: bn %d teams %d na %d nb %d nc %d smem %zu\n", rows,
                                              m, n, w8, one, p.bn, p.teams, p.na, p.nb, p.nc, p.smem);
