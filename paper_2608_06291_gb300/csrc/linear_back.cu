@@ -17,7 +17,7 @@
 namespace bakron {
 namespace {
 
-// ------------------------------------------------------------------ few tokens
+// ------------------------------------------------------------------ operands
 constexpr int FB_WARPS = 16;                     // form operands
 constexpr int FB_THREADS = 32 * (8 + FB_WARPS);  // warps 0 and 2 load, warp 1 issues MMAs, warps 4-7 write out
 constexpr uint32_t FB_A = LIN_BLOCK * LIN_BLOCK * 2;   // operands: [64 rows][64 columns], two by two
@@ -71,6 +71,153 @@ __device__ __forceinline__ uint32_t scaled8(uint32_t w, int odd, __half2 z1024, 
   return bf16_pack(c.x * s, c.y * s);
 }
 
+// ------------------------------------------------------------------ up to 8 tokens
+// No tensor memory, no shared operands: mma.sync takes What's columns as the rows of its first operand
+// and What's rows as its depth.  A warp has two column blocks and 16 rows at a time: lane group g one of
+// their 8 units (32 columns of a row), lane q of it rows 4q..4q+3, so that a word's 8 columns of two
+// rows become, halves exchanged, operand registers of 4 products.  The order of the 16 rows is free: the
+// tokens' values (its second operand, token g) are those of rows 4q..4q+3.
+constexpr int FEW_BACK = 8, FW_COLS = 256, FW_WARPS = 8;
+constexpr int FW_BLOCK = 129, FW_TOKEN = 265;      // strides of the warps' sums, so that lanes meet different banks
+constexpr int FW_SMEM = FW_WARPS * FEW_BACK * FW_TOKEN * 4;
+
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                            uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+struct FewParams {
+  const unsigned char* codes;
+  const float* scales;
+  const uint8_t* zeros;
+  int64_t mp;
+  int kblocks, chunks, G;
+  int rows, m, n, chunks16, per;      // 16-row chunks in all, of a CTA (a multiple of 8)
+  const __nv_bfloat16* dy;
+  int64_t lddy;
+  int yvec;                           // dy can be read 8 bytes at a time
+  float* part;                        // [split][token][column tiles' 256]
+  int* status;
+};
+
+template <bool W8, bool ONE>
+__global__ void __launch_bounds__(FW_WARPS * 32, W8 || !ONE ? 1 : 2) k_back_few(const FewParams P) {
+  constexpr int UNITS = W8 ? 8 : 4, H = W8 ? 2 : 1, GRIDS = ONE ? 1 : 4;
+  extern __shared__ float fw_sums[];      // [warp][token][column]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int cb = blockIdx.x * 2 + (g >> 2), t = g & 3;
+  const bool there = cb < P.kblocks;
+  if (blockIdx.x + blockIdx.y + threadIdx.x == 0) *P.status = 0;      // nothing here can run out
+  const int first = blockIdx.y * P.per, last = min(first + P.per, P.chunks16);
+  int grid[GRIDS];
+#pragma unroll
+  for (int j = 0; j < GRIDS; ++j) grid[j] = P.G == 1 ? 0 : min((cb * 4 + j) / P.chunks, P.G - 1);
+  struct Chunk {
+    uint4 u[4][H];
+    float4 s[GRIDS];
+    uint32_t z[GRIDS];
+    uint32_t y[2];
+  };
+  auto load = [&](int chunk, Chunk& to) {
+    const int row = chunk * 16 + 4 * q;
+    if (there) {
+      const uint4* at = reinterpret_cast<const uint4*>(P.codes) +
+                        (((int64_t)(row >> 7) * P.kblocks + cb) * UNITS + t) * LIN_BLOCK + (row & 127);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int h = 0; h < H; ++h) to.u[r][h] = __ldg(at + h * 4 * LIN_BLOCK + r);
+#pragma unroll
+      for (int j = 0; j < GRIDS; ++j) {
+        to.s[j] = __ldg(reinterpret_cast<const float4*>(P.scales + grid[j] * P.mp + row));
+        to.z[j] = __ldg(reinterpret_cast<const uint32_t*>(P.zeros + grid[j] * P.mp + row));
+      }
+    }
+    to.y[0] = to.y[1] = 0u;
+    if (g < P.rows) {
+      const __nv_bfloat16* y = P.dy + g * P.lddy + row;
+      if (P.yvec && row + 4 <= P.m) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(y));
+        to.y[0] = v.x;
+        to.y[1] = v.y;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (row + k < P.m) to.y[k >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(y)[k] << (16 * (k & 1));
+      }
+    }
+  };
+  float acc[16][4] = {};
+  Chunk next;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int h = 0; h < H; ++h) next.u[r][h] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+  for (int j = 0; j < GRIDS; ++j) next.s[j] = make_float4(0.f, 0.f, 0.f, 0.f), next.z[j] = 0u;
+  if (first + warp < last) load(first + warp, next);
+  for (int chunk = first + warp; chunk < last; chunk += FW_WARPS) {
+    const Chunk here = next;
+    if (chunk + FW_WARPS < last) load(chunk + FW_WARPS, next);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 s4 = here.s[ONE ? 0 : j];
+      const float sf[4] = {s4.x, s4.y, s4.z, s4.w};
+      uint32_t v[4][4];      // [row][pair of columns]
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float zf = (float)((here.z[ONE ? 0 : j] >> (8 * r)) & 255u);
+        if constexpr (W8) {
+          const __half2 z = __float2half2_rn(1024.f + zf);
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(&here.u[r][j >> 1]);
+#pragma unroll
+          for (int p = 0; p < 4; ++p) v[r][p] = scaled8(w[2 * (j & 1) + (p >> 1)], p & 1, z, sf[r]);
+        } else {
+          const __nv_bfloat162 z = __float2bfloat162_rn(128.f + zf), hi = __float2bfloat162_rn(sf[r]);
+          const __nv_bfloat162 lo = __float2bfloat162_rn(sf[r] - __low2float(hi));
+          const uint32_t w = reinterpret_cast<const uint32_t*>(&here.u[r][0])[j];
+#pragma unroll
+          for (int p = 0; p < 4; ++p) v[r][p] = scaled(pair4(w, p, z), hi, lo);
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        mma_16x8x16(acc[4 * j + p], __byte_perm(v[0][p], v[1][p], 0x5410), __byte_perm(v[0][p], v[1][p], 0x7632),
+                    __byte_perm(v[2][p], v[3][p], 0x5410), __byte_perm(v[2][p], v[3][p], 0x7632), here.y[0], here.y[1]);
+    }
+  }
+  float* mine = fw_sums + warp * FEW_BACK * FW_TOKEN + (g >> 2) * FW_BLOCK + 8 * t;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)      // column of the pair e >> 1, token 2q + (e & 1)
+      mine[(2 * q + (e & 1)) * FW_TOKEN + 32 * (i >> 2) + 2 * (i & 3) + (e >> 1)] = acc[i][e];
+  __syncthreads();
+  const int c = threadIdx.x;      // FW_COLS threads
+  for (int tok = 0; tok < P.rows; ++tok) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < FW_WARPS; ++w) v += fw_sums[(w * FEW_BACK + tok) * FW_TOKEN + c + (c >> 7) * (FW_BLOCK - 128)];
+    P.part[(((int64_t)blockIdx.y * P.rows + tok) * gridDim.x + blockIdx.x) * FW_COLS + c] = v;
+  }
+  pdl_trigger();
+}
+
+__global__ void __launch_bounds__(256) k_back_few_sum(const float* part, int splits, int rows, int tiles, int n,
+                                                      __nv_bfloat16* dx, int64_t ldx) {
+  const int col = blockIdx.x * 256 + threadIdx.x, tok = blockIdx.y;
+  pdl_wait();
+  if (col >= n) return;
+  float v = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < splits; ++s) v += part[((int64_t)s * rows + tok) * tiles * FW_COLS + col];
+  dx[tok * ldx + col] = __float2bfloat16_rn(v);
+}
+
+// ------------------------------------------------------------------ more, up to FUSED_TOKENS
 // A CTA takes an equal share of all tiles' blocks, one after another; a tile that several share is
 // summed from their parts, in their order, by a second kernel.  (As clusters that add
 // through each other's shared memory, no more than 15 of 8 CTAs ran at a time.)
@@ -383,7 +530,7 @@ __global__ void __launch_bounds__(256) k_back_copy(const __nv_bfloat16* from, in
 constexpr int FUSED_TOKENS = 512;
 constexpr uint32_t FB_SMEM = 227 * 1024 - 1024;      // beside the barriers
 
-// How few tokens are shared out.
+// How up to FUSED_TOKENS tokens are shared out.
 static_assert(ROW_SMS <= 256, "a thread a flag");
 struct FusedPlan {
   int bn, token_tiles, tiles, nk, ctas, teams, na, nb, nc;
@@ -405,6 +552,18 @@ struct FusedPlan {
   }
 };
 
+// How up to 8 tokens are: two CTAs an SM, each at least 128 rows, and no more than 64 parts to add.
+struct FewPlan {
+  int tiles, chunks, per, splits;
+  FewPlan(int m, int n) {
+    tiles = ceil_div(n, FW_COLS);
+    chunks = ceil_div(m, 16);
+    const int most = std::max(1, std::min(2 * ROW_SMS / tiles, 64));
+    per = (int)round_up(ceil_div(chunks, most), FW_WARPS);
+    splits = ceil_div(chunks, per);
+  }
+};
+
 struct BackLayout {
   size_t dy = 0, flags = 0, part = 0, w = 0, bytes;
   bool copy;
@@ -416,10 +575,13 @@ struct BackLayout {
       at += align256(b);
       return r;
     };
-    copy = !aligned16(p, rows > 1 ? ld * 2 : 0);
+    copy = rows > FEW_BACK && !aligned16(p, ld * 2);
     if (copy) dy = take((size_t)rows * round_up(m, 8) * 2);
     ldw = round_up(n, LIN_BLOCK);
-    if (rows <= FUSED_TOKENS) {
+    if (rows <= FEW_BACK) {
+      const FewPlan few(m, n);
+      part = take((size_t)few.splits * rows * few.tiles * FW_COLS * 4);
+    } else if (rows <= FUSED_TOKENS) {
       flags = take((size_t)F.ctas * sizeof(int));
       part = take((size_t)F.ctas * 2 * F.bn * LIN_BLOCK * 4);
     } else {
@@ -429,6 +591,17 @@ struct BackLayout {
   }
 };
 bool one_grid(int n, int group_size) { return group_size == 0 || group_size == n || group_size % LIN_BLOCK == 0; }
+
+template <bool W8, bool ONE>
+cudaError_t few_launch(const FewParams& P, const FewPlan& F, cudaStream_t s) {
+  static OncePerDevice once;
+  const cudaError_t e = once([] {
+    return cudaFuncSetAttribute(k_back_few<W8, ONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, FW_SMEM);
+  });
+  if (e != cudaSuccess) return e;
+  k_back_few<W8, ONE><<<dim3((unsigned)F.tiles, (unsigned)F.splits), FW_WARPS * 32, FW_SMEM, s>>>(P);
+  return cudaGetLastError();
+}
 
 template <bool W8, bool ONE, int TEAMS>
 cudaError_t fused_launch(const CUtensorMap& map, const FusedParams& P, const FusedPlan& F, cudaStream_t s) {
@@ -476,6 +649,19 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
   const unsigned char* p = (const unsigned char*)packed;
   cudaStream_t s = (cudaStream_t)stream;
   char* ws = (char*)workspace;
+  if (rows <= FEW_BACK) {
+    const FewPlan few(m, n);
+    FewParams F{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, L.mp, (int)(L.np / LIN_BLOCK),
+                L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, rows, m, n, few.chunks, few.per,
+                (const __nv_bfloat16*)dy, lddy, ((uintptr_t)dy | (uintptr_t)(rows > 1 ? lddy * 2 : 0)) % 8 == 0,
+                (float*)(ws + B.part), (int*)ws};
+    const auto launch = L.bytes8 ? (one ? few_launch<true, true> : few_launch<true, false>)
+                                 : (one ? few_launch<false, true> : few_launch<false, false>);
+    BK_CUDA_OK(launch(F, few, s));
+    BK_CUDA_OK(launch_pdl(k_back_few_sum, dim3((unsigned)ceil_div(n, 256), (unsigned)rows), dim3(256), 0, s, F.part, few.splits,
+                          rows, few.tiles, n, (__nv_bfloat16*)dx, lddx));
+    return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
+  }
   if (B.copy) {
     k_back_copy<<<(unsigned)std::min(rows, 8 * ROW_SMS), 256, 0, s>>>((const __nv_bfloat16*)dy, lddy, rows, m,
                                                                       (__nv_bfloat16*)(ws + B.dy), round_up(m, 8));
@@ -483,7 +669,7 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
     dy = ws + B.dy;
     lddy = round_up(m, 8);
   }
-  const int64_t ldmap = rows > 1 ? lddy : round_up(m, 8);
+  const int64_t ldmap = lddy;
   CUtensorMap a, b, o;
   if (rows <= FUSED_TOKENS) {
     if (!pair_map(&a, false, dy, rows, m, ldmap, 64, plan.bn)) return BAKRON_ERR_CUDA;
