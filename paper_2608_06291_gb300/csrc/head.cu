@@ -95,49 +95,83 @@ struct JoinParams {
   int* status;
 };
 
-// R rows and 256 / R threads for each: every thread joins each (256 / R)-th triple, then they join.
-template <int R>
-__global__ void __launch_bounds__(256) k_head_join(const JoinParams P) {
-  constexpr int N = 256 / R;
-  __shared__ float red[3][N][R];
-  const int r = threadIdx.x % R, n = threadIdx.x / R, row = blockIdx.x * R + r;
-  const bool in = row < P.rows;
-  pdl_wait();
-  if (blockIdx.x == 0) {
-    const int bad = __syncthreads_or((int)threadIdx.x < P.ctas && P.flags[threadIdx.x] != 0);
-    if (threadIdx.x == 0 && (bad || !P.more)) *P.status = bad ? BAKRON_ERR_TIMEOUT : 0;
+// What the parts' triples give together: (m, s, x) of two is that of the larger maximum.
+struct Triple {
+  float m = LOWEST, s = 0.f, x = 0.f;
+  __device__ __forceinline__ void add(float m2, float s2, float x2) {
+    const float top = max_nan(m, m2), a = max_nan((m - top) * LOG2E, -126.f), b = max_nan((m2 - top) * LOG2E, -126.f);
+    const float wa = exp2_fast(a), wb = exp2_fast(b);
+    x = fmaf(wa, fmaf(s, a, x), wb * fmaf(s2, b, x2));
+    s = fmaf(wa, s, wb * s2);
+    m = top;
   }
-  float m = LOWEST;
-  if (in)
-    for (int p = n; p < P.parts; p += N) m = max_nan(m, P.m[(int64_t)p * P.rows + row]);
-  red[0][n][r] = m;
-  __syncthreads();
-  m = LOWEST;
-  for (int i = 0; i < N; ++i) m = max_nan(m, red[0][i][r]);
-  float s = 0.f, x = 0.f;
-  if (in)
-    for (int p = n; p < P.parts; p += N) {
-      const int64_t at = (int64_t)p * P.rows + row;
-      const float t = max_nan((P.m[at] - m) * LOG2E, -126.f), w = exp2_fast(t);
-      s = fmaf(w, P.s[at], s);
-      x = fmaf(w, fmaf(P.s[at], t, P.x[at]), x);
-    }
-  red[1][n][r] = s;
-  red[2][n][r] = x;
-  __syncthreads();
-  if (n > 0 || !in) return;
-  s = x = 0.f;
-  for (int i = 0; i < N; ++i) {
-    s += red[1][i][r];
-    x += red[2][i][r];
+  __device__ __forceinline__ void warp() {      // always in the same order
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+      add(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o), __shfl_xor_sync(0xffffffffu, x, o));
   }
-  const float ls = logf(s), lse = m + ls;
+};
+
+__device__ __forceinline__ void head_status(const JoinParams& P) {
+  if (blockIdx.x != 0) return;
+  const int bad = __syncthreads_or((int)threadIdx.x < P.ctas && P.flags[threadIdx.x] != 0);
+  if (threadIdx.x == 0 && (bad || !P.more)) *P.status = bad ? BAKRON_ERR_TIMEOUT : 0;
+}
+__device__ __forceinline__ void head_result(const JoinParams& P, const Triple& t, int row) {
+  const float ls = logf(t.s), lse = t.m + ls;
   P.lse[row] = lse;
-  P.entropy[row] = ls - LN2 * (x / s);
+  P.entropy[row] = ls - LN2 * (t.x / t.s);
   if (P.logp) {
     const int64_t at = P.targets[row];
     P.logp[row] = at >= 0 && at < P.v ? P.picked[row] - lse : 0.f;
   }
+}
+
+// Few rows: a CTA each, a thread every 512th part.
+__global__ void __launch_bounds__(512) k_head_join_row(const JoinParams P) {
+  __shared__ float red[3][16];
+  const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();
+  head_status(P);
+  Triple t;
+  for (int p = threadIdx.x; p < P.parts; p += 512) {
+    const int64_t at = (int64_t)p * P.rows + row;
+    t.add(P.m[at], P.s[at], P.x[at]);
+  }
+  t.warp();
+  if (lane == 0) red[0][warp] = t.m, red[1][warp] = t.s, red[2][warp] = t.x;
+  __syncthreads();
+  if (warp > 0) return;
+  t = Triple();
+  if (lane < 16) t.m = red[0][lane], t.s = red[1][lane], t.x = red[2][lane];
+  t.warp();
+  if (lane == 0) head_result(P, t, row);
+}
+
+// 32 rows a CTA, their triples read together: a warp takes every 32nd part, then the parts' order of a row.
+__global__ void __launch_bounds__(1024) k_head_join(const JoinParams P) {
+  __shared__ float red[3][32][33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * 32 + lane;
+  pdl_wait();
+  head_status(P);
+  Triple t;
+  if (row < P.rows) {
+#pragma unroll 2
+    for (int p = warp; p < P.parts; p += 32) {
+      const int64_t at = (int64_t)p * P.rows + row;
+      t.add(P.m[at], P.s[at], P.x[at]);
+    }
+  }
+  red[0][warp][lane] = t.m;
+  red[1][warp][lane] = t.s;
+  red[2][warp][lane] = t.x;
+  __syncthreads();
+  t.m = red[0][lane][warp];
+  t.s = red[1][lane][warp];
+  t.x = red[2][lane][warp];
+  t.warp();
+  const int mine = blockIdx.x * 32 + warp;
+  if (lane == 0 && mine < P.rows) head_result(P, t, mine);
 }
 
 // Rows that TMA cannot read as they lie, copied to rows of 16-byte multiples.
@@ -233,44 +267,61 @@ __global__ void __launch_bounds__(128) k_head_more(const int64_t* targets, const
   const int t = blockIdx.x, c0 = blockIdx.y * MORE_COLS + threadIdx.x;
   const int64_t target = targets[t];
   if (target < v0 || target >= (int64_t)v0 + count || target >= v || first[target] != t) return;
-  __shared__ int found[128];
+  __shared__ uint32_t found[2][4];
   float acc[4] = {};
   int left = tokens[target];      // (a target that is not repeated is found at once)
-  for (int i0 = t; i0 < rows && left > 0; i0 += 128) {
+  for (int i0 = t, turn = 0; i0 < rows && left > 0; i0 += 128, turn ^= 1) {
     const int i = i0 + threadIdx.x;
-    found[threadIdx.x] = i < rows && targets[i] == target;
-    const int any = __syncthreads_count(found[threadIdx.x]);
-    left -= any;
-    if (any)
-      for (int j = 0; j < 128; ++j) {
-        if (!found[j]) continue;
-        const float w = own[i0 + j];
-        const __nv_bfloat16* row = h + (i0 + j) * ldh;
+    const uint32_t same = __ballot_sync(0xffffffffu, i < rows && targets[i] == target);
+    if ((threadIdx.x & 31) == 0) found[turn][threadIdx.x >> 5] = same;
+    __syncthreads();
+    for (int w = 0; w < 4; ++w)
+      for (uint32_t bits = found[turn][w]; bits; bits &= bits - 1, --left) {
+        const int at = i0 + 32 * w + __ffs((int)bits) - 1;
+        const float a = own[at];
+        const __nv_bfloat16* row = h + at * ldh;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (c0 + 128 * k < d) acc[k] = fmaf(w, __bfloat162float(row[c0 + 128 * k]), acc[k]);
+          if (c0 + 128 * k < d) acc[k] = fmaf(a, __bfloat162float(row[c0 + 128 * k]), acc[k]);
       }
-    __syncthreads();
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     if (c0 + 128 * k < d) more[(int64_t)t * ldmore + c0 + 128 * k] = acc[k];
 }
 
-// dh = the parts' sum + own W[target], rounded once.
+// dh = the parts' sum + own W[target], rounded once.  A thread has 4 columns.
 __global__ void __launch_bounds__(256) k_head_dh(const float* part, int splits, int64_t ldp, const int64_t* targets,
                                                  const float* own, const __nv_bfloat16* w, int64_t ldw, int rows,
-                                                 int d, int v, __nv_bfloat16* dh, int64_t lddh) {
+                                                 int d, int v, __nv_bfloat16* dh, int64_t lddh, int vec) {
   pdl_wait();
   const int row = blockIdx.x;
   const int64_t target = targets ? targets[row] : -1;
   const bool scored = target >= 0 && target < v;
   const float a = scored ? own[row] : 0.f;
-  for (int c = blockIdx.y * 256 + threadIdx.x; c < d; c += 256 * gridDim.y) {
-    float sum = 0.f;
-    for (int s = 0; s < splits; ++s) sum += part[((int64_t)s * rows + row) * ldp + c];
-    if (scored) sum = fmaf(a, __bfloat162float(w[target * ldw + c]), sum);
-    dh[row * lddh + c] = __float2bfloat16_rn(sum);
+  for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < d; c += 1024 * gridDim.y) {
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* from = part + row * ldp + c;      // (its rows are whole float4s)
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      const float4 u = *reinterpret_cast<const float4*>(from + (int64_t)s * rows * ldp);
+      sum.x += u.x;
+      sum.y += u.y;
+      sum.z += u.z;
+      sum.w += u.w;
+    }
+    float o[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (scored && c + k < d) o[k] = fmaf(a, __bfloat162float(w[target * ldw + c + k]), o[k]);
+    __nv_bfloat16* out = dh + row * lddh + c;
+    if (vec && c + 4 <= d) {
+      *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pack(o[0], o[1]), bf16_pack(o[2], o[3]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < d) out[k] = __float2bfloat16_rn(o[k]);
+    }
   }
 }
 
@@ -436,8 +487,8 @@ extern "C" int bakron_head_logprobs(const void* h, int64_t ldh, const void* weig
     BK_CUDA_OK((pair_launch<EpiLse, false, false>(a, b, b, S, E, s)));
     JoinParams J{E.targets, E.m, E.s, E.x, E.picked, 2 * S.tn, n, v, logp ? logp + r0 : nullptr, entropy + r0, lse + r0,
                  S.flags, (int)pair_ctas(S), r0 > 0, (int*)ws};
-    BK_CUDA_OK(n < 64 ? launch_pdl(k_head_join<1>, dim3(n), dim3(256), 0, s, J)
-                      : launch_pdl(k_head_join<16>, dim3(ceil_div(n, 16)), dim3(256), 0, s, J));
+    BK_CUDA_OK(n < 64 ? launch_pdl(k_head_join_row, dim3(n), dim3(512), 0, s, J)
+                      : launch_pdl(k_head_join, dim3(ceil_div(n, 32)), dim3(1024), 0, s, J));
   }
   return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
 }
@@ -531,8 +582,8 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
     EpiBf16::Params B{dw_tma ? nullptr : c, lddw, count, d, near ? first + v0 : nullptr, more, L.ldp};
     BK_CUDA_OK((pair_launch<EpiBf16, true, true>(a, b, dw_tma ? o : a, S, B, s)));
   }
-  BK_CUDA_OK(launch_pdl(k_head_dh, dim3((unsigned)rows, (unsigned)std::min(ceil_div(d, 256), 8)), dim3(256), 0, s, part,
+  BK_CUDA_OK(launch_pdl(k_head_dh, dim3((unsigned)rows, (unsigned)std::min(ceil_div(d, 1024), 8)), dim3(256), 0, s, part,
                         L.splits, L.ldp, dlogp ? targets : nullptr, own, (const __nv_bfloat16*)weight, ldw, rows, d, v,
-                        (__nv_bfloat16*)dh, lddh));
+                        (__nv_bfloat16*)dh, lddh, (int)(((uintptr_t)dh | (uintptr_t)(rows > 1 ? lddh * 2 : 0)) % 8 == 0)));
   return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
 }

@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(1024) k_layernorm_dx(const LayerBackParams P) 
   const float inv = 1.f / (float)P.d;
   const int step = blockDim.x * N;
   float mu = 0.f, mg = 0.f, ss = 0.f, gc = 0.f;
-#pragma unroll 2
+#pragma unroll 4
   for (int e = threadIdx.x * N; e < P.d; e += step) {
     float a[N], g[N];
     load_n(h + e, a);
@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(1024) k_layernorm_dx(const LayerBackParams P) 
   two_all(mu, mg, slots[0]);
   mu *= inv;
   mg *= inv;
-#pragma unroll 2
+#pragma unroll 4
   for (int e = threadIdx.x * N; e < P.d; e += step) {
     float a[N], g[N];
     load_n(h + e, a);
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(1024) k_layernorm_dx(const LayerBackParams P) 
     P.stats[2 * row] = mu;
     P.stats[2 * row + 1] = rho;
   }
-#pragma unroll 2
+#pragma unroll 4
   for (int e = threadIdx.x * N; e < P.d; e += step) {
     float a[N], g[N];
     load_n(h + e, a);

@@ -510,12 +510,16 @@ __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
   for (int j = 0; j < (W8 ? 2 : 4); ++j) {
     const int chunk = kb * 4 + (W8 ? half * 2 : 0) + j, grid = P.G == 1 ? 0 : min(chunk / P.chunks, P.G - 1);
     const float s = P.scales[grid * P.mp + row], z = (float)P.zeros[grid * P.mp + row];
-    const __nv_bfloat162 zz = __float2bfloat162_rn(z + (W8 ? 0.f : 128.f));
     uint32_t o[4];
+    if constexpr (W8) {
+      const __half2 zz = __float2half2_rn(1024.f + z);
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const uint32_t c = W8 ? pair8(words[2 * j], words[2 * j + 1], p, zz) : pair4(words[j], p, zz);
-      o[p] = bf16_pack(bf16_lo(c) * s, bf16_hi(c) * s);
+      for (int p = 0; p < 4; ++p) o[p] = scaled8(words[2 * j + (p >> 1)], p & 1, zz, s);
+    } else {
+      const __nv_bfloat162 zz = __float2bfloat162_rn(128.f + z), hi = __float2bfloat162_rn(s);
+      const __nv_bfloat162 lo = __float2bfloat162_rn(s - __low2float(hi));
+#pragma unroll
+      for (int p = 0; p < 4; ++p) o[p] = scaled(pair4(words[j], p, zz), hi, lo);
     }
     *reinterpret_cast<uint4*>(P.w + row * P.ldw + chunk * 32 + 8 * t) = make_uint4(o[0], o[1], o[2], o[3]);
   }
@@ -524,7 +528,7 @@ __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
 __global__ void __launch_bounds__(256) k_back_copy(const __nv_bfloat16* from, int64_t ld, int rows, int m, __nv_bfloat16* to,
                                                    int64_t ldt) {
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
-    for (int c = threadIdx.x; c < m; c += blockDim.x) to[row * ldt + c] = from[row * ld + c];
+    for (int c = blockIdx.y * 256 + threadIdx.x; c < m; c += 256 * gridDim.y) to[row * ldt + c] = from[row * ld + c];
 }
 
 constexpr int FUSED_TOKENS = 512;
@@ -663,8 +667,8 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
     return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
   }
   if (B.copy) {
-    k_back_copy<<<(unsigned)std::min(rows, 8 * ROW_SMS), 256, 0, s>>>((const __nv_bfloat16*)dy, lddy, rows, m,
-                                                                      (__nv_bfloat16*)(ws + B.dy), round_up(m, 8));
+    k_back_copy<<<dim3((unsigned)std::min(rows, 8 * ROW_SMS), (unsigned)std::min(ceil_div(m, 512), 16)), 256, 0, s>>>(
+        (const __nv_bfloat16*)dy, lddy, rows, m, (__nv_bfloat16*)(ws + B.dy), round_up(m, 8));
     BK_CUDA_OK(cudaGetLastError());
     dy = ws + B.dy;
     lddy = round_up(m, 8);
