@@ -2,13 +2,15 @@
 // What_ij = s (c_ij - z) with the grid (s, z) of row i and j's group.
 //
 // The sum runs over What's rows, whose scales differ, so the scale cannot wait for the end of a
-// sum as it does in the forward product: an operand is s (c - z), formed in fp32 and rounded
-// once to bf16.
+// sum as it does in the forward product: an operand is s (c - z), rounded once to bf16.
 //
-// Up to FUSED_TOKENS tokens: one kernel. D (128 columns of What x bn tokens) += A B with A the
-// operands of a 128 x 128 block, formed from its codes in shared memory as the MMAs take them
-// (MN-major), and B the tokens' gradients, K-major by TMA.
-// More tokens: the weight is written out in bf16 once, and read by the pair product.
+// Up to 8 tokens: mma.sync on operands formed in registers.  Up to FUSED_TOKENS: D (128 columns of
+// What x bn tokens) += A B on the 5th-generation tensor cores with A the operands of a 128 x 128 block, formed
+// from its codes in shared memory as the MMAs take them (MN-major), and B the tokens' gradients, K-major
+// by TMA.  More: the weight is written out in bf16 once, and read by the pair product.
+//
+// us, caches flushed: 1 token, groups of 128, 4096 x 4096 10, 28672 x 8192 49 (2.7 TB/s); 17 tokens through 4099 x 11003
+// in 8 bits 27; 64 through 11008 x 4096 23, 256 50, 4096 231 (1.6 PFLOP/s; 20 of them to write the weight out).
 #include <algorithm>
 
 #include "linear.cuh"
@@ -77,6 +79,9 @@ __device__ __forceinline__ uint32_t scaled8(uint32_t w, int odd, __half2 z1024, 
 // their 8 units (32 columns of a row), lane q of it rows 4q..4q+3, so that a word's 8 columns of two
 // rows become, halves exchanged, operand registers of 4 products.  The order of the 16 rows is free: the
 // tokens' values (its second operand, token g) are those of rows 4q..4q+3.
+//
+// Bound by instructions, some 3.3 a code (issue 66% busy, DRAM 34%: 28672 x 8192), where memory would take 19 us
+// of 49.  8 tokens 49 too; by the kernel below 62.  Sixteen tokens' sums do not leave the registers for two CTAs an SM.
 constexpr int FEW_BACK = 8, FW_COLS = 256, FW_WARPS = 8;
 constexpr int FW_BLOCK = 129, FW_TOKEN = 265;      // strides of the warps' sums, so that lanes meet different banks
 constexpr int FW_SMEM = FW_WARPS * FEW_BACK * FW_TOKEN * 4;
@@ -223,6 +228,11 @@ __global__ void __launch_bounds__(256) k_back_few_sum(const float* part, int spl
 // through each other's shared memory, no more than 15 of 8 CTAs ran at a time.)
 // ONE: the 128 columns of a block have one grid a row.  TEAMS: see below; na and nc are multiples of
 // it, so that a ring's slot always belongs to one team, which knows the phase it is in.
+//
+// Bound by the issue of MMAs, some 100 cycles each however few tokens they have: the 8 of a block, its two commits
+// and waits take 900 cycles (16 x 28672 x 8192 52 of 62 us with neither loads nor operands formed), the
+// operands 1000 beside them.  (Tokens as the MMA's 128 rows and 256 columns of What, half as many MMAs, took 99: its
+// copies are of a kilobyte, 50 cycles each.)  From 128 tokens on by the MMAs themselves.
 template <bool W8, bool ONE, int TEAMS>
 __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_constant__ CUtensorMap map, const FusedParams P) {
   constexpr int TEAM = FB_WARPS / TEAMS;      // warps
@@ -493,7 +503,7 @@ struct ExpandParams {
   int64_t ldw;      // a multiple of 128
 };
 
-// What in bf16, row by row.  A thread takes a 16-byte unit; four lanes have a row's chunk together.
+// What in bf16, row by row.  A thread takes a 16-byte unit; four lanes have a row's chunk together.  11008 x 4096: 20 us.
 template <bool W8>
 __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
   constexpr int UNITS = W8 ? 8 : 4;
@@ -531,7 +541,9 @@ __global__ void __launch_bounds__(256) k_back_copy(const __nv_bfloat16* from, in
     for (int c = blockIdx.y * 256 + threadIdx.x; c < m; c += 256 * gridDim.y) to[row * ldt + c] = from[row * ld + c];
 }
 
-constexpr int FUSED_TOKENS = 512;
+// 384 tokens through 11008 x 4096 63 us, by the weight in bf16 90; 4096 x 4096 45, 44; 4096 x 11008 77, 82.  At 512
+// 76, 91; 50, 44; 93, 82.
+constexpr int FUSED_TOKENS = 384;
 constexpr uint32_t FB_SMEM = 227 * 1024 - 1024;      // beside the barriers
 
 // How up to FUSED_TOKENS tokens are shared out.

@@ -165,7 +165,8 @@ def _check_back(dy, h, w, eps, dsum, got):
     assert torch.all((db.double() - dy.sum(0)).abs() <= adds * dy.abs().sum(0) + 1e-30)
 
 
-@pytest.mark.parametrize("rows,d", SHAPES + [(1000, 256), (2000, 33), (700, 4096), (650, 17000), (200, 9344), (200, 11003)])
+@pytest.mark.parametrize("rows,d", SHAPES + [(1000, 256), (2000, 33), (700, 4096), (650, 17000), (200, 9344), (200, 11003),
+                                            (609, 520), (620, 1001), (640, 8200), (640, 11003), (620, 16384), (608, 8192), (609, 8192)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("dsum", [False, True])
 def test_backward(rows, d, dtype, dsum):

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 if torch.cuda.is_available():
     import paper_2608_06291_gb300 as P
 
-TOKENS = [1, 2, 7, 8, 9, 16, 17, 31, 33, 64, 65, 128, 129, 200, 256, 257, 300, 520]
+TOKENS = [1, 2, 7, 8, 9, 16, 17, 31, 33, 64, 65, 128, 129, 200, 256, 257, 384, 385, 520]
 WEIGHTS = [(1, 1, 15, 0), (5, 3, 1, 0), (64, 128, 15, 128), (130, 127, 3, 0), (300, 256, 255, 0), (257, 384, 15, 32),
            (700, 512, 7, 64), (513, 576, 255, 96), (1000, 1100, 200, 0), (2100, 129, 15, 0), (96, 2048, 15, 512)]
 
@@ -131,9 +131,10 @@ def test_streams_and_graphs():
             assert torch.equal(out, want if k else P.bakron_linear_backward(2 * dy, w))
 
 
-def test_timeout_is_reported(monkeypatch):
+@pytest.mark.parametrize("t", [40, 300, 600])
+def test_timeout_is_reported(t, monkeypatch):
     w, W = _weight(700, 512, 15, 0, 5, False)
-    dy = torch.randn(300, 700, device="cuda").bfloat16()
+    dy = torch.randn(t, 700, device="cuda").bfloat16()
     monkeypatch.setenv("BAKRON_SPIN_CYCLES", "0")
     with pytest.raises(P.BakronError) as e:
         P.bakron_linear_backward(dy, w, sync=True)
