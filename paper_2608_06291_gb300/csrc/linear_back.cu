@@ -9,8 +9,8 @@
 // from its codes in shared memory as the MMAs take them (MN-major), and B the tokens' gradients, K-major
 // by TMA.  More: the weight is written out in bf16 once, and read by the pair product.
 //
-// us, caches flushed: 1 token, groups of 128, 4096 x 4096 10, 28672 x 8192 49 (2.7 TB/s); 17 tokens through 4099 x 11003
-// in 8 bits 27; 64 through 11008 x 4096 23, 256 50, 4096 231 (1.6 PFLOP/s; 20 of them to write the weight out).
+// us, caches flushed: 1 token, groups of 128, 4096 x 4096 10, 28672 x 8192 47 (2.8 TB/s); 17 tokens through 4099 x 11003
+// in 8 bits 25; 64 through 11008 x 4096 23, 256 50, 4096 231 (1.6 PFLOP/s; 20 of them to write the weight out).
 #include <algorithm>
 
 #include "linear.cuh"
@@ -66,11 +66,40 @@ __device__ __forceinline__ uint32_t scaled(uint32_t v, __nv_bfloat162 hi, __nv_b
   const __nv_bfloat162 r = __hfma2(c, hi, __hmul2(c, lo));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
+// A row's grid as the codes' expansion wants it.
+template <bool W8>
+struct RowGrid;
+template <>
+struct RowGrid<false> {
+  __nv_bfloat162 z, hi, lo;
+  __device__ __forceinline__ void set(float s, float zero) {
+    z = __float2bfloat162_rn(128.f + zero);
+    hi = __float2bfloat162_rn(s);
+    lo = __float2bfloat162_rn(s - __low2float(hi));
+  }
+};
+template <>
+struct RowGrid<true> {
+  __half2 z;
+  float s;
+  __device__ __forceinline__ void set(float scale, float zero) {
+    z = __float2half2_rn(1024.f + zero);
+    s = scale;
+  }
+};
 // Two 8-bit codes of a pair as c - z in fp16 (1024 + c is exact there), times s in fp32.
 __device__ __forceinline__ uint32_t scaled8(uint32_t w, int odd, __half2 z1024, float s) {
   uint32_t u = __byte_perm(w, 0x64646464u, odd ? 0x4341 : 0x4240);
   const float2 c = __half22float2(__hsub2(*reinterpret_cast<__half2*>(&u), z1024));
   return bf16_pack(c.x * s, c.y * s);
+}
+
+// Pair p of chunk j (32 columns, 8 of them a unit's) of a unit: columns 2p, 2p + 1 of its 8.
+__device__ __forceinline__ uint32_t operand(const uint4 (&u)[1], int j, int p, const RowGrid<false>& g) {
+  return scaled(pair4(reinterpret_cast<const uint32_t*>(&u[0])[j], p, g.z), g.hi, g.lo);
+}
+__device__ __forceinline__ uint32_t operand(const uint4 (&u)[2], int j, int p, const RowGrid<true>& g) {
+  return scaled8(reinterpret_cast<const uint32_t*>(&u[j >> 1])[2 * (j & 1) + (p >> 1)], p & 1, g.z, g.s);
 }
 
 // ------------------------------------------------------------------ up to 8 tokens
@@ -80,8 +109,9 @@ __device__ __forceinline__ uint32_t scaled8(uint32_t w, int odd, __half2 z1024, 
 // rows become, halves exchanged, operand registers of 4 products.  The order of the 16 rows is free: the
 // tokens' values (its second operand, token g) are those of rows 4q..4q+3.
 //
-// Bound by instructions, some 3.3 a code (issue 66% busy, DRAM 34%: 28672 x 8192), where memory would take 19 us
-// of 49.  8 tokens 49 too; by the kernel below 62.  Sixteen tokens' sums do not leave the registers for two CTAs an SM.
+// Bound by the products and the operands' forming one after the other: 1 x 28672 x 8192 takes 47 us (DRAM 34% busy; 19 at
+// the memory's rate), with a quarter of the products 29, without the codes' expansion 28.  8 tokens 49, by the kernel
+// below 62.  Sixteen tokens' sums do not leave the registers for two CTAs an SM.
 constexpr int FEW_BACK = 8, FW_COLS = 256, FW_WARPS = 8;
 constexpr int FW_BLOCK = 129, FW_TOKEN = 265;      // strides of the warps' sums, so that lanes meet different banks
 constexpr int FW_SMEM = FW_WARPS * FEW_BACK * FW_TOKEN * 4;
@@ -167,27 +197,20 @@ __global__ void __launch_bounds__(FW_WARPS * 32, W8 || !ONE ? 1 : 2) k_back_few(
   for (int chunk = first + warp; chunk < last; chunk += FW_WARPS) {
     const Chunk here = next;
     if (chunk + FW_WARPS < last) load(chunk + FW_WARPS, next);
+    RowGrid<W8> rg[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float4 s4 = here.s[ONE ? 0 : j];
-      const float sf[4] = {s4.x, s4.y, s4.z, s4.w};
+      if (j == 0 || !ONE) {
+        const float4 s4 = here.s[ONE ? 0 : j];
+        const float sf[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) rg[r].set(sf[r], (float)((here.z[ONE ? 0 : j] >> (8 * r)) & 255u));
+      }
       uint32_t v[4][4];      // [row][pair of columns]
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float zf = (float)((here.z[ONE ? 0 : j] >> (8 * r)) & 255u);
-        if constexpr (W8) {
-          const __half2 z = __float2half2_rn(1024.f + zf);
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(&here.u[r][j >> 1]);
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int p = 0; p < 4; ++p) v[r][p] = scaled8(w[2 * (j & 1) + (p >> 1)], p & 1, z, sf[r]);
-        } else {
-          const __nv_bfloat162 z = __float2bfloat162_rn(128.f + zf), hi = __float2bfloat162_rn(sf[r]);
-          const __nv_bfloat162 lo = __float2bfloat162_rn(sf[r] - __low2float(hi));
-          const uint32_t w = reinterpret_cast<const uint32_t*>(&here.u[r][0])[j];
-#pragma unroll
-          for (int p = 0; p < 4; ++p) v[r][p] = scaled(pair4(w, p, z), hi, lo);
-        }
-      }
+        for (int p = 0; p < 4; ++p) v[r][p] = operand(here.u[r], j, p, rg[r]);
 #pragma unroll
       for (int p = 0; p < 4; ++p)
         mma_16x8x16(acc[4 * j + p], __byte_perm(v[0][p], v[1][p], 0x5410), __byte_perm(v[0][p], v[1][p], 0x7632),
@@ -383,28 +406,16 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
         uint4 u[W8 ? 2 : 1];
 #pragma unroll
         for (int h = 0; h < (W8 ? 2 : 1); ++h) u[h] = *reinterpret_cast<const uint4*>(here + ((4 * h + t) * LIN_BLOCK + r) * 16);
-        float sf[GRIDS], zf[GRIDS];
+        RowGrid<W8> rg[GRIDS];
 #pragma unroll
-        for (int j = 0; j < (int)GRIDS; ++j) {
-          sf[j] = reinterpret_cast<const float*>(grid + j * GRID)[r];
-          zf[j] = (float)grid[j * GRID + LIN_BLOCK * 4 + r];
-        }
+        for (int j = 0; j < (int)GRIDS; ++j)
+          rg[j].set(reinterpret_cast<const float*>(grid + j * GRID)[r], (float)grid[j * GRID + LIN_BLOCK * 4 + r]);
         unsigned char* a = to + (i * 8 * TEAM / 64) * (FB_A / 2) + (i * 8 * TEAM % 64) * 128;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           uint32_t o[4];
-          if constexpr (W8) {
-            const __half2 z = __float2half2_rn(1024.f + zf[ONE ? 0 : j]);
-            const uint32_t* w = reinterpret_cast<const uint32_t*>(&u[j >> 1]);
 #pragma unroll
-            for (int p = 0; p < 4; ++p) o[p] = scaled8(w[2 * (j & 1) + (p >> 1)], p & 1, z, sf[ONE ? 0 : j]);
-          } else {
-            const __nv_bfloat162 z = __float2bfloat162_rn(128.f + zf[ONE ? 0 : j]), hi = __float2bfloat162_rn(sf[ONE ? 0 : j]);
-            const __nv_bfloat162 lo = __float2bfloat162_rn(sf[ONE ? 0 : j] - __low2float(hi));
-            const uint32_t w = reinterpret_cast<const uint32_t*>(&u[0])[j];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) o[p] = scaled(pair4(w, p, z), hi, lo);
-          }
+          for (int p = 0; p < 4; ++p) o[p] = operand(u, j, p, rg[ONE ? 0 : j]);
           *reinterpret_cast<uint4*>(a + (j >> 1) * 8192 + (((4 * (j & 1) + t) ^ (r & 7)) << 4)) =
               make_uint4(o[0], o[1], o[2], o[3]);
         }
@@ -521,15 +532,14 @@ __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
     const int chunk = kb * 4 + (W8 ? half * 2 : 0) + j, grid = P.G == 1 ? 0 : min(chunk / P.chunks, P.G - 1);
     const float s = P.scales[grid * P.mp + row], z = (float)P.zeros[grid * P.mp + row];
     uint32_t o[4];
-    if constexpr (W8) {
-      const __half2 zz = __float2half2_rn(1024.f + z);
+    RowGrid<W8> g;
+    g.set(s, z);
 #pragma unroll
-      for (int p = 0; p < 4; ++p) o[p] = scaled8(words[2 * j + (p >> 1)], p & 1, zz, s);
-    } else {
-      const __nv_bfloat162 zz = __float2bfloat162_rn(128.f + z), hi = __float2bfloat162_rn(s);
-      const __nv_bfloat162 lo = __float2bfloat162_rn(s - __low2float(hi));
-#pragma unroll
-      for (int p = 0; p < 4; ++p) o[p] = scaled(pair4(words[j], p, zz), hi, lo);
+    for (int p = 0; p < 4; ++p) {
+      if constexpr (W8)
+        o[p] = scaled8(words[2 * j + (p >> 1)], p & 1, g.z, g.s);
+      else
+        o[p] = scaled(pair4(words[j], p, g.z), g.hi, g.lo);
     }
     *reinterpret_cast<uint4*>(P.w + row * P.ldw + chunk * 32 + 8 * t) = make_uint4(o[0], o[1], o[2], o[3]);
   }
@@ -644,7 +654,7 @@ using namespace bakron;
 
 extern "C" size_t bakron_linear_backward_workspace_bytes(const void* dy, int rows, int64_t lddy, int m, int n, int qmax,
                                                          int group_size) {
-  return back_ok(rows, m, n, qmax, group_size) && rows > 0 
+  return back_ok(rows, m, n, qmax, group_size) && rows > 0
              ? BackLayout(dy, rows, lddy, m, n, FusedPlan(rows, m, n, qmax > 15, one_grid(n, group_size))).bytes
              : 0;
 }
@@ -719,7 +729,7 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
   S.splits = 1;
   S.band = 16;
   S.rows = rows;
-  S.a_rows = rows >= 128 ? 128 : (int)round_up(rows, 8);
+  S.a_rows = 128;
   S.status = (int*)ws;
   S.spin_cycles = spin_cycles_from_env();
   const bool tma = aligned16(dx, rows > 1 ? lddx * 2 : 0);
