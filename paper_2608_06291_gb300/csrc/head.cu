@@ -178,13 +178,6 @@ __global__ void __launch_bounds__(1024) k_head_join(const JoinParams P) {
   if (lane == 0 && mine < P.rows) head_result(P, t, mine);
 }
 
-// Rows that TMA cannot read as they lie, copied to rows of 16-byte multiples.
-__global__ void __launch_bounds__(256) k_head_copy(const __nv_bfloat16* from, int64_t ld, int64_t rows, int d,
-                                                   __nv_bfloat16* to, int64_t ldt) {
-  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
-    for (int c = threadIdx.x; c < d; c += blockDim.x) to[row * ldt + c] = from[row * ld + c];
-}
-
 // ------------------------------------------------------------------ backward
 struct EpiGrad {
   static constexpr bool CHUNKED = false;
@@ -426,12 +419,6 @@ struct HeadBackLayout {
   }
 };
 
-cudaError_t copy_rows(const void* from, int64_t ld, int64_t rows, int d, void* to, cudaStream_t s) {
-  k_head_copy<<<(unsigned)std::min<int64_t>(rows, 8 * ROW_SMS), 256, 0, s>>>((const __nv_bfloat16*)from, ld, rows, d,
-                                                                             (__nv_bfloat16*)to, round_up(d, 8));
-  return cudaGetLastError();
-}
-
 PairShape head_shape(int rows, int bn, int tn, int nk, int* status) {
   PairShape S{};
   S.tm = ceil_div(rows, PG_M);
@@ -471,12 +458,12 @@ extern "C" int bakron_head_logprobs(const void* h, int64_t ldh, const void* weig
   cudaStream_t s = (cudaStream_t)stream;
   char* ws = (char*)workspace;
   if (L.copy_h) {
-    BK_CUDA_OK(copy_rows(h, ldh, rows, d, ws + L.h, s));
+    BK_CUDA_OK(pair_copy(h, ldh, rows, d, ws + L.h, s));
     h = ws + L.h;
     ldh = round_up(d, 8);
   }
   if (L.copy_w) {
-    BK_CUDA_OK(copy_rows(weight, ldw, v, d, ws + L.w, s));
+    BK_CUDA_OK(pair_copy(weight, ldw, v, d, ws + L.w, s));
     weight = ws + L.w;
     ldw = round_up(d, 8);
   }
@@ -528,12 +515,12 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
   k_clear_status<<<1, 1, 0, s>>>((int*)ws);
   BK_CUDA_OK(cudaGetLastError());
   if (L.copy_h) {
-    BK_CUDA_OK(copy_rows(h, ldh, rows, d, ws + L.h, s));
+    BK_CUDA_OK(pair_copy(h, ldh, rows, d, ws + L.h, s));
     h = ws + L.h;
     ldh = round_up(d, 8);
   }
   if (L.copy_w) {
-    BK_CUDA_OK(copy_rows(weight, ldw, v, d, ws + L.w, s));
+    BK_CUDA_OK(pair_copy(weight, ldw, v, d, ws + L.w, s));
     weight = ws + L.w;
     ldw = round_up(d, 8);
   }

@@ -545,12 +545,6 @@ __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
   }
 }
 
-__global__ void __launch_bounds__(256) k_back_copy(const __nv_bfloat16* from, int64_t ld, int rows, int m, __nv_bfloat16* to,
-                                                   int64_t ldt) {
-  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
-    for (int c = blockIdx.y * 256 + threadIdx.x; c < m; c += 256 * gridDim.y) to[row * ldt + c] = from[row * ld + c];
-}
-
 // 384 tokens through 11008 x 4096 63 us, by the weight in bf16 90; 4096 x 4096 45, 44; 4096 x 11008 77, 82.  At 512
 // 76, 91; 50, 44; 93, 82.
 constexpr int FUSED_TOKENS = 384;
@@ -689,9 +683,7 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
     return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
   }
   if (B.copy) {
-    k_back_copy<<<dim3((unsigned)std::min(rows, 8 * ROW_SMS), (unsigned)std::min(ceil_div(m, 512), 16)), 256, 0, s>>>(
-        (const __nv_bfloat16*)dy, lddy, rows, m, (__nv_bfloat16*)(ws + B.dy), round_up(m, 8));
-    BK_CUDA_OK(cudaGetLastError());
+    BK_CUDA_OK(pair_copy(dy, lddy, rows, m, ws + B.dy, s));
     dy = ws + B.dy;
     lddy = round_up(m, 8);
   }

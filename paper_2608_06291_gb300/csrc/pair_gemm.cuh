@@ -432,6 +432,18 @@ inline bool pair_map(CUtensorMap* map, bool f32, const void* base, int64_t rows,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Rows that TMA cannot read as they lie, copied to rows of whole 16 bytes.
+static __global__ void __launch_bounds__(256) k_pair_copy(const __nv_bfloat16* from, int64_t ld, int64_t rows, int cols,
+                                                          __nv_bfloat16* to, int64_t ldt) {
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
+    for (int c = blockIdx.y * 256 + threadIdx.x; c < cols; c += 256 * gridDim.y) to[row * ldt + c] = from[row * ld + c];
+}
+inline cudaError_t pair_copy(const void* from, int64_t ld, int64_t rows, int cols, void* to, cudaStream_t s) {
+  const dim3 grid((unsigned)(rows < 8 * ROW_SMS ? rows : 8 * ROW_SMS), (unsigned)(cols < 16 * 512 ? ceil_div(cols, 512) : 16));
+  k_pair_copy<<<grid, 256, 0, s>>>((const __nv_bfloat16*)from, ld, rows, cols, (__nv_bfloat16*)to, round_up(cols, 8));
+  return cudaGetLastError();
+}
+
 constexpr int PG_PAIRS = ROW_SMS / 2;
 
 inline unsigned pair_ctas(const PairShape& S) {
