@@ -305,3 +305,28 @@ def test_refusals():
                 lambda: P.bakron_head_logprobs(h, w, at, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(P.BakronError):
             bad()
+
+
+def test_offsets_past_32_bits():
+    """A weight of 2.46e9 values: what lies behind the 2^31st is read and its gradient written."""
+    t, v, d = 5, 300000, 8192
+    g = torch.Generator(device="cuda").manual_seed(13)
+    h = torch.randn(t, d, generator=g, device="cuda").bfloat16()
+    w = torch.randn(v, d, generator=g, device="cuda", dtype=torch.bfloat16) * (2.5 / d ** 0.5)
+    at = torch.tensor([v - 1, 7, v - 3, -100, v - 1], device="cuda")
+    logp, ent, lse = P.bakron_head_logprobs(h, w, at)
+    x = torch.cat([h.double() @ w[i:i + 20000].double().t() for i in range(0, v, 20000)], 1)
+    want = torch.logsumexp(x, 1)
+    slack = (d / 16 + 16) * 2.0 ** -23 * (h.double().abs() @ w[:1000].double().abs().t()).amax() * 2 + 2.0 ** -19 + 2.0 ** -22 * 20
+    assert torch.all((lse.double() - want).abs() <= slack)
+    c = torch.randn(t, generator=g, device="cuda")
+    dh, dw = P.bakron_head_logprobs_backward(h, w, at, lse, c)
+    G = -(torch.where(at >= 0, c.double(), 0.0)[:, None] * (x - lse.double()[:, None]).exp())
+    G[torch.arange(t), at.clamp(min=0)] += torch.where(at >= 0, c.double(), 0.0)
+    for s in (slice(0, 300), slice(v - 300, v)):
+        rows = G[:, s].t() @ h.double()
+        # an entry of G: a rounding, the logits' error; one rounding of the result
+        cut = G[:, s].abs().t() @ h.double().abs()
+        assert torch.all((dw[s].double() - rows).abs() <= (1.01 * 2.0 ** -8 + 2 * slack) * cut + 1.01 * 2.0 ** -8 * rows.abs() + 1e-37)
+    back = sum(G[:, i:i + 20000] @ w[i:i + 20000].double() for i in range(0, v, 20000))
+    assert torch.linalg.norm(dh.double() - back) <= 2 * 2.0 ** -8 * torch.linalg.norm(back)
