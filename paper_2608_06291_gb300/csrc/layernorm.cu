@@ -159,24 +159,27 @@ struct LayerBackParams {
   float eps;
 };
 
-// Two sums over the CTA in one butterfly: the lower half warp goes on with a, the upper with b.
-__device__ __forceinline__ void two_all(float& a, float& b, float2* slots) {
+// Two sums over the CTA (at most 32 warps) in one butterfly: the lower half warp goes on with a, the
+// upper with b, in the warp and then over the warps.
+struct TwoSlots {
+  float v[2][32];
+};
+__device__ __forceinline__ void two_all(float& a, float& b, TwoSlots& slots) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const bool up = lane & 16;
+  const int up = lane >> 4, in = lane & 15;
   float v = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 16);
 #pragma unroll
   for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if ((lane & 15) == 0) (up ? slots[warp].y : slots[warp].x) = v;
-  if (warps > 1)
+  if (warps > 1) {
+    if (in == 0) slots.v[up][warp] = v;
     __syncthreads();
-  else
-    __syncwarp();
-  a = b = 0.f;
-  for (int w = 0; w < warps; ++w) {
-    const float2 s = slots[w];
-    a += s.x;
-    b += s.y;
+    v = in < warps ? slots.v[up][in] : 0.f;
+    if (in + 16 < warps) v += slots.v[up][in + 16];
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   }
+  a = __shfl_sync(0xffffffffu, v, 0);
+  b = __shfl_sync(0xffffffffu, v, 16);
 }
 
 // A CTA takes the rows blockIdx.x, + gridDim.x, ...; both parameters' gradients stay in registers
@@ -186,12 +189,12 @@ __device__ __forceinline__ void two_all(float& a, float& b, float2* slots) {
 // from a ring of RING rows that vector copies fill ahead, and kept in fp32, as pairs, through the three
 // passes (mean, sums of what is left, dx).  What bounds it is instructions before it is memory: with the
 // row read back from shared memory and widened in each pass, one value an instruction, 8192 x 4096
-// in bf16 with dsum took 98 us, now 72 with the parts' sum (issue 58% busy, DRAM 54%; 16 warps an SM, as the
+// in bf16 with dsum took 98 us, now 67 with the parts' sum (issue 53% busy, DRAM 60%; 16 warps an SM, as the
 // registers allow).
 constexpr int LB_GROUPS = 1024;      // groups of 8: 512 threads
 template <typename T, typename W, int RING, int MAXT>
 __global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const LayerBackParams P) {
-  __shared__ float2 slots[2][32];
+  __shared__ TwoSlots slots[2];
   extern __shared__ __align__(16) unsigned char lb_ring[];   // [RING][h, dy, dsum][d]
   const int t = threadIdx.x, nt = blockDim.x;
   auto pairs = [](const float (&v)[8], Two* p) {
@@ -321,7 +324,7 @@ template <typename T, typename W, bool VEC, int RING, int VPT>
 __global__ void __launch_bounds__(1024) k_layernorm_back_wide(const LayerBackParams P) {
   constexpr bool KEEP_W = RING > 1;
   static_assert(VEC || RING == 1, "whole vectors");
-  __shared__ float2 slots[2][32];
+  __shared__ TwoSlots slots[2];
   extern __shared__ __align__(16) unsigned char lb_ring[];   // [RING][h, dy, dsum][d]
   const int t = threadIdx.x, nt = blockDim.x;
   pdl_trigger();      // the parts' sum may get ready; it waits for this grid's end
@@ -461,7 +464,7 @@ __device__ __forceinline__ void load_n(const T* p, float (&v)[8]) { load8(p, v);
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(1024) k_layernorm_dx(const LayerBackParams P) {
   constexpr int N = VEC ? 8 : 1;
-  __shared__ float2 slots[2][32];
+  __shared__ TwoSlots slots[2];
   const int64_t row = blockIdx.x;
   const T* h = (const T*)P.h + row * P.ldh;
   const T* dy = (const T*)P.dy + row * P.lddy;
