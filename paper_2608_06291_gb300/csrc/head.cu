@@ -38,6 +38,15 @@ __device__ __forceinline__ float exp2_fast(float v) {      // 2 ulp, results bel
   return r;
 }
 
+// Column `at` of a thread's sums (written in C++ it becomes an index, and the sums local memory).
+__device__ __forceinline__ float column(const float (&acc)[128], int at) {
+  float l = 0.f;
+#pragma unroll
+  for (int u = 0; u < 128; ++u)
+    asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, %3;\n\t}" : "+f"(l) : "r"(at), "r"(u), "f"(acc[u]));
+  return l;
+}
+
 // ------------------------------------------------------------------ forward
 // Of 2^((l - m) log2 e) over a row's half tile: the maximum m, the sum s, and x, the sum weighted
 // with (l - m) log2 e.
@@ -49,7 +58,7 @@ struct EpiLse {
     float* picked;         // the targets' logits
     int rows, v;
   };
-  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, float (&acc)[128]) {
+  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, float (&acc)[128], const CUtensorMap*) {
     const int cols = min(O.cols, E.v - O.col);      // may be none
     float m = LOWEST;
 #pragma unroll
@@ -60,15 +69,7 @@ struct EpiLse {
     }
     if (O.row < E.rows && E.targets) {
       const int64_t at = E.targets[O.row] - O.col;
-      if (at >= 0 && at < cols) {
-        float l = 0.f;      // (written in C++ it became an index, and the sums local memory)
-#pragma unroll
-        for (int u = 0; u < 128; ++u)
-          asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, %3;\n\t}"
-              : "+f"(l)
-              : "r"((int)at), "r"(u), "f"(acc[u]));
-        E.picked[O.row] = l;
-      }
+      if (at >= 0 && at < cols) E.picked[O.row] = column(acc, (int)at);
     }
     float s[4] = {}, x[4] = {};
 #pragma unroll
@@ -179,24 +180,27 @@ __global__ void __launch_bounds__(1024) k_head_join(const JoinParams P) {
 }
 
 // ------------------------------------------------------------------ backward
+// G of a tile from its logits, summed in the forward pass's groups: a logit is then the same number there
+// and here, and in l - lse, where lse is nearly the target's own logit when the model is sure of it, what
+// both have lost cancels.
 struct EpiGrad {
-  static constexpr bool CHUNKED = false;
+  static constexpr bool CHUNKED = true;
   struct Params {
     const int64_t* targets;
     const float *lse, *dlogp, *entropy, *dentropy;
     float* own;      // the target's entry, where the target lies in the piece
     int rows, v, v0, count;
   };
-  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, const CUtensorMap* map) {
+  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, float (&acc)[128], const CUtensorMap* map) {
     float lse = 0.f, g = 0.f, u = 0.f, ent = 0.f;
-    int at = -1;      // the target's column in the piece
+    int at = -1;      // the target's column in the warp's half of the tile
     if (O.row < E.rows) {
       lse = E.lse[O.row];
       if (E.targets) {
         const int64_t target = E.targets[O.row];
         if (target >= 0 && target < E.v) {
           if (E.dlogp) g = E.dlogp[O.row];
-          if (target >= E.v0 && target < (int64_t)E.v0 + E.count) at = (int)(target - E.v0);
+          if (target >= E.v0 && target < (int64_t)E.v0 + E.count) at = (int)(target - E.v0) - O.col;
         }
       }
       if (E.dentropy) {
@@ -204,32 +208,29 @@ struct EpiGrad {
         ent = E.entropy[O.row];
       }
     }
-    for (int c = 0; c < O.cols; c += 64) {
+    if (at >= 0 && at < O.cols) {      // g (1 - p), without the difference
+      const float lp = max_nan(column(acc, at) - lse, -87.f);
+      E.own[O.row] = -fmaf(g, expm1f(lp), u * exp2_fast(lp * LOG2E) * (lp + ent));
+    }
+#pragma unroll
+    for (int c = 0; c < 128; c += 64) {
+      if (c >= O.cols) break;
       stage_free(O.lane);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t r[32];
-        tmem_ld32(O.tmem + c + 32 * h, r);
-        tmem_wait_ld();
-        const int own = at - (O.col + c + 32 * h);
+      for (int k = 0; k < 8; ++k) {
+        uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float lp = max_nan(__uint_as_float(r[j]) - lse, -87.f), p = exp2_fast(lp * LOG2E);
-          float z = -p * fmaf(u, lp + ent, g);
-          if (j == own) {
-            E.own[O.row] = g + z;
-            z = 0.f;
+        for (int j = 0; j < 4; ++j) {
+          float z[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int i = c + 8 * k + 2 * j + e;
+            const float lp = max_nan(acc[i] - lse, -87.f), p = exp2_fast(lp * LOG2E);
+            z[e] = i == at ? 0.f : -p * fmaf(u, lp + ent, g);
           }
-          r[j] = __float_as_uint(z);
+          w[j] = bf16_pack(z[0], z[1]);
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = bf16_pack(__uint_as_float(r[8 * k + 2 * j]), __uint_as_float(r[8 * k + 2 * j + 1]));
-          *staged(O.stage, O.lane, 4 * h + k) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        *staged(O.stage, O.lane, k) = make_uint4(w[0], w[1], w[2], w[3]);
       }
       stage_ready();
       if (O.lane == 0) {
@@ -540,6 +541,7 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
     CUtensorMap a, b, o;
     // G of the piece
     PairShape S = head_shape(rows, 256, ceil_div(count, 256), ceil_div(d, PG_K), (int*)ws);
+    S.group = LSE_GROUP;
     if (!pair_map(&a, false, h, rows, d, map_ld(rows, ldh, d), PG_K, S.a_rows) ||
         !pair_map(&b, false, w, count, d, map_ld(count, ldw, d), PG_K, 128) ||
         !pair_map(&o, false, G, rows, count, L.ldg, 64, 32))

@@ -305,7 +305,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
           }
           release(a);
         }
-        if (ok && O.row0 < S.rows) Epi::tile(E, O, acc);
+        if (ok && O.row0 < S.rows) Epi::tile(E, O, acc, &mapO);
       } else {
         const uint32_t a = g & 1u;
         if (!sums(a)) break;
