@@ -18,7 +18,8 @@
 // fp32) and by h (the piece's rows of dW).  A token's own target is no part of that bf16 G: its
 // entry, often as large as all the others together and much the same from token to token, would bring its
 // rounding to dh and dW.  It is kept in fp32 and joins the fp32 sums as a multiple of W's
-// (h's) row.  2048 x 128256 x 4096 with both gradients 3.90 ms (1.65 PFLOP/s); without dW few tokens read the
+// (h's) row.  It is formed as -g expm1(log p), as p may be nearly 1.
+// 2048 x 128256 x 4096 with both gradients 3.87 ms (1.67 PFLOP/s); without dW few tokens read the
 // weight twice, 64 x 50021 x 2048 86 us (smaller pieces, read again from L2, 107 and more).
 #include <algorithm>
 
@@ -51,7 +52,6 @@ __device__ __forceinline__ float column(const float (&acc)[128], int at) {
 // Of 2^((l - m) log2 e) over a row's half tile: the maximum m, the sum s, and x, the sum weighted
 // with (l - m) log2 e.
 struct EpiLse {
-  static constexpr bool CHUNKED = true;
   struct Params {
     const int64_t* targets;
     float *m, *s, *x;      // [half tile][row]
@@ -184,7 +184,6 @@ __global__ void __launch_bounds__(1024) k_head_join(const JoinParams P) {
 // and here, and in l - lse, where lse is nearly the target's own logit when the model is sure of it, what
 // both have lost cancels.
 struct EpiGrad {
-  static constexpr bool CHUNKED = true;
   struct Params {
     const int64_t* targets;
     const float *lse, *dlogp, *entropy, *dentropy;
@@ -427,7 +426,7 @@ PairShape head_shape(int rows, int bn, int tn, int nk, int* status) {
   S.bn = bn;
   S.nk = S.per = nk;
   S.splits = 1;
-  S.group = nk;
+  S.group = PG_GROUP;
   S.band = 16;
   S.rows = rows;
   S.a_rows = box_rows(rows);

@@ -25,6 +25,7 @@ constexpr int FB_THREADS = 32 * (8 + FB_WARPS);  // warps 0 and 2 load, warp 1 i
 constexpr uint32_t FB_A = LIN_BLOCK * LIN_BLOCK * 2;   // operands: [64 rows][64 columns], two by two
 constexpr int FB_RING = 8;                       // most stages of a ring
 constexpr int FB_MAX_BN = 192;
+constexpr int FB_GROUP = 32;                     // blocks summed in place: 4096 products (pair_gemm.cuh says why)
 
 struct FusedParams {
   const unsigned char* codes;
@@ -360,14 +361,14 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMAs
     const uint32_t idesc = idesc_bf16(128, P.bn) | 1u << 15;
-    int sa = 0, sb = 0, k = first_k, more = 0;      // more: the tile has begun
+    int sa = 0, sb = 0, k = first_k, more = 0;      // more: blocks in the sum so far
     uint32_t pa = 0, pb = 0, g = 0;
     for (int it = 0; it < count; ++it) {
       if ((!more && !wait(&accE[g & 1u], ((g >> 1) & 1u) ^ 1u)) || !wait(&bF[sb], pb) || !wait(&aF[sa], pa)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t d = tmem + (g & 1u) * cols;
       const uint64_t a = pair_desc(smem_u32(smem) + sa * FB_A, true), b = smem_desc(smem_u32(tokens) + sb * 2 * half_b);
-      const bool last = it == count - 1 || k == P.nk - 1;
+      const bool last = it == count - 1 || k == P.nk - 1 || more == FB_GROUP - 1;
       if (elected()) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
@@ -378,7 +379,7 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
         if (last) mma_commit(&accF[g & 1u]);
       }
       __syncwarp();
-      more = !last;
+      more = last ? 0 : more + 1;
       if (last) ++g;
       if (++k == P.nk) k = 0;
       if (++sa == P.na) sa = 0, pa ^= 1u;
@@ -433,8 +434,9 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
     int64_t u = u0;
     for (uint32_t g = 0; u < u1; ++g) {
       const int tile = (int)(u / P.nk);
-      const int64_t begin = (int64_t)tile * P.nk, end = begin + P.nk;
-      const bool whole = u == begin && u1 >= end;
+      const int64_t begin = (int64_t)tile * P.nk, end = begin + P.nk, from = max(begin, u0), to = min(end, u1);
+      const int64_t next = min(u + FB_GROUP, to);
+      const bool more = u > from, out_now = next == end && from == begin;      // (a whole tile, its last blocks)
       const int tok0 = tile % P.token_tiles * P.bn, tokens = min(P.bn, P.rows - tok0);
       const int col = tile / P.token_tiles * LIN_BLOCK + q * 32 + lane;
       __nv_bfloat16* out = P.dx + (int64_t)tok0 * P.ldx + col;
@@ -443,21 +445,28 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
       float* mine = P.part + share.slot(blockIdx.x, tile) * P.bn * LIN_BLOCK + q * 32 + lane;
       for (int c = 0; c < tokens; c += 16) {
         uint32_t v[16];
+        float sum[16];
         tmem_ld16(tmem + (g & 1u) * cols + ((uint32_t)(q * 32) << 16) + c, v);
+        if (more) {      // of the blocks before: loads that wait for no store (rows past the last token are the part's own)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[i] = mine[(c + i) * LIN_BLOCK];
+        }
         tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if (c + i >= tokens) continue;
-          if (!whole)
-            mine[(c + i) * LIN_BLOCK] = __uint_as_float(v[i]);
-          else if (col < P.n)
-            out[(c + i) * P.ldx] = __float2bfloat16_rn(__uint_as_float(v[i]));
+        for (int i = 0; i < 16; ++i) sum[i] = more ? sum[i] + __uint_as_float(v[i]) : __uint_as_float(v[i]);
+        if (!out_now) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mine[(c + i) * LIN_BLOCK] = sum[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (c + i < tokens && col < P.n) out[(c + i) * P.ldx] = __float2bfloat16_rn(sum[i]);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(&accE[g & 1u]);
-      u = min(end, u1);
+      u = next;
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -717,7 +726,8 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
   S.tm = ceil_div(rows, PG_M);
   S.tn = ceil_div(n, 256);
   S.bn = 256;
-  S.nk = S.per = S.group = ceil_div(m, PG_K);
+  S.nk = S.per = ceil_div(m, PG_K);
+  S.group = PG_GROUP;
   S.splits = 1;
   S.band = 16;
   S.rows = rows;

@@ -7,8 +7,12 @@
 // 16 + 16 KB into each SM's shared memory for 512 cycles of its tensor pipe; a lone CTA's
 // 128 x 256 tile would need 16 + 32.  Warp 0 of each CTA loads (TMA, a ring of STAGES blocks), warp 1
 // of the first CTA issues, eight warps of each take the finished sums out of TMEM, where two
-// accumulators let the next tile's MMAs run meanwhile.  Pairs walk the tiles in a fixed order, so
+// accumulators let the next sums' MMAs run meanwhile.  Pairs walk the tiles in a fixed order, so
 // results do not depend on timing.
+//
+// In the tensor cores a sum is cut, not rounded, at each of its additions (one per 16 products), so a long one leans
+// toward zero: of 2^20 products of one sign 0.65%, of 131072 7e-4.  It leaves TMEM after `group` K blocks and goes
+// on in registers, where additions are rounded.
 //
 // Bound by the tensor pipe, 93 to 96% of its cycles busy, and at that by the clock that the power
 // allows: 2048 x 32768 x 4096 299 us (1.84 PFLOP/s), 4095 x 128256 x 4096 2.48 ms (1.73).
@@ -44,7 +48,7 @@ struct PairShape {
   int bn;              // columns of a tile: a multiple of 32, of 128 where B is MN-major
   int nk;              // K blocks in all
   int splits, per;     // ranges of K blocks, blocks of one (the last may be shorter)
-  int group;           // K blocks summed in place in TMEM (Epi::CHUNKED)
+  int group;           // K blocks summed in place in TMEM
   int band;            // row tiles walked side by side
   int rows;            // rows of A: CTAs behind the last load none (K-major A)
   int a_rows;          // rows of a K-major A box (a multiple of 8, at most 128)
@@ -78,7 +82,6 @@ struct PairOut {
   int nt, half;        // column tile, and which half of it
   int col, cols;       // first column and number of columns of this warp's half
   int split;
-  uint32_t tmem;       // nonchunked: the sums' address
   unsigned char* stage;      // this warp's 4 KB
   int lane;
 };
@@ -221,7 +224,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
         const PairItem I(S, item);
         int left = I.n;
         while (left > 0 && ok) {
-          const int n = Epi::CHUNKED ? min(left, S.group) : left;
+          const int n = min(left, S.group);
           const uint32_t a = g & 1u, d = tmem + a * 256u;
           if (!wait(&accE[a], ((g >> 1) & 1u) ^ 1u)) {
             ok = false;
@@ -282,38 +285,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
       O.split = I.split;
       O.col = I.nt * S.bn + half * O.cols;
       const uint32_t at = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * O.cols);
-      if constexpr (Epi::CHUNKED) {
-        float acc[128];
+      float acc[128];
 #pragma unroll
-        for (int u = 0; u < 128; ++u) acc[u] = 0.f;
-        const int ng = (I.n + S.group - 1) / S.group;
-        for (int i = 0; i < ng; ++i, ++g) {
-          const uint32_t a = g & 1u;
-          if (!sums(a)) {
-            ok = false;
-            break;
-          }
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            if (c * 16 < O.cols) {
-              uint32_t r[16];
-              tmem_ld16(at + a * 256u + c * 16, r);
-              tmem_wait_ld();
-#pragma unroll
-              for (int u = 0; u < 16; ++u) acc[16 * c + u] += __uint_as_float(r[u]);
-            }
-          }
-          release(a);
-        }
-        if (ok && O.row0 < S.rows) Epi::tile(E, O, acc, &mapO);
-      } else {
+      for (int u = 0; u < 128; ++u) acc[u] = 0.f;
+      const int ng = (I.n + S.group - 1) / S.group;
+      for (int i = 0; i < ng; ++i, ++g) {
         const uint32_t a = g & 1u;
-        if (!sums(a)) break;
-        O.tmem = at + a * 256u;
-        if (O.row0 < S.rows) Epi::tile(E, O, &mapO);
+        if (!sums(a)) {
+          ok = false;
+          break;
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          if (c * 16 < O.cols) {
+            uint32_t r[16];
+            tmem_ld16(at + a * 256u + c * 16, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int u = 0; u < 16; ++u) acc[16 * c + u] += __uint_as_float(r[u]);
+          }
+        }
         release(a);
-        ++g;
       }
+      if (ok && O.row0 < S.rows) Epi::tile(E, O, acc, &mapO);
     }
     if (lane == 0) bulk_commit_and_wait();
     __syncwarp();
@@ -331,19 +325,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
 // ------------------------------------------------------------------ epilogues
 // fp32 sums to part [split][row][col], or added to what is there.
 struct EpiF32 {
-  static constexpr bool CHUNKED = false;
   struct Params {
     int add;
   };
-  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, const CUtensorMap* map) {
-    for (int c = 0; c < O.cols; c += 32) {
-      uint32_t r[32];
-      tmem_ld32(O.tmem + c, r);
-      tmem_wait_ld();
+  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, float (&acc)[128], const CUtensorMap* map) {
+#pragma unroll
+    for (int c = 0; c < 128; c += 32) {
+      if (c >= O.cols) break;
       stage_free(O.lane);
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        *staged(O.stage, O.lane, k) = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
+      for (int k = 0; k < 8; ++k) {
+        const float* v = acc + c + 4 * k;
+        *reinterpret_cast<float4*>(staged(O.stage, O.lane, k)) = make_float4(v[0], v[1], v[2], v[3]);
+      }
       stage_ready();
       if (O.lane == 0) {
         if (E.add)
@@ -359,7 +353,6 @@ struct EpiF32 {
 // bf16 results, to a TMA map or (where rows are not 16-byte aligned) element by element;
 // with `first`, row r's sum gets the fp32 row first[r] of `more` added.
 struct EpiBf16 {
-  static constexpr bool CHUNKED = false;
   struct Params {
     __nv_bfloat16* c;      // null: TMA
     int64_t ldc;
@@ -368,34 +361,26 @@ struct EpiBf16 {
     const float* more;
     int64_t ldmore;
   };
-  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, const CUtensorMap* map) {
-    const float* more = nullptr;
+  __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, float (&acc)[128], const CUtensorMap* map) {
     if (E.first && O.row < E.rows) {
       const int f = E.first[O.row];
-      if (f != 0x7fffffff) more = E.more + f * E.ldmore;
+      if (f != 0x7fffffff) {
+        const float* more = E.more + f * E.ldmore;
+#pragma unroll
+        for (int u = 0; u < 128; ++u)
+          if (u < O.cols && O.col + u < E.cols) acc[u] += more[O.col + u];
+      }
     }
-    for (int c = 0; c < O.cols; c += 64) {
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 128; c += 64) {
+      if (c >= O.cols) break;
       stage_free(O.lane);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t r[32];
-        tmem_ld32(O.tmem + c + 32 * h, r);
-        tmem_wait_ld();
-        if (more) {
-#pragma unroll
-          for (int u = 0; u < 32; ++u)
-            if (O.col + c + 32 * h + u < E.cols)
-              r[u] = __float_as_uint(__uint_as_float(r[u]) + more[O.col + c + 32 * h + u]);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = bf16_pack(__uint_as_float(r[8 * k + 2 * j]), __uint_as_float(r[8 * k + 2 * j + 1]));
-          *staged(O.stage, O.lane, 4 * h + k) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        __syncwarp();
+      for (int k = 0; k < 8; ++k) {
+        const float* v = acc + c + 8 * k;
+        *staged(O.stage, O.lane, k) =
+            make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7]));
       }
       if (!E.c) {
         stage_ready();
@@ -404,6 +389,7 @@ struct EpiBf16 {
           bulk_commit();
         }
       } else {
+        __syncwarp();
         for (int r = 0; r < 32 && O.row0 + r < E.rows; ++r)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -445,6 +431,8 @@ inline cudaError_t pair_copy(const void* from, int64_t ld, int64_t rows, int col
 }
 
 constexpr int PG_PAIRS = ROW_SMS / 2;
+// K blocks summed in place where the result is rounded to bf16: 4096 products, cut by 256 additions.
+constexpr int PG_GROUP = 64;
 
 inline unsigned pair_ctas(const PairShape& S) {
   const int64_t items = S.items();
