@@ -538,8 +538,9 @@ int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float*
  *   workspace device, >= bakron_linear_backward_workspace_bytes(...) bytes, 16-byte aligned; its
  *            first word is the status of this call
  *   sync     as for bakron_linear
- * The sum runs over rows of different scales, so s (c - z) is formed in fp32 and rounded to bf16
- * before it is multiplied; sums are fp32, in a fixed order, and the result is rounded once.
+ * The sum runs over rows of different scales, so these multiply an operand.  Up to 8 tokens c - z is
+ * exact and dy s is kept to 2^-15; above, s (c - z) is rounded to bf16 (within 2^-16 of half a step)
+ * before it is multiplied.  Sums are fp32, in a fixed order, and the result is rounded once.
  */
 size_t bakron_linear_backward_workspace_bytes(const void* dy, int rows, int64_t lddy, int m,
                                               int n, int qmax, int group_size);

@@ -2,15 +2,17 @@
 // What_ij = s (c_ij - z) with the grid (s, z) of row i and j's group.
 //
 // The sum runs over What's rows, whose scales differ, so the scale cannot wait for the end of a
-// sum as it does in the forward product: an operand is s (c - z), rounded once to bf16.
+// sum as it does in the forward product: it multiplies an operand.
 //
-// Up to 8 tokens: mma.sync on operands formed in registers.  Up to FUSED_TOKENS: D (128 columns of
+// Up to 8 tokens: mma.sync on operands formed in registers, c - z (exact) and dy s in two bf16 parts.  Up to FUSED_TOKENS: D (128 columns of
 // What x bn tokens) += A B on the 5th-generation tensor cores with A the operands of a 128 x 128 block, formed
 // from its codes in shared memory as the MMAs take them (MN-major), and B the tokens' gradients, K-major
 // by TMA.  More: the weight is written out in bf16 once, and read by the pair product.
 //
-// us, caches flushed: 1 token, groups of 128, 4096 x 4096 10, 28672 x 8192 47 (2.8 TB/s); 17 tokens through 4099 x 11003
+// us, caches flushed: 1 token, groups of 128, 4096 x 4096 10, 28672 x 8192 55 (2.4 TB/s with the scales); 17 tokens through 4099 x 11003
 // in 8 bits 25; 64 through 11008 x 4096 23, 256 50, 4096 231 (1.6 PFLOP/s; 20 of them to write the weight out).
+#include <float.h>
+
 #include <algorithm>
 
 #include "linear.cuh"
@@ -60,8 +62,7 @@ struct Shares {
   __host__ __device__ __forceinline__ int64_t slot(int cta, int tile) const { return 2 * (int64_t)cta + (begin(cta) / nk != tile); }
 };
 
-// Two values c - z times s, rounded once: s = hi + lo, and what the small product loses is
-// far below the sum's rounding.
+// Two values c - z times s, rounded: s = hi + lo, to 2^-16.
 __device__ __forceinline__ uint32_t scaled(uint32_t v, __nv_bfloat162 hi, __nv_bfloat162 lo) {
   const __nv_bfloat162 c = *reinterpret_cast<__nv_bfloat162*>(&v);
   const __nv_bfloat162 r = __hfma2(c, hi, __hmul2(c, lo));
@@ -105,17 +106,23 @@ __device__ __forceinline__ uint32_t operand(const uint4 (&u)[2], int j, int p, c
 
 // ------------------------------------------------------------------ up to 8 tokens
 // No tensor memory, no shared operands: mma.sync takes What's columns as the rows of its first operand
-// and What's rows as its depth.  A warp has two column blocks and 16 rows at a time: lane group g one of
-// their 8 units (32 columns of a row), lane q of it rows 4q..4q+3, so that a word's 8 columns of two
-// rows become, halves exchanged, operand registers of 4 products.  The order of the 16 rows is free: the
-// tokens' values (its second operand, token g) are those of rows 4q..4q+3.
+// and What's rows as its depth.  A warp has a column block and 16 rows at a time: lane group g unit g & 3 of
+// them (32 columns of a row), and of each word's 8 columns the four that g >> 2 says; lane q of it rows
+// 4q..4q+3, so that two rows' columns become, halves exchanged, operand registers of 2 products.  The order of the
+// 16 rows is free: the tokens' values (its second operand) are those of rows 4q..4q+3.
 //
-// Bound by the products and the operands' forming one after the other: 1 x 28672 x 8192 takes 47 us (DRAM 34% busy; 19 at
-// the memory's rate), with a quarter of the products 29, without the codes' expansion 28.  8 tokens 49, by the kernel
-// below 62.  Sixteen tokens' sums do not leave the registers for two CTAs an SM.
-constexpr int FEW_BACK = 8, FW_COLS = 256, FW_WARPS = 8;
-constexpr int FW_BLOCK = 129, FW_TOKEN = 265;      // strides of the warps' sums, so that lanes meet different banks
+// The first operand is c - z, an integer of 8 bits.  The scale goes to the tokens' side, where a lane has 4 values
+// instead of 64, and the 16 columns of a product have one grid: dy s = hi + lo, two bf16 numbers that keep it to
+// 2^-15, so that the result's rounding is all that counts (s (c - z) rounded to bf16 made the error 1.4 times that and
+// more).  Up to 4 tokens hi and lo are columns of one product, g and g + 4, added at the end; up to 8 a product each.
+//
+// 1 token x 28672 x 8192 55 us, 8 tokens 57: neither products nor codes bound it (twice the products cost nothing), but the
+// way of the codes into registers (2.1 TB/s; through shared memory, 4 stages a warp, 58 and 63).
+constexpr int FEW_BACK = 8, FW_COLS = LIN_BLOCK, FW_WARPS = 8;
+constexpr int FW_TOKEN = FW_COLS + 1;      // stride of the warps' sums
 constexpr int FW_SMEM = FW_WARPS * FEW_BACK * FW_TOKEN * 4;
+constexpr int few_ahead(bool w8, bool one) { return w8 || !one ? 1 : 2; }      // chunks of a warp on their way
+constexpr int few_ctas(bool w8, bool one) { return w8 && !one ? 1 : 2; }      // an SM holds, by their registers
 
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                             uint32_t b1) {
@@ -134,18 +141,58 @@ struct FewParams {
   int rows, m, n, chunks16, per;      // 16-row chunks in all, of a CTA (a multiple of 8)
   const __nv_bfloat16* dy;
   int64_t lddy;
-  int yvec;                           // dy can be read 8 bytes at a time
+  int yvec;                           // dy can be read 8 bytes at a time, and m is a multiple of 4
   float* part;                        // [split][token][column tiles' 256]
   int* status;
 };
 
-template <bool W8, bool ONE>
-__global__ void __launch_bounds__(FW_WARPS * 32, W8 || !ONE ? 1 : 2) k_back_few(const FewParams P) {
+// Two rows' codes of a chunk as c - z in bf16, in the products' order: o[0..1] the first columns of the pairs
+// p = 2 upper + k, o[2..3] their second ones, each register one column of the two rows.  A word is
+// transposed by its bytes first: a pair's columns lie in its bytes `upper` and 2 + `upper` (4 bits), or k and 2 + k.
+// zeros: a byte a row.
+template <bool W8>
+__device__ __forceinline__ void integers(uint32_t w0, uint32_t w1, bool upper, uint32_t zeros, int row, uint32_t (&o)[4]) {
+  if constexpr (W8) {      // 1024 + c in fp16, exact
+    const uint32_t z = __byte_perm(zeros, 0x64646464u, row | 0x4040 | (row + 1) << 8);
+    const uint32_t t[2] = {__byte_perm(w0, w1, 0x5140), __byte_perm(w0, w1, 0x7362)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t v = __byte_perm(t[i >> 1], 0x64646464u, i & 1 ? 0x4342 : 0x4140);
+      const float2 c = __half22float2(__hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&z)));
+      o[i] = bf16_pack(c.x, c.y);
+    }
+  } else {      // 128 + c in bf16
+    const uint32_t z = __byte_perm(zeros, 0x43434343u, row | 0x4040 | (row + 1) << 8);
+    const uint32_t t[2] = {__byte_perm(w0, w1, upper ? 0x0501 : 0x0400), __byte_perm(w0, w1, upper ? 0x0703 : 0x0602)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = pair4(t[i >> 1], i & 1, *reinterpret_cast<const __nv_bfloat162*>(&z));
+  }
+}
+// v = hi + lo: hi its leading 8 bits, lo the rest, rounded.  An infinity is all hi.
+__device__ __forceinline__ void two_parts(const float (&v)[4], uint32_t (&hi)[2], uint32_t (&lo)[2]) {
+  float r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = v[i] - __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+  if (fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))) > FLT_MAX) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = fabsf(v[i]) > FLT_MAX ? 0.f : r[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    hi[i] = __byte_perm(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]), 0x7632);
+    lo[i] = bf16_pack(r[2 * i], r[2 * i + 1]);
+  }
+}
+
+// ONE: the 128 columns of a block have one grid a row.  FOUR: up to 4 tokens.  VEC: dy can be read 8 bytes at a time, and
+// m is a multiple of 4.  (No load stands behind a branch: a value that two ways lead to is waited for where they meet.)
+template <bool W8, bool ONE, bool FOUR, bool VEC>
+__global__ void __launch_bounds__(FW_WARPS * 32, few_ctas(W8, ONE)) k_back_few(const FewParams P) {
   constexpr int UNITS = W8 ? 8 : 4, H = W8 ? 2 : 1, GRIDS = ONE ? 1 : 4;
-  extern __shared__ float fw_sums[];      // [warp][token][column]
+  extern __shared__ float fw_sums[];      // [warp][column of the products][What's column]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int cb = blockIdx.x * 2 + (g >> 2), t = g & 3;
-  const bool there = cb < P.kblocks;
+  const int cb = blockIdx.x, t = g & 3, token = FOUR ? t : g;
+  const bool upper = g >> 2;
   if (blockIdx.x + blockIdx.y + threadIdx.x == 0) *P.status = 0;      // nothing here can run out
   const int first = blockIdx.y * P.per, last = min(first + P.per, P.chunks16);
   int grid[GRIDS];
@@ -155,81 +202,92 @@ __global__ void __launch_bounds__(FW_WARPS * 32, W8 || !ONE ? 1 : 2) k_back_few(
     uint4 u[4][H];
     float4 s[GRIDS];
     uint32_t z[GRIDS];
-    uint32_t y[2];
+    uint32_t y[VEC ? 2 : 4];
   };
+  const __nv_bfloat16* dy = P.dy + min(token, P.rows - 1) * P.lddy;
   auto load = [&](int chunk, Chunk& to) {
     const int row = chunk * 16 + 4 * q;
-    if (there) {
-      const uint4* at = reinterpret_cast<const uint4*>(P.codes) +
-                        (((int64_t)(row >> 7) * P.kblocks + cb) * UNITS + t) * LIN_BLOCK + (row & 127);
+    const uint4* at = reinterpret_cast<const uint4*>(P.codes) +
+                      (((int64_t)(row >> 7) * P.kblocks + cb) * UNITS + t) * LIN_BLOCK + (row & 127);
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int h = 0; h < H; ++h) to.u[r][h] = __ldg(at + h * 4 * LIN_BLOCK + r);
+      for (int h = 0; h < H; ++h) to.u[r][h] = __ldg(at + h * 4 * LIN_BLOCK + r);
 #pragma unroll
-      for (int j = 0; j < GRIDS; ++j) {
-        to.s[j] = __ldg(reinterpret_cast<const float4*>(P.scales + grid[j] * P.mp + row));
-        to.z[j] = __ldg(reinterpret_cast<const uint32_t*>(P.zeros + grid[j] * P.mp + row));
-      }
+    for (int j = 0; j < GRIDS; ++j) {
+      to.s[j] = __ldg(reinterpret_cast<const float4*>(P.scales + grid[j] * P.mp + row));
+      to.z[j] = __ldg(reinterpret_cast<const uint32_t*>(P.zeros + grid[j] * P.mp + row));
     }
-    to.y[0] = to.y[1] = 0u;
-    if (g < P.rows) {
-      const __nv_bfloat16* y = P.dy + g * P.lddy + row;
-      if (P.yvec && row + 4 <= P.m) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(y));
-        to.y[0] = v.x;
-        to.y[1] = v.y;
-      } else {
+    if constexpr (VEC) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(dy + min(row, P.m - 4)));
+      to.y[0] = v.x;
+      to.y[1] = v.y;
+    } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (row + k < P.m) to.y[k >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(y)[k] << (16 * (k & 1));
+      for (int k = 0; k < 4; ++k) to.y[k] = __ldg(reinterpret_cast<const unsigned short*>(dy) + min(row + k, P.m - 1));
+    }
+  };
+  float acc[8][4] = {};
+  auto products = [&](const Chunk& here, int chunk) {
+    uint32_t hi[2], lo[2];
+    float y[4];      // 0 for no token, and behind the last row
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t v = VEC ? (k & 1 ? here.y[k >> 1] & 0xffff0000u : here.y[k >> 1] << 16) : here.y[k] << 16;
+      y[k] = token < P.rows && chunk * 16 + 4 * q + k < P.m ? __uint_as_float(v) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j < GRIDS) {
+        const float4 s = here.s[j];
+        const float v[4] = {y[0] * s.x, y[1] * s.y, y[2] * s.z, y[3] * s.w};
+        two_parts(v, hi, lo);
+        if (FOUR && upper) hi[0] = lo[0], hi[1] = lo[1];
+      }
+      uint32_t a[4], b[4];      // rows 4q, 4q + 1; 4q + 2, 4q + 3
+      auto word = [&](int r) -> uint32_t {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(here.u[r]);
+        return W8 ? (upper ? w[2 * j + 1] : w[2 * j]) : w[j];
+      };
+      integers<W8>(word(0), word(1), upper, here.z[j < GRIDS ? j : 0], 0, a);
+      integers<W8>(word(2), word(3), upper, here.z[j < GRIDS ? j : 0], 2, b);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        mma_16x8x16(acc[2 * j + k], a[k], a[2 + k], b[k], b[2 + k], hi[0], hi[1]);
+        if (!FOUR) mma_16x8x16(acc[2 * j + k], a[k], a[2 + k], b[k], b[2 + k], lo[0], lo[1]);
       }
     }
   };
-  float acc[16][4] = {};
-  Chunk next;
+  constexpr int AHEAD = few_ahead(W8, ONE);
+  Chunk next[AHEAD];
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+  for (int i = 0; i < AHEAD; ++i)
+    if (first + warp + i * FW_WARPS < last) load(first + warp + i * FW_WARPS, next[i]);
+  for (int chunk = first + warp; chunk < last; chunk += AHEAD * FW_WARPS) {
 #pragma unroll
-    for (int h = 0; h < H; ++h) next.u[r][h] = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-  for (int j = 0; j < GRIDS; ++j) next.s[j] = make_float4(0.f, 0.f, 0.f, 0.f), next.z[j] = 0u;
-  if (first + warp < last) load(first + warp, next);
-  for (int chunk = first + warp; chunk < last; chunk += FW_WARPS) {
-    const Chunk here = next;
-    if (chunk + FW_WARPS < last) load(chunk + FW_WARPS, next);
-    RowGrid<W8> rg[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (j == 0 || !ONE) {
-        const float4 s4 = here.s[ONE ? 0 : j];
-        const float sf[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-        for (int r = 0; r < 4; ++r) rg[r].set(sf[r], (float)((here.z[ONE ? 0 : j] >> (8 * r)) & 255u));
-      }
-      uint32_t v[4][4];      // [row][pair of columns]
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int p = 0; p < 4; ++p) v[r][p] = operand(here.u[r], j, p, rg[r]);
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-        mma_16x8x16(acc[4 * j + p], __byte_perm(v[0][p], v[1][p], 0x5410), __byte_perm(v[0][p], v[1][p], 0x7632),
-                    __byte_perm(v[2][p], v[3][p], 0x5410), __byte_perm(v[2][p], v[3][p], 0x7632), here.y[0], here.y[1]);
+    for (int i = 0; i < AHEAD; ++i) {
+      const int c = chunk + i * FW_WARPS;
+      if (i > 0 && c >= last) break;
+      const Chunk here = next[i];
+      if (c + AHEAD * FW_WARPS < last) load(c + AHEAD * FW_WARPS, next[i]);
+      products(here, c);
     }
   }
-  float* mine = fw_sums + warp * FEW_BACK * FW_TOKEN + (g >> 2) * FW_BLOCK + 8 * t;
+  float* mine = fw_sums + warp * FEW_BACK * FW_TOKEN + 8 * t + (upper ? 4 : 0);
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)      // column of the pair e >> 1, token 2q + (e & 1)
-      mine[(2 * q + (e & 1)) * FW_TOKEN + 32 * (i >> 2) + 2 * (i & 3) + (e >> 1)] = acc[i][e];
+    for (int e = 0; e < 4; ++e)      // column of the pair e >> 1, of the products 2q + (e & 1)
+      mine[(2 * q + (e & 1)) * FW_TOKEN + 32 * (i >> 1) + 2 * (i & 1) + (e >> 1)] = acc[i][e];
   __syncthreads();
-  const int c = threadIdx.x;      // FW_COLS threads
-  for (int tok = 0; tok < P.rows; ++tok) {
+  const int c = threadIdx.x % FW_COLS;
+  for (int tok = threadIdx.x / FW_COLS; tok < P.rows; tok += FW_WARPS * 32 / FW_COLS) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < FW_WARPS; ++w) v += fw_sums[(w * FEW_BACK + tok) * FW_TOKEN + c + (c >> 7) * (FW_BLOCK - 128)];
+    for (int w = 0; w < FW_WARPS; ++w) {
+      v += fw_sums[(w * FEW_BACK + tok) * FW_TOKEN + c];
+      if (FOUR) v += fw_sums[(w * FEW_BACK + tok + 4) * FW_TOKEN + c];
+    }
     P.part[(((int64_t)blockIdx.y * P.rows + tok) * gridDim.x + blockIdx.x) * FW_COLS + c] = v;
   }
   pdl_trigger();
@@ -559,6 +617,8 @@ __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
 constexpr int FUSED_TOKENS = 384;
 constexpr uint32_t FB_SMEM = 227 * 1024 - 1024;      // beside the barriers
 
+bool one_grid(int n, int group_size) { return group_size == 0 || group_size == n || group_size % LIN_BLOCK == 0; }
+
 // How up to FUSED_TOKENS tokens are shared out.
 static_assert(ROW_SMS <= 256, "a thread a flag");
 struct FusedPlan {
@@ -581,15 +641,24 @@ struct FusedPlan {
   }
 };
 
-// How up to 8 tokens are: two CTAs an SM, each at least 128 rows, and no more than 64 parts to add.
+// How up to 8 tokens are: the rows in so many parts (64 at most) that the CTAs, as many at a time as the SMs hold, are done
+// first, where a CTA costs 256 rows (16 chunks) beside its own.  1 token x 28672 x 8192, 64 tiles: 4 parts (256 CTAs of 304)
+// 59 us, 9 (576 of 608) 55, 14 56; 4096 x 11008, 86 tiles: 3 parts 18, 4 20.
 struct FewPlan {
   int tiles, chunks, per, splits;
-  FewPlan(int m, int n) {
+  FewPlan(int m, int n, bool bytes8, bool one) {
     tiles = ceil_div(n, FW_COLS);
     chunks = ceil_div(m, 16);
-    const int most = std::max(1, std::min(2 * ROW_SMS / tiles, 64));
-    per = (int)round_up(ceil_div(chunks, most), FW_WARPS);
-    splits = ceil_div(chunks, per);
+    const int slots = few_ctas(bytes8, one) * ROW_SMS;
+    int64_t best = INT64_MAX;
+    for (int s = 1; s <= 64; ++s) {
+      const int rows = (int)round_up(ceil_div(chunks, s), FW_WARPS), parts = ceil_div(chunks, rows);
+      const int64_t cost = (int64_t)ceil_div(tiles * parts, slots) * (rows + 16);
+      if (cost >= best) continue;
+      best = cost;
+      per = rows;
+      splits = parts;
+    }
   }
 };
 
@@ -597,7 +666,7 @@ struct BackLayout {
   size_t dy = 0, flags = 0, part = 0, w = 0, bytes;
   bool copy;
   int64_t ldw;
-  BackLayout(const void* p, int rows, int64_t ld, int m, int n, const FusedPlan& F) {
+  BackLayout(const void* p, int rows, int64_t ld, int m, int n, bool bytes8, bool one, const FusedPlan& F) {
     size_t at = 256;
     auto take = [&](size_t b) {
       const size_t r = at;
@@ -608,7 +677,7 @@ struct BackLayout {
     if (copy) dy = take((size_t)rows * round_up(m, 8) * 2);
     ldw = round_up(n, LIN_BLOCK);
     if (rows <= FEW_BACK) {
-      const FewPlan few(m, n);
+      const FewPlan few(m, n, bytes8, one);
       part = take((size_t)few.splits * rows * few.tiles * FW_COLS * 4);
     } else if (rows <= FUSED_TOKENS) {
       flags = take((size_t)F.ctas * sizeof(int));
@@ -619,16 +688,13 @@ struct BackLayout {
     bytes = at;
   }
 };
-bool one_grid(int n, int group_size) { return group_size == 0 || group_size == n || group_size % LIN_BLOCK == 0; }
 
 template <bool W8, bool ONE>
 cudaError_t few_launch(const FewParams& P, const FewPlan& F, cudaStream_t s) {
-  static OncePerDevice once;
-  const cudaError_t e = once([] {
-    return cudaFuncSetAttribute(k_back_few<W8, ONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, FW_SMEM);
-  });
-  if (e != cudaSuccess) return e;
-  k_back_few<W8, ONE><<<dim3((unsigned)F.tiles, (unsigned)F.splits), FW_WARPS * 32, FW_SMEM, s>>>(P);
+  const dim3 grid((unsigned)F.tiles, (unsigned)F.splits);
+  const auto kernel = P.rows <= 4 ? (P.yvec ? k_back_few<W8, ONE, true, true> : k_back_few<W8, ONE, true, false>)
+                                  : (P.yvec ? k_back_few<W8, ONE, false, true> : k_back_few<W8, ONE, false, false>);
+  kernel<<<grid, FW_WARPS * 32, FW_SMEM, s>>>(P);
   return cudaGetLastError();
 }
 
@@ -658,7 +724,7 @@ using namespace bakron;
 extern "C" size_t bakron_linear_backward_workspace_bytes(const void* dy, int rows, int64_t lddy, int m, int n, int qmax,
                                                          int group_size) {
   return back_ok(rows, m, n, qmax, group_size) && rows > 0
-             ? BackLayout(dy, rows, lddy, m, n, FusedPlan(rows, m, n, qmax > 15, one_grid(n, group_size))).bytes
+             ? BackLayout(dy, rows, lddy, m, n, qmax > 15, one_grid(n, group_size), FusedPlan(rows, m, n, qmax > 15, one_grid(n, group_size))).bytes
              : 0;
 }
 
@@ -672,17 +738,17 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
     return BAKRON_ERR_INVALID_ARG;
   const bool one = one_grid(n, group_size);
   const FusedPlan plan(rows, m, n, qmax > 15, one);
-  const BackLayout B(dy, rows, lddy, m, n, plan);
+  const BackLayout B(dy, rows, lddy, m, n, qmax > 15, one, plan);
   if (workspace_bytes < B.bytes) return BAKRON_ERR_WORKSPACE;
   const WeightLayout L(m, n, qmax, group_size);
   const unsigned char* p = (const unsigned char*)packed;
   cudaStream_t s = (cudaStream_t)stream;
   char* ws = (char*)workspace;
   if (rows <= FEW_BACK) {
-    const FewPlan few(m, n);
+    const FewPlan few(m, n, L.bytes8, one);
     FewParams F{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, L.mp, (int)(L.np / LIN_BLOCK),
                 L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, rows, m, n, few.chunks, few.per,
-                (const __nv_bfloat16*)dy, lddy, ((uintptr_t)dy | (uintptr_t)(rows > 1 ? lddy * 2 : 0)) % 8 == 0,
+                (const __nv_bfloat16*)dy, lddy, m % 4 == 0 && ((uintptr_t)dy | (uintptr_t)(rows > 1 ? lddy * 2 : 0)) % 8 == 0,
                 (float*)(ws + B.part), (int*)ws};
     const auto launch = L.bytes8 ? (one ? few_launch<true, true> : few_launch<true, false>)
                                  : (one ? few_launch<false, true> : few_launch<false, false>);
