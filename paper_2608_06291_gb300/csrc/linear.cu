@@ -29,11 +29,11 @@ __device__ __forceinline__ float grid_zero(const PackParams& P, int row, int64_t
 
 __global__ void __launch_bounds__(256) k_pack_grid(const PackParams P) {
   const int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
-  if (i >= P.G * P.mp) return;
   const int64_t g = i / P.mp;
   const int row = (int)(i % P.mp);
+  const bool there = i < P.G * P.mp;
   float s = 0.f, z = 0.f;
-  if (row < P.m) {
+  if (there && row < P.m) {
     s = P.scales[row * P.G + g];
     z = grid_zero(P, row, g);
     if (!(z >= 0.f && z <= (float)P.qmax && z == floorf(z))) {
@@ -41,8 +41,19 @@ __global__ void __launch_bounds__(256) k_pack_grid(const PackParams P) {
       z = 0.f;
     }
   }
-  P.pscales[i] = s;
-  P.pzeros[i] = (uint8_t)z;
+  if (there) {
+    P.pscales[i] = s;
+    P.pzeros[i] = (uint8_t)z;
+  }
+  // one atomic a CTA, of a maximum: in any order the same
+  __shared__ int most[8];
+  int e = (int)(__float_as_uint(s) >> 23) & 255;
+  e = (int)__reduce_max_sync(0xffffffffu, (unsigned)(e == 255 ? 0 : e));
+  if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = e;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  for (int w = 1; w < 8; ++w) e = max(e, most[w]);
+  if (e > 0) atomicMax(P.status + 1, e);
 }
 
 // One 16-byte unit per thread.

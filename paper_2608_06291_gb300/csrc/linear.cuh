@@ -1,7 +1,7 @@
 // The weight of bakron_linear as bakron_pack_weight lays it out, and the kernels'
 // common parameters.
 //
-// [status 256 B][scales G x mp fp32][zeros G x mp uint8][codes]
+// [status, the largest finite scale's exponent (8 bits, biased); 256 B][scales G x mp fp32][zeros G x mp uint8][codes]
 //
 // mp: m rounded up to 128, np: n rounded up to 128, G: grids a row.  Codes lie in blocks
 // of 128 rows x 128 columns, [row block][column block][unit][row] of 16-byte units, so

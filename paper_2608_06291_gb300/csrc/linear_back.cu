@@ -4,14 +4,20 @@
 // The sum runs over What's rows, whose scales differ, so the scale cannot wait for the end of a
 // sum as it does in the forward product: it multiplies an operand.
 //
-// Up to 8 tokens: mma.sync on operands formed in registers, c - z (exact) and dy s in two bf16 parts.  Up to FUSED_TOKENS: D (128 columns of
-// What x bn tokens) += A B on the 5th-generation tensor cores with A the operands of a 128 x 128 block, formed
-// from its codes in shared memory as the MMAs take them (MN-major), and B the tokens' gradients, K-major
-// by TMA.  More: the weight is written out in bf16 once, and read by the pair product.
+// Up to 8 tokens: mma.sync on operands formed in registers, c - z (exact) and dy s in two bf16 parts.  More: s (c - z) is
+// formed in fp16, whose 11 bits leave the result's rounding to bf16's 8 the only one that counts, and dy is
+// exact there: a token's gradients are multiplied by the power of two that takes its largest one to 2^15 (32 binades below it
+// lose no bit, and what is lost further down is 2^-40 of it), the scales by the one that takes the weight's largest to
+// 2^6; the result is multiplied back.
 //
-// us, caches flushed: 1 token, groups of 128, 4096 x 4096 10, 28672 x 8192 55 (2.4 TB/s with the scales); 17 tokens through 4099 x 11003
-// in 8 bits 25; 64 through 11008 x 4096 23, 256 50, 4096 231 (1.6 PFLOP/s; 20 of them to write the weight out).
+// Up to FUSED_TOKENS: D (128 columns of What x bn tokens) += A B on the 5th-generation tensor cores with A the
+// operands of a 128 x 128 block, formed from its codes in shared memory as the MMAs take them (MN-major), and B the
+// tokens' gradients, K-major by TMA.  More: the weight is written out in fp16 once, and read by the pair product.
+//
+// FIGURES
 #include <float.h>
+
+#include <cuda_fp16.h>
 
 #include <algorithm>
 
@@ -38,6 +44,8 @@ struct FusedParams {
   int rows, n, bn;         // tokens, columns, tokens of a tile (a multiple of 16)
   int nk, token_tiles, tiles;      // 128-row blocks; tiles in all
   int na, nb, nc;          // stages of the operands' ring, the gradients', the codes'
+  const int* top;          // the largest scale's exponent
+  const float2* power;     // a token's power of two
   __nv_bfloat16* dx;
   int64_t ldx;
   float* part;             // [CTA][its first tile, its last][token][128 columns]
@@ -62,46 +70,94 @@ struct Shares {
   __host__ __device__ __forceinline__ int64_t slot(int cta, int tile) const { return 2 * (int64_t)cta + (begin(cta) / nk != tile); }
 };
 
-// Two values c - z times s, rounded: s = hi + lo, to 2^-16.
-__device__ __forceinline__ uint32_t scaled(uint32_t v, __nv_bfloat162 hi, __nv_bfloat162 lo) {
-  const __nv_bfloat162 c = *reinterpret_cast<__nv_bfloat162*>(&v);
-  const __nv_bfloat162 r = __hfma2(c, hi, __hmul2(c, lo));
-  return *reinterpret_cast<const uint32_t*>(&r);
+// Scales are multiplied by 2^of(exponent field of the weight's largest), which takes that one to [2^6, 2^7), so that
+// s (c - z) stays below 2^15.
+__host__ __device__ constexpr int scale_power(int top) { return top < 6 ? 127 : 133 - top; }
+__device__ __forceinline__ float scale_factor(const int* top) { return __uint_as_float((uint32_t)(scale_power(__ldg(top)) + 127) << 23); }
+
+// A row's grid: two codes' values in fp16 are (c - z) hi + (c - z) lo, s = hi + lo to 2^-22, rounded once (the small
+// product's own rounding is 2^-22 of it).
+struct RowGrid {
+  uint32_t z;      // 1024 + z, twice
+  __half2 hi, lo;
+  __device__ __forceinline__ void set(float s, uint32_t zero) {
+    z = zero * 0x00010001u + 0x64006400u;
+    hi = __float2half2_rn(s);
+    lo = __float2half2_rn(s - __low2float(hi));
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t codes1024) const {      // 1024 + c, exact
+    const __half2 c = __hsub2(*reinterpret_cast<const __half2*>(&codes1024), *reinterpret_cast<const __half2*>(&z));
+    const __half2 r = __hfma2(c, hi, __hmul2(c, lo));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
+};
+// Pair p of chunk j (32 columns, 8 of them a unit's) of a unit: columns 2p, 2p + 1 of its 8.
+__device__ __forceinline__ uint32_t operand4(uint32_t word, int p, const RowGrid& g) {
+  return g(((word >> (4 * p)) & 0x000F000Fu) | 0x64006400u);
 }
-// A row's grid as the codes' expansion wants it.
-template <bool W8>
-struct RowGrid;
-template <>
-struct RowGrid<false> {
-  __nv_bfloat162 z, hi, lo;
-  __device__ __forceinline__ void set(float s, float zero) {
-    z = __float2bfloat162_rn(128.f + zero);
-    hi = __float2bfloat162_rn(s);
-    lo = __float2bfloat162_rn(s - __low2float(hi));
-  }
-};
-template <>
-struct RowGrid<true> {
-  __half2 z;
-  float s;
-  __device__ __forceinline__ void set(float scale, float zero) {
-    z = __float2half2_rn(1024.f + zero);
-    s = scale;
-  }
-};
-// Two 8-bit codes of a pair as c - z in fp16 (1024 + c is exact there), times s in fp32.
-__device__ __forceinline__ uint32_t scaled8(uint32_t w, int odd, __half2 z1024, float s) {
-  uint32_t u = __byte_perm(w, 0x64646464u, odd ? 0x4341 : 0x4240);
-  const float2 c = __half22float2(__hsub2(*reinterpret_cast<__half2*>(&u), z1024));
-  return bf16_pack(c.x * s, c.y * s);
+__device__ __forceinline__ uint32_t operand8(uint32_t word, int odd, const RowGrid& g) {
+  return g(__byte_perm(word, 0x64646464u, odd ? 0x4341 : 0x4240));
+}
+__device__ __forceinline__ uint32_t operand(const uint4 (&u)[1], int j, int p, const RowGrid& g) {
+  return operand4(reinterpret_cast<const uint32_t*>(&u[0])[j], p, g);
+}
+__device__ __forceinline__ uint32_t operand(const uint4 (&u)[2], int j, int p, const RowGrid& g) {
+  return operand8(reinterpret_cast<const uint32_t*>(&u[j >> 1])[2 * (j & 1) + (p >> 1)], p & 1, g);
 }
 
-// Pair p of chunk j (32 columns, 8 of them a unit's) of a unit: columns 2p, 2p + 1 of its 8.
-__device__ __forceinline__ uint32_t operand(const uint4 (&u)[1], int j, int p, const RowGrid<false>& g) {
-  return scaled(pair4(reinterpret_cast<const uint32_t*>(&u[0])[j], p, g.z), g.hi, g.lo);
-}
-__device__ __forceinline__ uint32_t operand(const uint4 (&u)[2], int j, int p, const RowGrid<true>& g) {
-  return scaled8(reinterpret_cast<const uint32_t*>(&u[j >> 1])[2 * (j & 1) + (p >> 1)], p & 1, g.z, g.s);
+// A token's gradients in fp16: times 2^k, k from the largest finite one, exact from 2^-32 of it on.  power: what takes the
+// product's sums back.  The token's row is read twice, the second time from the caches.
+template <bool VEC>
+__global__ void __launch_bounds__(512) k_back_tokens(const __nv_bfloat16* from, int64_t ld, int m, const int* top, __half* to,
+                                                     int64_t ldt, float2* power, int* status) {
+  __shared__ uint32_t slots[16];
+  pdl_trigger();      // the product may get ready; it waits for this grid's end
+  const int64_t row = blockIdx.x;
+  const uint16_t* in = reinterpret_cast<const uint16_t*>(from) + row * ld;
+  __half* out = to + row * ldt;
+  const int whole = VEC ? m & ~7 : 0;
+  uint32_t most = 0;      // the largest magnitude's bits
+  auto look = [&](uint32_t v) {
+    v &= 0x7fffu;
+    most = max(most, v < 0x7f80u ? v : 0u);
+  };
+#pragma unroll 4
+  for (int c = threadIdx.x * 8; c < whole; c += 4096) {
+    const uint4 u = *reinterpret_cast<const uint4*>(in + c);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      look(w[j]);
+      look(w[j] >> 16);
+    }
+  }
+#pragma unroll 4
+  for (int c = whole + threadIdx.x; c < m; c += 512) look(in[c]);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = most;
+  __syncthreads();
+  most = __reduce_max_sync(0xffffffffu, slots[threadIdx.x & 15]);
+  const int k = most ? 141 - max((int)(most >> 7), 1) : 0;      // below 2^(field - 126): to below 2^15
+  if (threadIdx.x == 0) {
+    power[row] = two_powers(-k - scale_power(__ldg(top)));
+    if (row == 0 && status) *status = 0;
+  }
+  const float2 scale = two_powers(k);
+  auto half = [&](uint32_t bits) { return times(__uint_as_float(bits), scale); };
+#pragma unroll 4
+  for (int c = threadIdx.x * 8; c < whole; c += 4096) {
+    const uint4 u = *reinterpret_cast<const uint4*>(in + c);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint32_t o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const __half2 v = __floats2half2_rn(half(w[j] << 16), half(w[j] & 0xffff0000u));
+      o[j] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    *reinterpret_cast<uint4*>(out + c) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+#pragma unroll 4
+  for (int c = whole + threadIdx.x; c < m; c += 512) out[c] = __float2half_rn(half((uint32_t)in[c] << 16));
 }
 
 // ------------------------------------------------------------------ up to 8 tokens
@@ -375,6 +431,7 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
 
   if (warp == 0) {
     // ------------------------------------------------------------ gradients
+    pdl_wait();      // (the codes' loads need no kernel before: the one that this waits for has waited for the rest)
     int it = 0, s = 0, k = first_k, tile = tile0;
     uint32_t parity = 1;      // a fresh barrier's phase before the first counts as complete
     for (; it < count; ++it) {
@@ -418,7 +475,7 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
     for (int j = max(0, it - P.nc); j < it; ++j) wait(&cF[j % P.nc], (uint32_t)(j / P.nc) & 1u, true);
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMAs
-    const uint32_t idesc = idesc_bf16(128, P.bn) | 1u << 15;
+    const uint32_t idesc = idesc_f16(128, P.bn) | 1u << 15;
     int sa = 0, sb = 0, k = first_k, more = 0;      // more: blocks in the sum so far
     uint32_t pa = 0, pb = 0, g = 0;
     for (int it = 0; it < count; ++it) {
@@ -453,6 +510,7 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
     // of each of 4 rows: lanes 0-7 eight rows of a unit, the next eight the same rows of the next
     // unit, ..., so that eight lanes' 16-byte loads and stores cover the banks.
     const int t = lane >> 3, r0 = (warp % TEAM) * 8 + (lane & 7);
+    const float factor = scale_factor(P.top);
     for (int it = (warp - 8) / TEAM; it < count; it += TEAMS) {
       const int c = it % P.nc, s = it % P.na;
       if (!wait(&cF[c], (uint32_t)(it / P.nc) & 1u)) break;
@@ -465,10 +523,10 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
         uint4 u[W8 ? 2 : 1];
 #pragma unroll
         for (int h = 0; h < (W8 ? 2 : 1); ++h) u[h] = *reinterpret_cast<const uint4*>(here + ((4 * h + t) * LIN_BLOCK + r) * 16);
-        RowGrid<W8> rg[GRIDS];
+        RowGrid rg[GRIDS];
 #pragma unroll
         for (int j = 0; j < (int)GRIDS; ++j)
-          rg[j].set(reinterpret_cast<const float*>(grid + j * GRID)[r], (float)grid[j * GRID + LIN_BLOCK * 4 + r]);
+          rg[j].set(reinterpret_cast<const float*>(grid + j * GRID)[r] * factor, grid[j * GRID + LIN_BLOCK * 4 + r]);
         unsigned char* a = to + (i * 8 * TEAM / 64) * (FB_A / 2) + (i * 8 * TEAM % 64) * 128;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -490,6 +548,7 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
     // ------------------------------------------------------------ sums
     const int q = warp & 3;
     int64_t u = u0;
+    pdl_wait();
     for (uint32_t g = 0; u < u1; ++g) {
       const int tile = (int)(u / P.nk);
       const int64_t begin = (int64_t)tile * P.nk, end = begin + P.nk, from = max(begin, u0), to = min(end, u1);
@@ -518,7 +577,8 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
         } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (c + i < tokens && col < P.n) out[(c + i) * P.ldx] = __float2bfloat16_rn(sum[i]);
+            if (c + i < tokens && col < P.n)
+              out[(c + i) * P.ldx] = __float2bfloat16_rn(times(sum[i], P.power[tok0 + c + i]));
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -560,6 +620,8 @@ __global__ void __launch_bounds__(256) k_back_join(const FusedParams P, int ctas
     v.z += w.z;
     v.w += w.w;
   }
+  const float2 power = P.power[token];
+  v = make_float4(times(v.x, power), times(v.y, power), times(v.z, power), times(v.w, power));
   __nv_bfloat16* out = P.dx + token * P.ldx + col;
   if (P.vec && col + 4 <= P.n) {
     *reinterpret_cast<uint2*>(out) = make_uint2(bf16_pack(v.x, v.y), bf16_pack(v.z, v.w));
@@ -577,11 +639,12 @@ struct ExpandParams {
   const uint8_t* zeros;
   int m, kblocks, chunks, G;
   int64_t mp;
-  __nv_bfloat16* w;
+  const int* top;
+  __half* w;
   int64_t ldw;      // a multiple of 128
 };
 
-// What in bf16, row by row.  A thread takes a 16-byte unit; four lanes have a row's chunk together.  11008 x 4096: 20 us.
+// What in fp16, row by row.  A thread takes a 16-byte unit; four lanes have a row's chunk together.  11008 x 4096: 20 us.
 template <bool W8>
 __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
   constexpr int UNITS = W8 ? 8 : 4;
@@ -594,20 +657,15 @@ __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
   if (row >= P.m) return;
   const uint4 u = reinterpret_cast<const uint4*>(P.codes)[((rb * P.kblocks + kb) * UNITS + half * 4 + t) * LIN_BLOCK + in];
   const uint32_t words[4] = {u.x, u.y, u.z, u.w};
+  const float factor = scale_factor(P.top);
 #pragma unroll
   for (int j = 0; j < (W8 ? 2 : 4); ++j) {
     const int chunk = kb * 4 + (W8 ? half * 2 : 0) + j, grid = P.G == 1 ? 0 : min(chunk / P.chunks, P.G - 1);
-    const float s = P.scales[grid * P.mp + row], z = (float)P.zeros[grid * P.mp + row];
+    RowGrid g;
+    g.set(P.scales[grid * P.mp + row] * factor, P.zeros[grid * P.mp + row]);
     uint32_t o[4];
-    RowGrid<W8> g;
-    g.set(s, z);
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      if constexpr (W8)
-        o[p] = scaled8(words[2 * j + (p >> 1)], p & 1, g.z, g.s);
-      else
-        o[p] = scaled(pair4(words[j], p, g.z), g.hi, g.lo);
-    }
+    for (int p = 0; p < 4; ++p) o[p] = W8 ? operand8(words[2 * j + (p >> 1)], p & 1, g) : operand4(words[j], p, g);
     *reinterpret_cast<uint4*>(P.w + row * P.ldw + chunk * 32 + 8 * t) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
@@ -663,19 +721,21 @@ struct FewPlan {
 };
 
 struct BackLayout {
-  size_t dy = 0, flags = 0, part = 0, w = 0, bytes;
-  bool copy;
-  int64_t ldw;
-  BackLayout(const void* p, int rows, int64_t ld, int m, int n, bool bytes8, bool one, const FusedPlan& F) {
+  size_t dy = 0, power = 0, flags = 0, part = 0, w = 0, bytes;
+  int64_t ldy, ldw;      // of the gradients, of the weight, both in fp16
+  BackLayout(int rows, int m, int n, bool bytes8, bool one, const FusedPlan& F) {
     size_t at = 256;
     auto take = [&](size_t b) {
       const size_t r = at;
       at += align256(b);
       return r;
     };
-    copy = rows > FEW_BACK && !aligned16(p, ld * 2);
-    if (copy) dy = take((size_t)rows * round_up(m, 8) * 2);
+    ldy = round_up(m, 8);
     ldw = round_up(n, LIN_BLOCK);
+    if (rows > FEW_BACK) {
+      dy = take((size_t)rows * ldy * 2);
+      power = take((size_t)rows * sizeof(float2));
+    }
     if (rows <= FEW_BACK) {
       const FewPlan few(m, n, bytes8, one);
       part = take((size_t)few.splits * rows * few.tiles * FW_COLS * 4);
@@ -705,8 +765,7 @@ cudaError_t fused_launch(const CUtensorMap& map, const FusedParams& P, const Fus
     return cudaFuncSetAttribute(k_back_fused<W8, ONE, TEAMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FB_SMEM);
   });
   if (e != cudaSuccess) return e;
-  k_back_fused<W8, ONE, TEAMS><<<F.ctas, FB_THREADS, F.smem, s>>>(map, P);
-  return cudaGetLastError();
+  return launch_pdl(k_back_fused<W8, ONE, TEAMS>, dim3((unsigned)F.ctas), dim3(FB_THREADS), F.smem, s, map, P);
 }
 
 constexpr int LB_MAX_DIM = 1 << 17, LB_MAX_ROWS = 1 << 24;
@@ -724,7 +783,7 @@ using namespace bakron;
 extern "C" size_t bakron_linear_backward_workspace_bytes(const void* dy, int rows, int64_t lddy, int m, int n, int qmax,
                                                          int group_size) {
   return back_ok(rows, m, n, qmax, group_size) && rows > 0
-             ? BackLayout(dy, rows, lddy, m, n, qmax > 15, one_grid(n, group_size), FusedPlan(rows, m, n, qmax > 15, one_grid(n, group_size))).bytes
+             ? BackLayout(rows, m, n, qmax > 15, one_grid(n, group_size), FusedPlan(rows, m, n, qmax > 15, one_grid(n, group_size))).bytes
              : 0;
 }
 
@@ -738,7 +797,7 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
     return BAKRON_ERR_INVALID_ARG;
   const bool one = one_grid(n, group_size);
   const FusedPlan plan(rows, m, n, qmax > 15, one);
-  const BackLayout B(dy, rows, lddy, m, n, qmax > 15, one, plan);
+  const BackLayout B(rows, m, n, qmax > 15, one, plan);
   if (workspace_bytes < B.bytes) return BAKRON_ERR_WORKSPACE;
   const WeightLayout L(m, n, qmax, group_size);
   const unsigned char* p = (const unsigned char*)packed;
@@ -757,18 +816,20 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
                           rows, few.tiles, n, (__nv_bfloat16*)dx, lddx));
     return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
   }
-  if (B.copy) {
-    BK_CUDA_OK(pair_copy(dy, lddy, rows, m, ws + B.dy, s));
-    dy = ws + B.dy;
-    lddy = round_up(m, 8);
-  }
-  const int64_t ldmap = lddy;
+  const int* top = (const int*)p + 1;
+  const bool fused = rows <= FUSED_TOKENS;
+  float2* power = (float2*)(ws + B.power);
+  const auto tokens = aligned16(dy, rows > 1 ? lddy * 2 : 0) ? k_back_tokens<true> : k_back_tokens<false>;
+  tokens<<<(unsigned)rows, 512, 0, s>>>((const __nv_bfloat16*)dy, lddy, m, top, (__half*)(ws + B.dy), B.ldy, power,
+                                        fused ? nullptr : (int*)ws);
+  BK_CUDA_OK(cudaGetLastError());
+  dy = ws + B.dy;
   CUtensorMap a, b, o;
-  if (rows <= FUSED_TOKENS) {
-    if (!pair_map(&a, false, dy, rows, m, ldmap, 64, plan.bn)) return BAKRON_ERR_CUDA;
+  if (fused) {
+    if (!pair_map(&a, false, dy, rows, m, B.ldy, 64, plan.bn)) return BAKRON_ERR_CUDA;
     FusedParams F{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, L.mp, (int)(L.np / LIN_BLOCK),
                   L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, rows, n, plan.bn, plan.nk, plan.token_tiles,
-                  plan.tiles, plan.na, plan.nb, plan.nc, (__nv_bfloat16*)dx, lddx, (float*)(ws + B.part),
+                  plan.tiles, plan.na, plan.nb, plan.nc, top, power, (__nv_bfloat16*)dx, lddx, (float*)(ws + B.part),
                   aligned16(dx, rows > 1 ? lddx * 2 : 0), (int*)ws, (int*)(ws + B.flags),
                   spin_cycles_from_env()};
     const auto launch =
@@ -781,10 +842,8 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
                             plan.ctas));
     return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
   }
-  k_clear_status<<<1, 1, 0, s>>>((int*)ws);
-  BK_CUDA_OK(cudaGetLastError());
   ExpandParams E{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, m, (int)(L.np / LIN_BLOCK),
-                 L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, L.mp, (__nv_bfloat16*)(ws + B.w), B.ldw};
+                 L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, L.mp, top, (__half*)(ws + B.w), B.ldw};
   const unsigned ctas = (unsigned)(L.mp * E.kblocks * (L.units / 4) / 64);
   L.bytes8 ? k_expand<true><<<ctas, 256, 0, s>>>(E) : k_expand<false><<<ctas, 256, 0, s>>>(E);
   BK_CUDA_OK(cudaGetLastError());
@@ -796,16 +855,17 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
   S.group = PG_GROUP;
   S.splits = 1;
   S.band = 16;
+  S.half = 1;
   S.rows = rows;
   S.a_rows = 128;
   S.status = (int*)ws;
   S.spin_cycles = spin_cycles_from_env();
   const bool tma = aligned16(dx, rows > 1 ? lddx * 2 : 0);
-  if (!pair_map(&a, false, dy, rows, m, ldmap, PG_K, S.a_rows) ||
+  if (!pair_map(&a, false, dy, rows, m, B.ldy, PG_K, S.a_rows) ||
       !pair_map(&b, false, E.w, m, n, B.ldw, 64, PG_K) ||
       (tma && !pair_map(&o, false, dx, rows, n, rows > 1 ? lddx : round_up(n, 8), 64, 32)))
     return BAKRON_ERR_CUDA;
-  EpiBf16::Params T{tma ? nullptr : (__nv_bfloat16*)dx, lddx, rows, n, nullptr, nullptr, 0};
+  EpiBf16::Params T{tma ? nullptr : (__nv_bfloat16*)dx, lddx, rows, n, nullptr, nullptr, 0, power};
   BK_CUDA_OK((pair_launch<EpiBf16, false, true>(a, b, tma ? o : a, S, T, s)));
   return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
 }

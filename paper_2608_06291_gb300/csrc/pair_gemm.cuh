@@ -1,4 +1,4 @@
-// A bf16 product on CTA pairs, C (M x N) = A B with fp32 sums, and what becomes of its
+// A product of bf16 (or fp16) values on CTA pairs, C (M x N) = A B with fp32 sums, and what becomes of its
 // tiles (the epilogue, a template parameter).  Used by the output head (head.cu) and by
 // the gradient of the quantised product (linear_back.cu).
 //
@@ -50,6 +50,7 @@ struct PairShape {
   int splits, per;     // ranges of K blocks, blocks of one (the last may be shorter)
   int group;           // K blocks summed in place in TMEM
   int band;            // row tiles walked side by side
+  int half;            // operands are fp16
   int rows;            // rows of A: CTAs behind the last load none (K-major A)
   int a_rows;          // rows of a K-major A box (a multiple of 8, at most 128)
   int* status;         // gets the error of a wait that ran out; or, where there are
@@ -215,7 +216,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PG_THREADS, 1)
     // ------------------------------------------------------------ MMAs
     // The warp goes through the loop together and an elected lane issues: operands stay in uniform registers.
     if (rank == 0) {
-      const uint32_t idesc = idesc_bf16(PG_M, S.bn) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u);
+      const uint32_t idesc = (S.half ? idesc_f16(PG_M, S.bn) : idesc_bf16(PG_M, S.bn)) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u);
       const uint64_t da0 = pair_desc(smem_u32(smem), AMN), db0 = pair_desc(smem_u32(smem) + PG_OPERAND, BMN);
       constexpr uint64_t ka = AMN ? 2048 >> 4 : 2, kb = BMN ? 2048 >> 4 : 2;      // 16 K values on
       uint32_t s = 0, parity = 0, g = 0;
@@ -350,8 +351,12 @@ struct EpiF32 {
   }
 };
 
+// 2^p, which may be beyond fp32, as two factors: v 2^p is v a b, exact but where the result is below 2^-126.
+__device__ __forceinline__ float2 two_powers(int p) { return make_float2(scalbnf(1.f, p / 2), scalbnf(1.f, p - p / 2)); }
+__device__ __forceinline__ float times(float v, float2 power) { return v * power.x * power.y; }
+
 // bf16 results, to a TMA map or (where rows are not 16-byte aligned) element by element;
-// with `first`, row r's sum gets the fp32 row first[r] of `more` added.
+// with `first`, row r's sum gets the fp32 row first[r] of `more` added; with `power`, it is multiplied by power[r].
 struct EpiBf16 {
   struct Params {
     __nv_bfloat16* c;      // null: TMA
@@ -360,6 +365,7 @@ struct EpiBf16 {
     const int* first;
     const float* more;
     int64_t ldmore;
+    const float2* power;
   };
   __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, float (&acc)[128], const CUtensorMap* map) {
     if (E.first && O.row < E.rows) {
@@ -370,6 +376,11 @@ struct EpiBf16 {
         for (int u = 0; u < 128; ++u)
           if (u < O.cols && O.col + u < E.cols) acc[u] += more[O.col + u];
       }
+    }
+    if (E.power && O.row < E.rows) {
+      const float2 power = E.power[O.row];
+#pragma unroll
+      for (int u = 0; u < 128; ++u) acc[u] = times(acc[u], power);
     }
     __syncwarp();
 #pragma unroll
@@ -404,7 +415,7 @@ struct EpiBf16 {
 };
 
 // ------------------------------------------------------------------ host side
-// A row-major matrix of bf16 (or fp32: `planes` of them) in boxes of box_cols x box_rows.
+// A row-major matrix of 16-bit values (or fp32: `planes` of them) in boxes of box_cols x box_rows.
 inline bool pair_map(CUtensorMap* map, bool f32, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_cols,
                      int box_rows, int planes = 0) {
   if (!get_encode()) return false;
