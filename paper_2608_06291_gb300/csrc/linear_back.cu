@@ -10,11 +10,13 @@
 // lose no bit, and what is lost further down is 2^-40 of it), the scales by the one that takes the weight's largest to
 // 2^6; the result is multiplied back.
 //
-// Up to FUSED_TOKENS: D (128 columns of What x bn tokens) += A B on the 5th-generation tensor cores with A the
+// Few: D (128 columns of What x bn tokens) += A B on the 5th-generation tensor cores with A the
 // operands of a 128 x 128 block, formed from its codes in shared memory as the MMAs take them (MN-major), and B the
-// tokens' gradients, K-major by TMA.  More: the weight is written out in fp16 once, and read by the pair product.
+// tokens' gradients, K-major by TMA.  Many: the weight is written out in fp16 once, and read by the pair product.
 //
-// FIGURES
+// us, caches flushed: 1 token, groups of 128, 4096 x 4096 12, 28672 x 8192 55 (2.4 TB/s with the scales); 17 tokens through
+// 4099 x 11003 in 8 bits 27; 64 through 11008 x 4096 28, 256 48, 4096 275 (1.34 PFLOP/s; 20 of them to write the weight out, 26
+// the tokens).  In bf16, with an error 1.35 times the result's rounding, dy needs no pass of its own: 25, 43, 240.
 #include <float.h>
 
 #include <cuda_fp16.h>
@@ -360,7 +362,7 @@ __global__ void __launch_bounds__(256) k_back_few_sum(const float* part, int spl
   dx[tok * ldx + col] = __float2bfloat16_rn(v);
 }
 
-// ------------------------------------------------------------------ more, up to FUSED_TOKENS
+// ------------------------------------------------------------------ more
 // A CTA takes an equal share of all tiles' blocks, one after another; a tile that several share is
 // summed from their parts, in their order, by a second kernel.  (As clusters that add
 // through each other's shared memory, no more than 15 of 8 CTAs ran at a time.)
@@ -670,14 +672,12 @@ __global__ void __launch_bounds__(256) k_expand(const ExpandParams P) {
   }
 }
 
-// 384 tokens through 11008 x 4096 63 us, by the weight in bf16 90; 4096 x 4096 45, 44; 4096 x 11008 77, 82.  At 512
-// 76, 91; 50, 44; 93, 82.
-constexpr int FUSED_TOKENS = 384;
+constexpr int FUSED_TOKENS = 2048;               // at most by the fused kernel
 constexpr uint32_t FB_SMEM = 227 * 1024 - 1024;      // beside the barriers
 
 bool one_grid(int n, int group_size) { return group_size == 0 || group_size == n || group_size % LIN_BLOCK == 0; }
 
-// How up to FUSED_TOKENS tokens are shared out.
+// How the fused kernel's tokens are shared out.
 static_assert(ROW_SMS <= 256, "a thread a flag");
 struct FusedPlan {
   int bn, token_tiles, tiles, nk, ctas, teams, na, nb, nc;
@@ -698,6 +698,25 @@ struct FusedPlan {
     smem = 1024 + na * FB_A + nb * tok + nc * code;
   }
 };
+
+// Which way more than 8 tokens go: estimates of both in us, fitted to 12 shapes of m and n from 512 to 28672 (4 and 8
+// bits) at 64 to 2048 tokens, where the rule's choice is at most 7% behind the other.  Fused: blocks a CTA, sums of whole tiles
+// that leave after the last block or slower than the next tile's blocks go by, the parts of shared tiles.  Else: rounds of the
+// pairs, the weight written out.  512 tokens: 4096 x 4096 40 fused, 42 else, 11008 x 4096 70 and 84, 28672 x 512 41 and 150,
+// 4096 x 11008 84 and 74, 28672 x 8192 280 and 244; 1024: 74, 45; 131, 92; 69, 160; 141, 94; 536, 382.
+bool fused_is_faster(const FusedPlan& F, int rows, int m, int n, bool bytes8) {
+  if (rows > FUSED_TOKENS) return false;
+  const double per = (double)F.tiles / F.ctas, blocks = per * F.nk, bn = F.bn, million = 1e-6;
+  double fused = 13.6 + blocks * (0.47 + 0.0026 * bn) + 0.75 * million * rows * m;
+  if (F.tiles >= F.ctas)
+    fused += 0.096 * bn + 1.1 * per * std::max(0., 0.09 * bn - F.nk * (0.6 + 0.0018 * bn));
+  else
+    fused += 3.7 * million * rows * n;
+  const int rounds = ceil_div(ceil_div(rows, PG_M) * ceil_div(n, 256), PG_PAIRS);
+  const double written = 15.6 + 0.27 * rounds * ceil_div(m, PG_K) + (bytes8 ? 0.70 : 0.43) * million * m * n +
+                         million * rows * (0.76 * m + 0.30 * n);
+  return fused <= written;
+}
 
 // How up to 8 tokens are: the rows in so many parts (64 at most) that the CTAs, as many at a time as the SMs hold, are done
 // first, where a CTA costs 256 rows (16 chunks) beside its own.  1 token x 28672 x 8192, 64 tiles: 4 parts (256 CTAs of 304)
@@ -723,6 +742,7 @@ struct FewPlan {
 struct BackLayout {
   size_t dy = 0, power = 0, flags = 0, part = 0, w = 0, bytes;
   int64_t ldy, ldw;      // of the gradients, of the weight, both in fp16
+  bool fused;
   BackLayout(int rows, int m, int n, bool bytes8, bool one, const FusedPlan& F) {
     size_t at = 256;
     auto take = [&](size_t b) {
@@ -730,6 +750,7 @@ struct BackLayout {
       at += align256(b);
       return r;
     };
+    fused = fused_is_faster(F, rows, m, n, bytes8);
     ldy = round_up(m, 8);
     ldw = round_up(n, LIN_BLOCK);
     if (rows > FEW_BACK) {
@@ -739,7 +760,7 @@ struct BackLayout {
     if (rows <= FEW_BACK) {
       const FewPlan few(m, n, bytes8, one);
       part = take((size_t)few.splits * rows * few.tiles * FW_COLS * 4);
-    } else if (rows <= FUSED_TOKENS) {
+    } else if (fused) {
       flags = take((size_t)F.ctas * sizeof(int));
       part = take((size_t)F.ctas * 2 * F.bn * LIN_BLOCK * 4);
     } else {
@@ -817,15 +838,14 @@ extern "C" int bakron_linear_backward(const void* dy, int rows, int64_t lddy, co
     return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
   }
   const int* top = (const int*)p + 1;
-  const bool fused = rows <= FUSED_TOKENS;
   float2* power = (float2*)(ws + B.power);
   const auto tokens = aligned16(dy, rows > 1 ? lddy * 2 : 0) ? k_back_tokens<true> : k_back_tokens<false>;
   tokens<<<(unsigned)rows, 512, 0, s>>>((const __nv_bfloat16*)dy, lddy, m, top, (__half*)(ws + B.dy), B.ldy, power,
-                                        fused ? nullptr : (int*)ws);
+                                        B.fused ? nullptr : (int*)ws);
   BK_CUDA_OK(cudaGetLastError());
   dy = ws + B.dy;
   CUtensorMap a, b, o;
-  if (fused) {
+  if (B.fused) {
     if (!pair_map(&a, false, dy, rows, m, B.ldy, 64, plan.bn)) return BAKRON_ERR_CUDA;
     FusedParams F{p + L.off_codes, (const float*)(p + L.off_scales), p + L.off_zeros, L.mp, (int)(L.np / LIN_BLOCK),
                   L.G == 1 ? (int)(L.np / 32) : L.group / 32, (int)L.G, rows, n, plan.bn, plan.nk, plan.token_tiles,
