@@ -539,8 +539,9 @@ int bakron_linear(const void* x, int xdtype, int rows, int64_t ldx, const float*
  *            first word is the status of this call
  *   sync     as for bakron_linear
  * The sum runs over rows of different scales, so these multiply an operand.  Up to 8 tokens c - z is
- * exact and dy s is kept to 2^-15; above, s (c - z) is rounded to bf16 (within 2^-16 of half a step)
- * before it is multiplied.  Sums are fp32, in a fixed order, and the result is rounded once.
+ * exact and dy s is kept to 2^-15.  Above, s (c - z) is rounded to fp16 (2^-11 of it; where a scale is
+ * below 2^-20 of the weight's largest, 2^-31 of that one) and dy is exact (below 2^-32 of its token's
+ * largest, to 2^-40 of that one).  Sums are fp32, in a fixed order, and the result is rounded once.
  */
 size_t bakron_linear_backward_workspace_bytes(const void* dy, int rows, int64_t lddy, int m,
                                               int n, int qmax, int group_size);
@@ -654,8 +655,8 @@ int bakron_token_logprobs_backward(const void* logits, int dtype, int rows, int 
  *            first word is the status of this call
  *   sync     as for bakron_linear
  * Products of bf16 values are exact and their sums fp32.  Rows and matrices that start on 16 bytes
- * (base and stride) are read as they lie; others are copied into the workspace first.  A row of h
- * that holds a NaN or an infinity affects its own results alone (they are then no finite numbers).
+ * (base and stride) are read as they lie; others are copied into the workspace first.  Infinite logits are
+ * as for bakron_token_logprobs.  A row of h that holds a NaN or an infinity affects its own results alone.
  */
 size_t bakron_head_logprobs_workspace_bytes(const void* h, int64_t ldh, const void* weight,
                                             int64_t ldw, int rows, int v, int d);

@@ -30,7 +30,8 @@ namespace bakron {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float LOWEST = -1e38f;      // stands for -inf, so that differences stay finite
+// What logits are taken relative to: their maximum, or 0 where that is -inf.
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 constexpr int NO_TOKEN = 0x7fffffff;
 
 __device__ __forceinline__ float exp2_fast(float v) {      // 2 ulp, results below 2^-126 are 0
@@ -60,13 +61,13 @@ struct EpiLse {
   };
   __device__ static __forceinline__ void tile(const Params& E, const PairOut& O, float (&acc)[128], const CUtensorMap*) {
     const int cols = min(O.cols, E.v - O.col);      // may be none
-    float m = LOWEST;
+    float m = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 128; ++u) {
-      if (u >= cols) acc[u] = LOWEST;
-      acc[u] = max_nan(acc[u], LOWEST);
+      if (u >= cols) acc[u] = -INFINITY;
       m = max_nan(m, acc[u]);
     }
+    const float base = base_of(m);
     if (O.row < E.rows && E.targets) {
       const int64_t at = E.targets[O.row] - O.col;
       if (at >= 0 && at < cols) E.picked[O.row] = column(acc, (int)at);
@@ -74,7 +75,7 @@ struct EpiLse {
     float s[4] = {}, x[4] = {};
 #pragma unroll
     for (int u = 0; u < 128; ++u) {
-      const float t = max_nan((acc[u] - m) * LOG2E, -126.f), e = exp2_fast(t);
+      const float t = max_nan((acc[u] - base) * LOG2E, -126.f), e = exp2_fast(t);
       if (u < cols) {
         s[u & 3] += e;
         x[u & 3] = fmaf(e, t, x[u & 3]);
@@ -102,9 +103,10 @@ struct JoinParams {
 
 // What the parts' triples give together: (m, s, x) of two is that of the larger maximum.
 struct Triple {
-  float m = LOWEST, s = 0.f, x = 0.f;
+  float m = -INFINITY, s = 0.f, x = 0.f;
   __device__ __forceinline__ void add(float m2, float s2, float x2) {
-    const float top = max_nan(m, m2), a = max_nan((m - top) * LOG2E, -126.f), b = max_nan((m2 - top) * LOG2E, -126.f);
+    const float top = max_nan(m, m2), base = base_of(top);
+    const float a = max_nan((m - base) * LOG2E, -126.f), b = max_nan((m2 - base) * LOG2E, -126.f);
     const float wa = exp2_fast(a), wb = exp2_fast(b);
     x = fmaf(wa, fmaf(s, a, x), wb * fmaf(s2, b, x2));
     s = fmaf(wa, s, wb * s2);
@@ -123,12 +125,13 @@ __device__ __forceinline__ void head_status(const JoinParams& P) {
   if (threadIdx.x == 0 && (bad || !P.more)) *P.status = bad ? BAKRON_ERR_TIMEOUT : 0;
 }
 __device__ __forceinline__ void head_result(const JoinParams& P, const Triple& t, int row) {
-  const float ls = logf(t.s), lse = t.m + ls;
+  const bool none = t.m == -INFINITY;      // no logit but -inf
+  const float ls = logf(t.s), lse = none ? -INFINITY : t.m + ls;
   P.lse[row] = lse;
-  P.entropy[row] = ls - LN2 * (t.x / t.s);
+  P.entropy[row] = none ? 0.f : ls - LN2 * (t.x / t.s);
   if (P.logp) {
     const int64_t at = P.targets[row];
-    P.logp[row] = at >= 0 && at < P.v ? P.picked[row] - lse : 0.f;
+    P.logp[row] = at < 0 || at >= P.v ? 0.f : none ? -INFINITY : P.picked[row] - lse;
   }
 }
 
@@ -206,6 +209,7 @@ struct EpiGrad {
         u = E.dentropy[O.row];
         ent = E.entropy[O.row];
       }
+      if (lse == -INFINITY) lse = g = u = ent = 0.f;      // no logit but -inf: zeros
     }
     if (at >= 0 && at < O.cols) {      // g (1 - p), without the difference
       const float lp = max_nan(column(acc, at) - lse, -87.f);
