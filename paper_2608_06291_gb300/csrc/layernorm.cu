@@ -80,8 +80,8 @@ __global__ void __launch_bounds__(AHEAD || VPT > 1 ? 512 : 1024, AHEAD && VPT * 
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        h[i][j] -= mu;
-        if (inside<VEC>(i, j, t, nt, P.d)) ss = fmaf(h[i][j], h[i][j], ss);
+        h[i][j] = inside<VEC>(i, j, t, nt, P.d) ? h[i][j] - mu : 0.f;      // (0 - mu) rho may be infinite
+        ss = fmaf(h[i][j], h[i][j], ss);
       }
     ss = cta_all(ss, AddOp(), slots[turn][1]);
     const float rho = 1.f / sqrtf(ss / (float)P.d + P.eps);
