@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const Layer
     s1.get(mg, hi);
     mg += hi;
     two_all(mu, mg, slots[0]);
-    mu *= inv;
+    mu /= (float)P.d;      // as the norm has it: a product with 1 / d may miss a constant row's value
     mg *= inv;
     const Two minus_mu(-mu, -mu);
 #pragma unroll
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(1024) k_layernorm_back_wide(const LayerBackPar
       }
     }
     two_all(mu, mg, slots[0]);
-    mu *= inv;
+    mu /= (float)P.d;      // as the norm has it: a product with 1 / d may miss a constant row's value
     mg *= inv;
     float ss = 0.f, gc = 0.f;
 #pragma unroll
@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(1024) k_layernorm_dx(const LayerBackParams P) 
     }
   }
   two_all(mu, mg, slots[0]);
-  mu *= inv;
+  mu /= (float)P.d;      // as the norm has it
   mg *= inv;
 #pragma unroll 4
   for (int e = threadIdx.x * N; e < P.d; e += step) {
