@@ -590,7 +590,9 @@ int bakron_rmsnorm_backward(const void* dy, int64_t lddy, const void* h, int64_t
  * row, var(h) the mean of (h - mean(h))^2.  Arguments as for bakron_rmsnorm, and
  *   bias     device, d values, bdtype BAKRON_F32 or BAKRON_BF16, or NULL: none
  * All in fp32, the mean before the squares; y comes from the unrounded h.  A row that holds a NaN
- * or an infinity gives NaNs; in 8 bits a NaN scale too.  eps 0 and a constant row: NaNs.
+ * or an infinity gives NaNs; in 8 bits a NaN scale too.  A sum of squares beyond fp32's largest number
+ * (entries of some 1e19) counts as infinite: y is the bias.  eps 0 and a row whose mean leaves nothing of
+ * it: NaNs.
  */
 int bakron_layernorm(const void* x, int dtype, int rows, int d, int64_t ldx,
                      const void* residual, int64_t ldr, const void* weight, int wdtype,
@@ -604,6 +606,7 @@ int bakron_layernorm(const void* x, int dtype, int rows, int d, int64_t ldx,
  *   db = sum over rows of dy
  * Arguments as for bakron_rmsnorm_backward, and
  *   db       device, d fp32, written (zeros for no rows); summed in a fixed order
+ * A row whose sum of squares counts as infinite adds nothing to dw, and its dx is dsum.
  */
 size_t bakron_layernorm_backward_workspace_bytes(int rows, int d);
 int bakron_layernorm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh,
