@@ -679,8 +679,9 @@ int bakron_head_logprobs(const void* h, int64_t ldh, const void* weight, int64_t
  *   workspace device, >= bakron_head_logprobs_backward_workspace_bytes(...) bytes (weight_grad:
  *            whether dweight is given), 16-byte aligned; its first word is the status of this call
  *   sync     as for bakron_linear
- * G's entries are rounded to bf16 but for each token's own target, which stays in fp32; sums are
- * fp32, in a fixed order, and each result is rounded once.
+ * G's entries are rounded to bf16 (of up to 128 tokens kept to 2^-15, in two bf16 parts) but for each
+ * token's own target, which stays in fp32; sums are fp32, in a fixed order, and each result is rounded
+ * once.
  */
 size_t bakron_head_logprobs_backward_workspace_bytes(const void* h, int64_t ldh,
                                                      const void* weight, int64_t ldw, int rows,

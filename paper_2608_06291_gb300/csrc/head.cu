@@ -15,12 +15,12 @@
 //
 // Backward: the vocabulary goes in pieces.  A piece's logits are formed again, G of the
 // piece is written in bf16 and multiplied by W's rows of the piece (a sum over pieces, in
-// fp32) and by h (the piece's rows of dW).  A token's own target is no part of that bf16 G: its
+// fp32) and by h (the piece's rows of dW); of up to 128 tokens in two bf16 parts.  A token's own target is no part of that bf16 G: its
 // entry, often as large as all the others together and much the same from token to token, would bring its
 // rounding to dh and dW.  It is kept in fp32 and joins the fp32 sums as a multiple of W's
 // (h's) row.  It is formed as -g expm1(log p), as p may be nearly 1.
-// 2048 x 128256 x 4096 with both gradients 3.87 ms (1.67 PFLOP/s); without dW few tokens read the
-// weight twice, 64 x 50021 x 2048 86 us (smaller pieces, read again from L2, 107 and more).
+// 2048 x 128256 x 4096 with both gradients 3.88 ms (1.66 PFLOP/s); without dW few tokens read the
+// weight twice, 64 x 50021 x 2048 96 us (G in one part 87; smaller pieces, read again from L2, 20 more).
 #include <algorithm>
 
 #include "linear.cuh"
@@ -186,6 +186,8 @@ __global__ void __launch_bounds__(1024) k_head_join(const JoinParams P) {
 // G of a tile from its logits, summed in the forward pass's groups: a logit is then the same number there
 // and here, and in l - lse, where lse is nearly the target's own logit when the model is sure of it, what
 // both have lost cancels.
+// TWO: G in two parts, hi in the first plane and lo in the second.
+template <bool TWO>
 struct EpiGrad {
   struct Params {
     const int64_t* targets;
@@ -218,27 +220,35 @@ struct EpiGrad {
 #pragma unroll
     for (int c = 0; c < 128; c += 64) {
       if (c >= O.cols) break;
-      stage_free(O.lane);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        uint32_t w[4];
+      for (int plane = 0; plane <= (int)TWO; ++plane) {
+        stage_free(O.lane);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float z[2];
+        for (int k = 0; k < 8; ++k) {
+          uint32_t w[4];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int i = c + 8 * k + 2 * j + e;
-            const float lp = max_nan(acc[i] - lse, -87.f), p = exp2_fast(lp * LOG2E);
-            z[e] = i == at ? 0.f : -p * fmaf(u, lp + ent, g);
+          for (int j = 0; j < 4; ++j) {
+            float* z = acc + c + 8 * k + 2 * j;
+            if (plane == 0) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float lp = max_nan(z[e] - lse, -87.f), p = exp2_fast(lp * LOG2E);
+                z[e] = c + 8 * k + 2 * j + e == at ? 0.f : -p * fmaf(u, lp + ent, g);
+              }
+            }
+            w[j] = bf16_pack(z[0], z[1]);
+            if (TWO && plane == 0) {
+              z[0] -= bf16_lo(w[j]);
+              z[1] -= bf16_hi(w[j]);
+            }
           }
-          w[j] = bf16_pack(z[0], z[1]);
+          *staged(O.stage, O.lane, k) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        *staged(O.stage, O.lane, k) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-      stage_ready();
-      if (O.lane == 0) {
-        tma_store_2d(map, O.stage, O.col + c, O.row0);
-        bulk_commit();
+        stage_ready();
+        if (O.lane == 0) {
+          tma_store_3d(map, O.stage, O.col + c, O.row0, plane);
+          bulk_commit();
+        }
       }
     }
   }
@@ -291,8 +301,8 @@ __global__ void __launch_bounds__(128) k_head_more(const int64_t* targets, const
     if (c0 + 128 * k < d) more[(int64_t)t * ldmore + c0 + 128 * k] = acc[k];
 }
 
-// dh = the parts' sum + own W[target], rounded once.  A thread has 4 columns.
-__global__ void __launch_bounds__(256) k_head_dh(const float* part, int splits, int64_t ldp, const int64_t* targets,
+// dh = the parts' sum (with two parts of G: of both) + own W[target], rounded once.  A thread has 4 columns.
+__global__ void __launch_bounds__(256) k_head_dh(const float* part, int splits, int planes, int64_t ldp, const int64_t* targets,
                                                  const float* own, const __nv_bfloat16* w, int64_t ldw, int rows,
                                                  int d, int v, __nv_bfloat16* dh, int64_t lddh, int vec) {
   pdl_wait();
@@ -304,7 +314,7 @@ __global__ void __launch_bounds__(256) k_head_dh(const float* part, int splits, 
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* from = part + row * ldp + c;      // (its rows are whole float4s)
 #pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
+    for (int s = 0; s < splits * planes; ++s) {
       const float4 u = *reinterpret_cast<const float4*>(from + (int64_t)s * rows * ldp);
       sum.x += u.x;
       sum.y += u.y;
@@ -326,6 +336,12 @@ __global__ void __launch_bounds__(256) k_head_dh(const float* part, int splits, 
   }
 }
 
+// h one below the other, for the two parts of G.
+__global__ void __launch_bounds__(256) k_head_twice(const __nv_bfloat16* h, int64_t ldh, int rows, int d, __nv_bfloat16* to, int64_t ldt) {
+  const __nv_bfloat16* from = h + (int64_t)(blockIdx.x % rows) * ldh;
+  for (int c = blockIdx.y * 256 + threadIdx.x; c < d; c += 256 * gridDim.y) to[blockIdx.x * ldt + c] = from[c];
+}
+
 // ------------------------------------------------------------------ host side
 constexpr int HEAD_MAX_ROWS = 1 << 24, HEAD_MAX_V = 1 << 24, HEAD_MAX_D = 1 << 16;
 constexpr int LSE_ROWS = 16384;        // tokens of one forward pass over the weight: bounds the triples
@@ -333,6 +349,10 @@ constexpr int LSE_ROWS = 16384;        // tokens of one forward pass over the we
 // additions.  2048 x 32768 x 4096 in place all the way 294 us and lse up to 3.8e-5 off, so 300 and 3.5e-6.
 constexpr int LSE_GROUP = 8;
 constexpr int64_t G_BYTES = 256 << 20; // of G kept at a time
+// Tokens up to which G is kept in two bf16 parts, rows one below the other: they fill a tile's rows, which cost nothing.  In one
+// part its rounding is as large as a result's own; over many tokens and a large vocabulary it averages out beside
+// the targets' entries, and two parts would take 3/5 more time.
+constexpr int TWO_PARTS = PG_M / 2;
 
 bool head_ok(int rows, int v, int d) {
   return rows >= 0 && rows <= HEAD_MAX_ROWS && v >= 1 && v <= HEAD_MAX_V && d >= 1 && d <= HEAD_MAX_D;
@@ -388,9 +408,9 @@ struct HeadLayout {
   }
 };
 struct HeadBackLayout {
-  size_t h = 0, w = 0, own, first = 0, tokens = 0, more = 0, g, part, bytes;
+  size_t h = 0, w = 0, twice = 0, own, first = 0, tokens = 0, more = 0, g, part, bytes;
   bool copy_h, copy_w;
-  int piece, splits;
+  int planes, piece, splits;      // parts of G
   int64_t ldg, ldp;      // of G, and of the fp32 sums
   HeadBackLayout(const void* ph, int64_t ldh, const void* pw, int64_t ldw, int rows, int v, int d, bool dw) {
     Carve c;
@@ -398,14 +418,16 @@ struct HeadBackLayout {
     copy_w = !in_place(pw, v, ldw);
     if (copy_h) h = c.take((size_t)rows * round_up(d, 8) * 2);
     if (copy_w) w = c.take((size_t)v * round_up(d, 8) * 2);
-    const int64_t most = std::max<int64_t>(256, G_BYTES / 2 / std::max(rows, 1) / 256 * 256);
+    planes = rows <= TWO_PARTS ? 2 : 1;
+    if (dw && planes == 2) twice = c.take((size_t)2 * rows * round_up(d, 8) * 2);
+    const int64_t most = std::max<int64_t>(256, G_BYTES / 2 / std::max(planes * rows, 1) / 256 * 256);
     const int pieces = (int)((v + most - 1) / most);
     piece = (int)std::min<int64_t>(v, round_up(ceil_div(v, pieces), 256));
     ldg = round_up(piece, 8);
     ldp = round_up(d, 4);
     // dh's sum runs over the piece in `splits` ranges: what the busiest pair takes, a range costing
     // some 4 blocks beside its own (2048 tokens x 128256 x 4096 by 2 ranges 4.00 ms forward and back, by 4 3.86)
-    const int64_t tiles = (int64_t)ceil_div(rows, PG_M) * ceil_div(d, 256);
+    const int64_t tiles = (int64_t)ceil_div(planes * rows, PG_M) * ceil_div(d, 256);
     const int nk = ceil_div(piece, PG_K);
     auto cost = [&](int s) { return (tiles * s + PG_PAIRS - 1) / PG_PAIRS * (ceil_div(nk, s) + 4); };
     splits = 1;
@@ -417,8 +439,8 @@ struct HeadBackLayout {
       tokens = c.take((size_t)v * 4);
       more = c.take((size_t)rows * ldp * 4);
     }
-    g = c.take((size_t)rows * ldg * 2);
-    part = c.take((size_t)splits * rows * ldp * 4);
+    g = c.take((size_t)planes * rows * ldg * 2);
+    part = c.take((size_t)splits * planes * rows * ldp * 4);
     bytes = c.at;
   }
 };
@@ -536,6 +558,16 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
     k_head_first<<<ceil_div(rows, 256), 256, 0, s>>>(targets, rows, v, first, tokens);
     BK_CUDA_OK(cudaGetLastError());
   }
+  const int grows = L.planes * rows;      // rows of G
+  const void* hg = h;                     // h for them
+  int64_t ldhg = ldh;
+  if (dweight && L.planes == 2) {
+    hg = ws + L.twice;
+    ldhg = round_up(d, 8);
+    k_head_twice<<<dim3((unsigned)grows, (unsigned)std::min(ceil_div(d, 512), 16)), 256, 0, s>>>((const __nv_bfloat16*)h, ldh, rows, d,
+                                                                                             (__nv_bfloat16*)hg, ldhg);
+    BK_CUDA_OK(cudaGetLastError());
+  }
   const bool dw_tma = dweight && in_place(dweight, v, lddw);
   for (int v0 = 0; v0 < v; v0 += L.piece) {
     const int count = std::min(v - v0, L.piece);
@@ -547,22 +579,26 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
     S.group = LSE_GROUP;
     if (!pair_map(&a, false, h, rows, d, map_ld(rows, ldh, d), PG_K, S.a_rows) ||
         !pair_map(&b, false, w, count, d, map_ld(count, ldw, d), PG_K, 128) ||
-        !pair_map(&o, false, G, rows, count, L.ldg, 64, 32))
+        !pair_map(&o, false, G, rows, count, L.ldg, 64, 32, L.planes))
       return BAKRON_ERR_CUDA;
-    EpiGrad::Params E{dlogp ? targets : nullptr, lse, dlogp, entropy, dentropy, own, rows, v, v0, count};
-    BK_CUDA_OK((pair_launch<EpiGrad, false, false>(a, b, o, S, E, s)));
+    auto g_of_piece = [&](auto epi) -> cudaError_t {
+      using Epi = decltype(epi);
+      const typename Epi::Params E{dlogp ? targets : nullptr, lse, dlogp, entropy, dentropy, own, rows, v, v0, count};
+      return pair_launch<Epi, false, false>(a, b, o, S, E, s);
+    };
+    BK_CUDA_OK(L.planes == 2 ? g_of_piece(EpiGrad<true>()) : g_of_piece(EpiGrad<false>()));
     // dh's part
-    S = head_shape(rows, 256, ceil_div(d, 256), ceil_div(count, PG_K), (int*)ws);
+    S = head_shape(grows, 256, ceil_div(d, 256), ceil_div(count, PG_K), (int*)ws);
     S.splits = L.splits;
     S.per = ceil_div(S.nk, S.splits);
     S.splits = ceil_div(S.nk, S.per);
-    if (!pair_map(&a, false, G, rows, count, L.ldg, PG_K, S.a_rows) ||
+    if (!pair_map(&a, false, G, grows, count, L.ldg, PG_K, S.a_rows) ||
         !pair_map(&b, false, w, count, d, map_ld(count, ldw, d), 64, PG_K) ||
-        !pair_map(&o, true, part, rows, d, L.ldp, 32, 32, L.splits))
+        !pair_map(&o, true, part, grows, d, L.ldp, 32, 32, L.splits))
       return BAKRON_ERR_CUDA;
     if (S.splits < L.splits && v0 == 0)      // no part of the rest: zeros
-      BK_CUDA_OK(cudaMemsetAsync(part + (int64_t)S.splits * rows * L.ldp, 0,
-                                 (size_t)(L.splits - S.splits) * rows * L.ldp * 4, s));
+      BK_CUDA_OK(cudaMemsetAsync(part + (int64_t)S.splits * grows * L.ldp, 0,
+                                 (size_t)(L.splits - S.splits) * grows * L.ldp * 4, s));
     BK_CUDA_OK((pair_launch<EpiF32, false, true>(a, b, o, S, EpiF32::Params{v0 > 0}, s)));
     if (!dweight) continue;
     // the piece's rows of dW
@@ -572,17 +608,17 @@ extern "C" int bakron_head_logprobs_backward(const void* h, int64_t ldh, const v
       BK_CUDA_OK(cudaGetLastError());
     }
     __nv_bfloat16* c = (__nv_bfloat16*)dweight + v0 * lddw;
-    S = head_shape(count, 256, ceil_div(d, 256), ceil_div(rows, PG_K), (int*)ws);
+    S = head_shape(count, 256, ceil_div(d, 256), ceil_div(grows, PG_K), (int*)ws);
     S.band = 8;
-    if (!pair_map(&a, false, G, rows, count, L.ldg, 64, PG_K) ||
-        !pair_map(&b, false, h, rows, d, map_ld(rows, ldh, d), 64, PG_K) ||
+    if (!pair_map(&a, false, G, grows, count, L.ldg, 64, PG_K) ||
+        !pair_map(&b, false, hg, grows, d, map_ld(grows, ldhg, d), 64, PG_K) ||
         (dw_tma && !pair_map(&o, false, c, count, d, map_ld(count, lddw, d), 64, 32)))
       return BAKRON_ERR_CUDA;
     EpiBf16::Params B{dw_tma ? nullptr : c, lddw, count, d, near ? first + v0 : nullptr, more, L.ldp};
     BK_CUDA_OK((pair_launch<EpiBf16, true, true>(a, b, dw_tma ? o : a, S, B, s)));
   }
   BK_CUDA_OK(launch_pdl(k_head_dh, dim3((unsigned)rows, (unsigned)std::min(ceil_div(d, 1024), 8)), dim3(256), 0, s, part,
-                        L.splits, L.ldp, dlogp ? targets : nullptr, own, (const __nv_bfloat16*)weight, ldw, rows, d, v,
+                        L.splits, L.planes, L.ldp, dlogp ? targets : nullptr, own, (const __nv_bfloat16*)weight, ldw, rows, d, v,
                         (__nv_bfloat16*)dh, lddh, (int)(((uintptr_t)dh | (uintptr_t)(rows > 1 ? lddh * 2 : 0)) % 8 == 0)));
   return sync ? bakron_read_status(workspace, stream) : BAKRON_OK;
 }
