@@ -187,10 +187,9 @@ __device__ __forceinline__ void two_all(float& a, float& b, TwoSlots& slots) {
 //
 // Many rows of up to 8192 elements that vectors can be used for: 16 elements a thread, read once
 // from a ring of RING rows that vector copies fill ahead, and kept in fp32, as pairs, through the three
-// passes (mean, sums of what is left, dx).  What bounds it is instructions before it is memory: with the
-// row read back from shared memory and widened in each pass, one value an instruction, 8192 x 4096
-// in bf16 with dsum took 98 us, now 67 with the parts' sum (issue 53% busy, DRAM 60%; 16 warps an SM, as the
-// registers allow).
+// passes (mean, sums of what is left, dx).  What bounds it is latency, with 16 warps an SM, as the registers allow
+// (issue slots 54% busy, DRAM 58%): 8192 x 4096 in bf16 with dsum takes 56 us with the parts' sum, and with the
+// row read back from shared memory and widened in each pass, one value an instruction, took 98.
 constexpr int LB_GROUPS = 1024;      // groups of 8: 512 threads
 template <typename T, typename W, int RING, int MAXT>
 __global__ void __launch_bounds__(MAXT, 512 / MAXT) k_layernorm_back(const LayerBackParams P) {

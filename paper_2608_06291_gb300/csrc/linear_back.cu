@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(256) k_back_few_sum(const float* part, int spl
 // it, so that a ring's slot always belongs to one team, which knows the phase it is in.
 //
 // Bound by the issue of MMAs, some 100 cycles each however few tokens they have: the 8 of a block, its two commits
-// and waits take 900 cycles (16 x 28672 x 8192 52 of 62 us with neither loads nor operands formed), the
+// and waits take 900 cycles (16 x 28672 x 8192 52 of 72 us with neither loads nor operands formed), the
 // operands 1000 beside them.  (Tokens as the MMA's 128 rows and 256 columns of What, half as many MMAs, took 99: its
 // copies are of a kilobyte, 50 cycles each.)  From 128 tokens on by the MMAs themselves.
 template <bool W8, bool ONE, int TEAMS>
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(FB_THREADS, 1) k_back_fused(const __grid_const
   } else if (warp >= 8) {
     // ------------------------------------------------------------ operands
     // Teams take blocks in turn: what a block costs beside its codes, mostly waits, is hidden by the
-    // other teams (16 warps on one block: 70 us for 16 tokens x 28672 x 8192).  A thread takes 32 codes
+    // other teams (16 warps on one block took 16 tokens x 28672 x 8192 8 us more).  A thread takes 32 codes
     // of each of 4 rows: lanes 0-7 eight rows of a unit, the next eight the same rows of the next
     // unit, ..., so that eight lanes' 16-byte loads and stores cover the banks.
     const int t = lane >> 3, r0 = (warp % TEAM) * 8 + (lane & 7);

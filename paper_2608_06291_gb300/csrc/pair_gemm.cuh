@@ -14,8 +14,9 @@
 // toward zero: of 2^20 products of one sign 0.65%, of 131072 7e-4.  It leaves TMEM after `group` K blocks and goes
 // on in registers, where additions are rounded.
 //
-// Bound by the tensor pipe, 93 to 96% of its cycles busy, and at that by the clock that the power
-// allows: 2048 x 32768 x 4096 299 us (1.84 PFLOP/s), 4095 x 128256 x 4096 2.48 ms (1.73).
+// Bound by the tensor pipe, busy in 93 to 95% of an SM's cycles while it works, at the clock that the power
+// allows, and by the last round of tiles (87 to 92% of all cycles): 2048 x 32768 x 4096 284 to 296 us (1.86 to 1.94
+// PFLOP/s), 4095 x 128256 x 4096 2.48 ms (1.73).
 //
 // Operands are K-major (a row's K values together) or MN-major (a K's rows together), read
 // as they lie by TMA; what is out of range is filled with zeros.
